@@ -420,6 +420,122 @@ typedef struct {
 ncodec_status ncodec_timing_enable(ncodec_ctx* ctx, int32_t enable);
 ncodec_status ncodec_timing_read(ncodec_ctx* ctx, ncodec_kernel_timing* out, int32_t max_kinds, int32_t* n_kinds);
 
+/* ---- Token operators ------------------------------------------------------
+ * What a mixer over latent tokens is made of: a learned temporal prior that
+ * sees more of the past than the previous frame.  A token is one position
+ * (t, h, w) of the 1/16 latent grid.  Matrix products with their epilogue, the
+ * norms of queries and keys with the rotation by the token's position, and
+ * attention whose memory of all earlier tokens is a state of fixed size.
+ *
+ * These calls need no context.  Each enqueues on hip_stream (a hipStream_t;
+ * NULL = default stream) on the current device, allocates nothing, clears
+ * nothing and never synchronises, so it may be captured into a graph.
+ * Elements are IEEE binary16 or bfloat16 (ncodec_dtype), device pointers need
+ * the alignment of an element only (16-byte aligned rows are faster), and
+ * strides count elements.  A zero count of rows, tokens or sequences is a call
+ * that does nothing.  EINVAL: a null pointer, enum or value out of range;
+ * ESHAPE: a size or stride out of range; ENOMEM: workspace too small or
+ * misaligned; EHIP: a HIP call failed.  ncodec_last_error(NULL) gives the
+ * message.  Outputs must not overlap inputs unless stated. */
+typedef enum { NCODEC_DTYPE_FP16 = 0, NCODEC_DTYPE_BF16 = 1 } ncodec_dtype;
+
+/* Activations: v; max(v, 0.1 v); v sigmoid(4 v); v sigmoid(v); v Phi(v). */
+typedef enum {
+  NCODEC_ACT_NONE = 0,
+  NCODEC_ACT_LRELU = 1,
+  NCODEC_ACT_WSILU = 2,
+  NCODEC_ACT_SILU = 3,
+  NCODEC_ACT_GELU = 4
+} ncodec_act;
+
+/* y = act(x W^T + b) + r, or with the gate (W = [W1; W2], 2n rows, b likewise)
+ * y = act(x W1^T + b1) * (x W2^T + b2) + r.  x is m x k, W n x k (gated 2n x k),
+ * y and r m x n, all row-major with the row strides ldx >= k, ldw >= k, ldy >= n,
+ * ldr >= n.  Products are summed in fp32, and everything after them is fp32 up
+ * to the one rounding of y.  b and r may be NULL.  y may be r itself
+ * (same pointer and ldy = ldr), otherwise it overlaps nothing.
+ * m in [0, 2^31), n and k in [1, 2^20]. */
+typedef struct {
+  int32_t dtype; /* ncodec_dtype */
+  int32_t act;   /* ncodec_act */
+  int32_t gated; /* 0 or 1 */
+  int32_t reserved; /* 0 */
+  int64_t m, n, k;
+  int64_t ldx, ldw, ldr, ldy;
+} ncodec_linear_shape;
+
+ncodec_status ncodec_linear(const ncodec_linear_shape* shape, const void* d_x, const void* d_w, const void* d_b,
+                            const void* d_r, void* d_y, void* hip_stream);
+
+/* RMS norm of each head of q and k, x / sqrt(mean(x^2) + eps) * w (norm = 1;
+ * d_wq and d_wk head_dim weights each, NULL: ones; norm = 0: none), and then
+ * the rotation by the token's position.  A head's first 2 P dimensions are P
+ * pairs, (p, p + P), or (2p, 2p + 1) with interleaved = 1; dimensions past 2 P
+ * are not rotated.  The pairs are given to the axes in order, section[a] to
+ * axis a (sections past `axes` must be 0; P = their sum, at most head_dim / 2),
+ * and pair p of axis a is turned by pos[token][a] * freq[p] radians:
+ * (u, v) -> (u cos - v sin, u sin + v cos).  d_pos: tokens x axes int32,
+ * d_freq: P float32.  The angle is formed and reduced in 64 bits, so it stays
+ * exact at any position.  axes = 0: no rotation (d_pos, d_freq ignored).
+ * q: tokens x q_heads x head_dim at q_token_stride, q_head_stride (the last
+ * dimension is contiguous), k, and both outputs likewise; q_heads or k_heads
+ * may be 0.  Outputs may be the inputs themselves (same pointer and
+ * strides).  head_dim in [1, 256], heads in [0, 4096], tokens in [0, 2^31). */
+typedef struct {
+  int32_t dtype;
+  int32_t norm;
+  int32_t axes; /* 0 .. 3 */
+  int32_t section[3];
+  int32_t interleaved;
+  int32_t q_heads, k_heads, head_dim;
+  float eps;
+  int32_t reserved; /* 0 */
+  int64_t tokens;
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+  int64_t qo_token_stride, qo_head_stride, ko_token_stride, ko_head_stride;
+} ncodec_qk_shape;
+
+ncodec_status ncodec_qk_norm_rope(const ncodec_qk_shape* shape, const void* d_q, const void* d_k, const void* d_wq,
+                                  const void* d_wk, const int32_t* d_pos, const float* d_freq, void* d_qo, void* d_ko,
+                                  void* hip_stream);
+
+/* Linear attention with a decay for each head, lambda_h = exp(log_decay[h]):
+ *   S_t = lambda_h S_{t-1} + k_t v_t^T,   o_t = scale * q_t S_t
+ * over each sequence of a batch (the present token is part of its own
+ * output).  q: batch x tokens x heads x head_dim, k and v: batch x tokens x
+ * kv_heads x head_dim (value_dim), o: batch x tokens x heads x value_dim, each at
+ * its batch, token and head strides, the last dimension contiguous.  Query
+ * head h reads key head h / (heads / kv_heads).  d_log_decay: heads float32,
+ * values above 0 are taken as 0, -inf keeps nothing.  d_lengths: batch int32, the
+ * tokens of each sequence, clamped to [0, tokens]; NULL: all.  Past its length a
+ * sequence's inputs are not used, its outputs are zero and its state stands
+ * still.  d_state_in: batch x heads x head_dim x value_dim float32, contiguous,
+ * the state before the first token (NULL: zero); d_state_out: the state after
+ * the last one (NULL: not wanted), may be d_state_in itself.
+ * tokens = 1 is the recurrent form of a stream that goes on token by token.
+ * head_dim and value_dim in [1, 128], heads and kv_heads in [1, 4096],
+ * batch * heads < 2^24, tokens in [0, 2^31). */
+typedef struct {
+  int32_t dtype;
+  int32_t heads, kv_heads, head_dim, value_dim;
+  float scale;
+  int64_t batch, tokens;
+  int64_t q_batch_stride, q_token_stride, q_head_stride;
+  int64_t k_batch_stride, k_token_stride, k_head_stride;
+  int64_t v_batch_stride, v_token_stride, v_head_stride;
+  int64_t o_batch_stride, o_token_stride, o_head_stride;
+} ncodec_decay_shape;
+
+/* Bytes of workspace (256-byte aligned device memory) that the call needs,
+ * which may be 0 (then the workspace may be NULL); 0 for an invalid shape too.
+ * Its content matters to no later call.  Pure host function. */
+size_t ncodec_decay_attention_workspace_bytes(const ncodec_decay_shape* shape);
+
+ncodec_status ncodec_decay_attention(const ncodec_decay_shape* shape, const void* d_q, const void* d_k, const void* d_v,
+                                     const float* d_log_decay, const int32_t* d_lengths, const float* d_state_in,
+                                     float* d_state_out, void* d_o, void* d_workspace, size_t ws_bytes,
+                                     void* hip_stream);
+
 /* Message for the last error on ctx (or the last create failure if ctx is NULL). */
 const char* ncodec_last_error(const ncodec_ctx* ctx);
 

@@ -17,6 +17,8 @@ CVPR 2025):
                       interleaved rANS streams (Fig. 4 "AE"/"AD", Fig. 6).
 * ``hyperprior``   -- the two-step entropy model with the hyper latent z
                       (Sec. 4.4; supplementary "Entropy model").
+* ``tokens``       -- the token operators: product with epilogue, head norms with
+                      rotation, attention with a decay (imported by itself).
 * ``params``       -- its own reading of the canonical flat parameter list.
 
 Parity status of each function is stated in its docstring; every function is

@@ -51,6 +51,34 @@ class ncodec_kernel_timing(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_char * 16), ("launches", ctypes.c_int32), ("total_ms", ctypes.c_double)]
 
 
+# token operators: element types and activations
+NCODEC_DTYPE_FP16, NCODEC_DTYPE_BF16 = 0, 1
+ACTS = {"none": 0, "lrelu": 1, "wsilu": 2, "silu": 3, "gelu": 4}
+
+
+class ncodec_linear_shape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "act", "gated", "reserved")]
+                + [(n, ctypes.c_int64) for n in ("m", "n", "k", "ldx", "ldw", "ldr", "ldy")])
+
+
+class ncodec_qk_shape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "norm", "axes")] + [("section", ctypes.c_int32 * 3)]
+                + [(n, ctypes.c_int32) for n in ("interleaved", "q_heads", "k_heads", "head_dim")]
+                + [("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
+                + [(n, ctypes.c_int64) for n in (
+                    "tokens", "q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
+                    "qo_token_stride", "qo_head_stride", "ko_token_stride", "ko_head_stride")])
+
+
+class ncodec_decay_shape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "heads", "kv_heads", "head_dim", "value_dim")]
+                + [("scale", ctypes.c_float)]
+                + [(n, ctypes.c_int64) for n in (
+                    "batch", "tokens", "q_batch_stride", "q_token_stride", "q_head_stride", "k_batch_stride",
+                    "k_token_stride", "k_head_stride", "v_batch_stride", "v_token_stride", "v_head_stride",
+                    "o_batch_stride", "o_token_stride", "o_head_stride")])
+
+
 class NcodecError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"ncodec status {status}: {message}")
@@ -87,6 +115,11 @@ _SIGNATURES = {
     "ncodec_block_chain_status": (ctypes.c_int, [_P, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]),
     "ncodec_timing_read": (ctypes.c_int, [_P, ctypes.POINTER(ncodec_kernel_timing), ctypes.c_int32,
                                           ctypes.POINTER(ctypes.c_int32)]),
+    "ncodec_linear": (ctypes.c_int, [ctypes.POINTER(ncodec_linear_shape)] + [_P] * 6),
+    "ncodec_qk_norm_rope": (ctypes.c_int, [ctypes.POINTER(ncodec_qk_shape)] + [_P] * 9),
+    "ncodec_decay_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(ncodec_decay_shape)]),
+    "ncodec_decay_attention": (ctypes.c_int, [ctypes.POINTER(ncodec_decay_shape)] + [_P] * 9
+                               + [ctypes.c_size_t, _P]),
     "ncodec_last_error": (ctypes.c_char_p, [_P]),
     "ncodec_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "ncodec_destroy": (None, [_P]),
@@ -252,6 +285,30 @@ def ncodec_timing_read(ctx) -> dict:
     n = ctypes.c_int32(0)
     _check(load_library().ncodec_timing_read(ctx, buf, 32, ctypes.byref(n)), ctx)
     return {buf[i].kind.decode(): (int(buf[i].launches), float(buf[i].total_ms)) for i in range(min(n.value, 32))}
+
+
+def ncodec_linear(shape: ncodec_linear_shape, d_x: int, d_w: int, d_b: int, d_r: int, d_y: int,
+                  stream: int = 0) -> None:
+    _check(load_library().ncodec_linear(ctypes.byref(shape), _p(d_x), _p(d_w), _p(d_b), _p(d_r), _p(d_y),
+                                        stream or None))
+
+
+def ncodec_qk_norm_rope(shape: ncodec_qk_shape, d_q: int, d_k: int, d_wq: int, d_wk: int, d_pos: int, d_freq: int,
+                        d_qo: int, d_ko: int, stream: int = 0) -> None:
+    _check(load_library().ncodec_qk_norm_rope(ctypes.byref(shape), _p(d_q), _p(d_k), _p(d_wq), _p(d_wk), _p(d_pos),
+                                              _p(d_freq), _p(d_qo), _p(d_ko), stream or None))
+
+
+def ncodec_decay_attention_workspace_bytes(shape: ncodec_decay_shape) -> int:
+    return int(load_library().ncodec_decay_attention_workspace_bytes(ctypes.byref(shape)))
+
+
+def ncodec_decay_attention(shape: ncodec_decay_shape, d_q: int, d_k: int, d_v: int, d_log_decay: int, d_lengths: int,
+                           d_state_in: int, d_state_out: int, d_o: int, d_workspace: int = 0, ws_bytes: int = 0,
+                           stream: int = 0) -> None:
+    _check(load_library().ncodec_decay_attention(ctypes.byref(shape), _p(d_q), _p(d_k), _p(d_v), _p(d_log_decay),
+                                                 _p(d_lengths), _p(d_state_in), _p(d_state_out), _p(d_o),
+                                                 _p(d_workspace), ws_bytes, stream or None))
 
 
 def ncodec_last_error(ctx=None) -> str:
