@@ -3,6 +3,7 @@
 // Computed transposed like the codec's pointwise kernels: the weight rows are
 // the MFMA A operand, the tokens are the columns, and a lane of the
 // accumulator holds one token and four consecutive features at a time.
+// Operands are read as they lie in memory: nothing is packed beforehand.
 #include "tokens.hpp"
 
 namespace nc {
@@ -13,7 +14,7 @@ namespace {
 // rounding of y); v Phi(v) goes through erfc, whose fit is relative, so the
 // tail keeps its digits.
 template <int ACT>
-__device__ __forceinline__ float activate(float v) {
+__device__ __forceinline__ float act1(float v) {
   if (ACT == NCODEC_ACT_LRELU) return v >= 0.f ? v : 0.1f * v;
   if (ACT == NCODEC_ACT_WSILU) return v * __builtin_amdgcn_rcpf(1.f + __expf(-4.f * v));
   if (ACT == NCODEC_ACT_SILU) return v * __builtin_amdgcn_rcpf(1.f + __expf(-v));
@@ -23,82 +24,352 @@ __device__ __forceinline__ float activate(float v) {
   }
   return v;
 }
-
-constexpr int kTile = 64, kStep = 64, kPitch = kStep + 8;
-
-// 64 tokens x 64 features a workgroup, four waves of 32 x 32.
-template <class E, int ACT, bool GATED>
-__global__ __launch_bounds__(256) void k_tok_linear(LinearArgs a) {
-  typedef typename E::T T;
-  typedef typename E::V8 V8;
-  __shared__ __align__(16) T xs[kTile * kPitch];
-  __shared__ __align__(16) T wsm[(GATED ? 2 : 1) * kTile * kPitch];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int tm = (wave & 1) * 32, tn = (wave >> 1) * 32;
-  const int64_t nt = (a.s.n + kTile - 1) / kTile;
-  const int64_t m0 = (int64_t)(blockIdx.x / nt) * kTile, n0 = (int64_t)(blockIdx.x % nt) * kTile;
-  const T* x = (const T*)a.x;
-  const T* w = (const T*)a.w;
-  floatx16 acc[GATED ? 2 : 1] = {};
-  for (int64_t k0 = 0; k0 < a.s.k; k0 += kStep) {
-    for (int i = threadIdx.x; i < kTile * kStep; i += 256) {
-      const int row = i / kStep, kk = i % kStep;
-      const bool in = k0 + kk < a.s.k;
-      xs[row * kPitch + kk] = in && m0 + row < a.s.m ? x[(m0 + row) * a.s.ldx + k0 + kk] : (T)0.f;
-#pragma unroll
-      for (int g = 0; g < (GATED ? 2 : 1); ++g)
-        wsm[(g * kTile + row) * kPitch + kk] =
-            in && n0 + row < a.s.n ? w[(g * a.s.n + n0 + row) * a.s.ldw + k0 + kk] : (T)0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int s = 0; s < kStep; s += 16) {
-      const int kk = s + 8 * (lane >> 5);
-      const V8 b = *(const V8*)&xs[(tm + (lane & 31)) * kPitch + kk];
-#pragma unroll
-      for (int g = 0; g < (GATED ? 2 : 1); ++g)
-        acc[g] = E::mfma(*(const V8*)&wsm[(g * kTile + tn + (lane & 31)) * kPitch + kk], b, acc[g]);
-    }
-    __syncthreads();
-  }
-  const int64_t m = m0 + tm + (lane & 31);
-  if (m >= a.s.m) return;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int64_t n = n0 + tn + drow(r, lane >> 5);
-    if (n >= a.s.n) continue;
-    float v = acc[0][r] + (a.b ? (float)((const T*)a.b)[n] : 0.f);
-    v = activate<ACT>(v);
-    if (GATED) v *= acc[1][r] + (a.b ? (float)((const T*)a.b)[a.s.n + n] : 0.f);
-    if (a.r) v += (float)((const T*)a.r)[m * a.s.ldr + n];
-    ((T*)a.y)[m * a.s.ldy + n] = (T)v;
+// act is uniform over the launch, so the branch is a scalar one.
+template <int N>
+__device__ __forceinline__ void activate(float (&v)[N], int act) {
+  switch (act) {
+#define NC_CASE(A)                                      \
+  case A:                                               \
+    _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = act1<A>(v[i]); \
+    break;
+    NC_CASE(NCODEC_ACT_LRELU)
+    NC_CASE(NCODEC_ACT_WSILU)
+    NC_CASE(NCODEC_ACT_SILU)
+    NC_CASE(NCODEC_ACT_GELU)
+#undef NC_CASE
+    default: break;
   }
 }
 
-template <class E, int ACT, bool GATED>
-hipError_t go(const LinearArgs& a, hipStream_t st) {
-  const int64_t grid = ((a.s.m + kTile - 1) / kTile) * ((a.s.n + kTile - 1) / kTile);
+template <class V>
+__device__ __forceinline__ V load_any(const void* p) {  // any alignment
+  V v;
+  __builtin_memcpy(&v, p, sizeof(V));
+  return v;
+}
+template <class V>
+__device__ __forceinline__ void store_any(void* p, V v) {
+  __builtin_memcpy(p, &v, sizeof(V));
+}
+// Eight elements of a row from k on, zeros past its end (rem = K - k).
+template <class E>
+__device__ __forceinline__ typename E::V8 load_row8(const typename E::T* p, int64_t rem) {
+  if (rem >= 8) return load_any<typename E::V8>(p);
+  typename E::V8 v = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < rem) v[i] = p[i];
+  return v;
+}
+
+__device__ __align__(16) uint32_t zero16[4];  // what a load past the end of the contraction reads
+
+// ---- tiles ------------------------------------------------------------------
+// WN x WM waves of 64 weight rows x 32 TB tokens each.  K streams through LDS
+// in stages of 32 (a row's stage is 64 bytes, four 16-byte units; unit u of row
+// r lies at slot u ^ (r / 4 % 4), so that 16 consecutive rows of one unit touch
+// every bank once).  DMA: rows 16-byte aligned and K a multiple of 8, staged by
+// direct global->LDS loads two stages ahead; otherwise through registers.
+// With the gate each 64-row group holds 32 rows of W1 and the same 32 of W2.
+constexpr int kBK = 32;
+
+template <class E, bool GATED, bool DMA, int WN, int WM, int TB>
+struct Tile {
+  static constexpr int NW = WN * WM, TN = 64 * WN, TM = 32 * TB * WM, ROWS = TN + TM;
+  static constexpr int OF = GATED ? 32 : 64;       // output features of a wave
+  static constexpr int ST = DMA ? 3 : 2;
+  static constexpr int STAGE = ROWS * kBK * 2;     // bytes
+  static constexpr int LOADS = ROWS / 16 / NW;     // 1 KiB loads of a wave and stage
+  static constexpr int PITCH = OF * 2 + 16;        // bytes of a token's row in the epilogue
+  static constexpr int LDS = ST * STAGE > NW * 32 * PITCH ? ST * STAGE : NW * 32 * PITCH;
+  static_assert(ROWS / 16 % NW == 0, "every wave stages the same number of rows");
+};
+
+template <class E, bool GATED, bool DMA, int WN, int WM, int TB>
+__global__ __launch_bounds__(64 * WN * WM, 2) void k_tok_linear(LinearArgs a) {
+  typedef Tile<E, GATED, DMA, WN, WM, TB> C;
+  typedef typename E::T T;
+  typedef typename E::V8 V8;
+  typedef typename E::V4 V4;
+  __shared__ __align__(1024) char lds[C::LDS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, l32 = lane & 31;
+  const int wn = wave % WN, wm = wave / WN;
+  const int K = (int)a.s.k;
+  // token tiles of one XCD follow each other, all feature tiles of a token tile together
+  const uint32_t nt = (uint32_t)((a.s.n + C::OF * WN - 1) / (C::OF * WN));
+  const uint32_t tile = xcd_tile(blockIdx.x, gridDim.x);
+  const int64_t m0 = (int64_t)(tile / nt) * C::TM, n0 = (int64_t)(tile % nt) * (C::OF * WN);
+  if (m0 >= a.s.m) return;  // the grid is rounded up to the XCDs
+
+  // this lane's source of each staged unit
+  const T* src[C::LOADS];
+  int kof[C::LOADS];
+#pragma unroll
+  for (int i = 0; i < C::LOADS; ++i) {
+    const int row = 16 * (wave + C::NW * i) + (lane >> 2);
+    const int unit = (lane & 3) ^ ((row >> 2) & 3);
+    if (row < C::TN) {
+      int64_t n = GATED ? n0 + 32 * (row >> 6) + (row & 31) : n0 + row;
+      n = min(n, a.s.n - 1);
+      if (GATED && (row & 32)) n += a.s.n;
+      src[i] = (const T*)a.w + n * a.s.ldw + 8 * unit;
+    } else {
+      const int64_t m = min(m0 + row - C::TN, a.s.m - 1);
+      src[i] = (const T*)a.x + m * a.s.ldx + 8 * unit;
+    }
+    kof[i] = 8 * unit;
+  }
+  const int nk = (K + kBK - 1) / kBK;
+  auto stage_dma = [&](int kt, int buf) {
+    const bool tail = (kt + 1) * kBK > K;
+#pragma unroll
+    for (int i = 0; i < C::LOADS; ++i) {
+      const void* p = src[i] + (int64_t)kt * kBK;
+      if (tail && kt * kBK + kof[i] >= K) p = zero16;
+      dma16(p, lds + buf * C::STAGE + 1024 * (wave + C::NW * i));
+    }
+  };
+
+  floatx16 acc[2][TB] = {};
+  auto compute = [&](int buf) {
+    const char* base = lds + buf * C::STAGE;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      V8 fa[2], fb[TB];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = 64 * wn + 32 * i + l32;
+        fa[i] = *(const V8*)(base + row * 64 + (((2 * s + h) ^ ((row >> 2) & 3)) << 4));
+      }
+#pragma unroll
+      for (int t = 0; t < TB; ++t) {
+        const int row = C::TN + 32 * (TB * wm + t) + l32;
+        fb[t] = *(const V8*)(base + row * 64 + (((2 * s + h) ^ ((row >> 2) & 3)) << 4));
+      }
+#pragma unroll
+      for (int t = 0; t < TB; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) acc[i][t] = E::mfma(fa[i], fb[t], acc[i][t]);
+    }
+  };
+
+  if (DMA) {
+    stage_dma(0, 0);
+    if (nk > 1) stage_dma(1, 1);
+    int buf = 0;
+    for (int kt = 0; kt < nk; ++kt) {
+      // this wave's loads of stage kt have landed (those of kt + 1 may be in flight) ...
+      if (kt + 1 < nk)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(C::LOADS) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      // ... and everyone's, and everyone is done with the buffer that stage kt + 2 goes to
+      lds_barrier();
+      if (kt + 2 < nk) stage_dma(kt + 2, buf == 0 ? 2 : buf - 1);
+      compute(buf);
+      buf = buf == 2 ? 0 : buf + 1;
+    }
+  } else {
+    V8 reg[C::LOADS];
+    auto fetch = [&](int kt) {
+#pragma unroll
+      for (int i = 0; i < C::LOADS; ++i) reg[i] = load_row8<E>(src[i] + (int64_t)kt * kBK, K - kt * kBK - kof[i]);
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+      for (int i = 0; i < C::LOADS; ++i)
+        *(V8*)(lds + buf * C::STAGE + 1024 * (wave + C::NW * i) + 16 * lane) = reg[i];
+    };
+    fetch(0);
+    put(0);
+    for (int kt = 0; kt < nk; ++kt) {
+      if (kt + 1 < nk) fetch(kt + 1);
+      __syncthreads();
+      compute(kt & 1);
+      if (kt + 1 < nk) put((kt + 1) & 1);
+    }
+  }
+  lds_barrier();  // the stages are read; each wave's part of LDS is its own from here on
+
+  // Epilogue, 32 tokens at a time: results (and the residual before them) go
+  // through LDS so that global accesses are whole 16-byte units of a row.
+  char* mine = lds + wave * 32 * C::PITCH;
+  constexpr int UNITS = C::OF / 8;            // 16-byte units of a token's row
+  constexpr int RPI = 64 / UNITS;             // tokens an instruction covers
+  constexpr int ITER = 32 / RPI;
+  const int eu = lane % UNITS, er = lane / UNITS;
+  const int64_t nw0 = n0 + C::OF * wn, mw0 = m0 + 32 * TB * wm;
+  const int64_t ne = nw0 + 8 * eu;            // first feature of this lane's unit
+  const int nval = (int)min(max(a.s.n - ne, (int64_t)0), (int64_t)8);
+  const T* bias = (const T*)a.b;
+  const T* res = (const T*)a.r;
+  T* y = (T*)a.y;
+  auto get_bias = [&](int64_t n, int64_t half, float (&v)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = bias && n + j < a.s.n ? (float)bias[half + n + j] : 0.f;
+  };
+#pragma unroll
+  for (int t = 0; t < TB; ++t) {
+    const int64_t mt = mw0 + 32 * t;
+    if (res) {
+#pragma unroll
+      for (int it = 0; it < ITER; ++it) {
+        const int64_t m = mt + RPI * it + er;
+        V8 v = {};
+        if (m < a.s.m) v = load_row8<E>(res + m * a.s.ldr + ne, nval);
+        *(V8*)(mine + (RPI * it + er) * C::PITCH + 16 * eu) = v;
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+#pragma unroll
+    for (int i = 0; i < (GATED ? 1 : 2); ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int f = 32 * i + 8 * q + 4 * h;  // first of the lane's four features
+        float v[4], bv[4];
+        get_bias(nw0 + f, 0, bv);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = acc[i][t][4 * q + j] + bv[j];
+        activate(v, a.s.act);
+        if (GATED) {
+          get_bias(nw0 + f, a.s.n, bv);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] *= acc[1][t][4 * q + j] + bv[j];
+        }
+        V4* slot = (V4*)(mine + l32 * C::PITCH + 2 * f);
+        if (res) {
+          const V4 r4 = *slot;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] += (float)r4[j];
+        }
+        V4 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = (T)v[j];
+        *slot = o;
+      }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int it = 0; it < ITER; ++it) {
+      const int64_t m = mt + RPI * it + er;
+      const V8 o = *(const V8*)(mine + (RPI * it + er) * C::PITCH + 16 * eu);
+      if (m < a.s.m) {
+        T* p = y + m * a.s.ldy + ne;
+        if (nval == 8)
+          store_any(p, o);
+        else
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j < nval) p[j] = o[j];
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// ---- few rows -----------------------------------------------------------------
+// 16 features x 16 TB tokens a workgroup; its eight waves take turns along K
+// (32 at a time, both operands straight from memory) and their partial sums
+// meet in LDS in wave order.  The weights are read once and the launch is wide
+// enough to read them from every CU.
+__device__ __forceinline__ floatx4 mfma16(half8 a, half8 b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx4 mfma16(bhalf8 a, bhalf8 b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+template <class E, bool GATED, int TB>
+__global__ __launch_bounds__(512) void k_tok_linear_rows(LinearArgs a) {
+  typedef typename E::T T;
+  typedef typename E::V8 V8;
+  constexpr int G = GATED ? 2 : 1;
+  __shared__ float part[8][G][TB][16][17];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int l16 = lane & 15, kl = 8 * (lane >> 4);
+  const uint32_t nt = (uint32_t)((a.s.n + 15) / 16);
+  const int64_t m0 = (int64_t)(blockIdx.x / nt) * (16 * TB), n0 = (int64_t)(blockIdx.x % nt) * 16;
+  const int K = (int)a.s.k;
+  const T* wp = (const T*)a.w + min(n0 + l16, a.s.n - 1) * a.s.ldw;
+  const T* xp[TB];
+#pragma unroll
+  for (int t = 0; t < TB; ++t) xp[t] = (const T*)a.x + min(m0 + 16 * t + l16, a.s.m - 1) * a.s.ldx;
+  floatx4 acc[G][TB] = {};
+#pragma unroll 2
+  for (int k0 = 32 * wave; k0 < K; k0 += 256) {
+    const int k = k0 + kl;
+    V8 fa[G], fb[TB];
+#pragma unroll
+    for (int g = 0; g < G; ++g) fa[g] = load_row8<E>(wp + g * a.s.n * a.s.ldw + k, K - k);
+#pragma unroll
+    for (int t = 0; t < TB; ++t) fb[t] = load_row8<E>(xp[t] + k, K - k);
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+      for (int g = 0; g < G; ++g) acc[g][t] = mfma16(fa[g], fb[t], acc[g][t]);
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) part[wave][g][t][l16][4 * (lane >> 4) + r] = acc[g][t][r];
+  __syncthreads();
+  const T* bias = (const T*)a.b;
+  for (int i = threadIdx.x; i < 256 * TB; i += 512) {
+    const int f = i & 15, tok = i >> 4;
+    const int64_t m = m0 + tok, n = n0 + f;
+    if (m >= a.s.m || n >= a.s.n) continue;
+    float s[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      s[g] = 0.f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) s[g] += part[w][g][tok >> 4][tok & 15][f];
+      if (bias) s[g] += (float)bias[g * a.s.n + n];
+    }
+    float v[1] = {s[0]};
+    activate(v, a.s.act);
+    if (GATED) v[0] *= s[G - 1];
+    if (a.r) v[0] += (float)((const T*)a.r)[m * a.s.ldr + n];
+    ((T*)a.y)[m * a.s.ldy + n] = (T)v[0];
+  }
+}
+
+template <class E, bool GATED, bool DMA, int WN, int WM, int TB>
+hipError_t go_tile(const LinearArgs& a, hipStream_t st) {
+  typedef Tile<E, GATED, DMA, WN, WM, TB> C;
+  int64_t grid = ((a.s.m + C::TM - 1) / C::TM) * ((a.s.n + C::OF * WN - 1) / (C::OF * WN));
+  grid = (grid + kNumXCD - 1) / kNumXCD * kNumXCD;
   if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
-  launch(k_tok_linear<E, ACT, GATED>, dim3((unsigned)grid), dim3(256), st, a);
+  launch(k_tok_linear<E, GATED, DMA, WN, WM, TB>, dim3((unsigned)grid), dim3(64 * C::NW), st, a);
+  return hipGetLastError();
+}
+
+template <class E, bool GATED, int TB>
+hipError_t go_rows(const LinearArgs& a, hipStream_t st) {
+  const int64_t grid = ((a.s.m + 16 * TB - 1) / (16 * TB)) * ((a.s.n + 15) / 16);
+  launch(k_tok_linear_rows<E, GATED, TB>, dim3((unsigned)grid), dim3(512), st, a);
   return hipGetLastError();
 }
 
 template <class E, bool GATED>
-hipError_t by_act(const LinearArgs& a, hipStream_t st) {
-  switch (a.s.act) {
-    case NCODEC_ACT_LRELU: return go<E, NCODEC_ACT_LRELU, GATED>(a, st);
-    case NCODEC_ACT_WSILU: return go<E, NCODEC_ACT_WSILU, GATED>(a, st);
-    case NCODEC_ACT_SILU: return go<E, NCODEC_ACT_SILU, GATED>(a, st);
-    case NCODEC_ACT_GELU: return go<E, NCODEC_ACT_GELU, GATED>(a, st);
-    default: return go<E, NCODEC_ACT_NONE, GATED>(a, st);
-  }
+hipError_t pick(const LinearArgs& a, hipStream_t st) {
+  const ncodec_linear_shape& s = a.s;
+  const int64_t nf = s.n * (GATED ? 2 : 1);
+  if (s.m <= 16) return go_rows<E, GATED, 1>(a, st);
+  if (s.m <= 128) return go_rows<E, GATED, 2>(a, st);
+  const bool dma = s.k % 8 == 0 && s.ldx % 8 == 0 && s.ldw % 8 == 0 && (uintptr_t)a.x % 16 == 0 && (uintptr_t)a.w % 16 == 0;
+  const int64_t big = ((s.m + 255) / 256) * ((nf + 127) / 128);
+  if (big >= 256) return dma ? go_tile<E, GATED, true, 2, 2, 4>(a, st) : go_tile<E, GATED, false, 2, 2, 4>(a, st);
+  return dma ? go_tile<E, GATED, true, 2, 2, 1>(a, st) : go_tile<E, GATED, false, 2, 2, 1>(a, st);
 }
 
 }  // namespace
 
 hipError_t launch_linear(const LinearArgs& a, hipStream_t st) {
-  if (a.s.dtype == NCODEC_DTYPE_FP16) return a.s.gated ? by_act<F16, true>(a, st) : by_act<F16, false>(a, st);
-  return a.s.gated ? by_act<BF16, true>(a, st) : by_act<BF16, false>(a, st);
+  if (a.s.dtype == NCODEC_DTYPE_FP16) return a.s.gated ? pick<F16, true>(a, st) : pick<F16, false>(a, st);
+  return a.s.gated ? pick<BF16, true>(a, st) : pick<BF16, false>(a, st);
 }
 
 }  // namespace nc
