@@ -1,5 +1,16 @@
 // Linear attention with a decay for each head:
 //   S_t = lambda S_{t-1} + k_t v_t^T,  o_t = scale q_t S_t.
+//
+// Two forms.  A few tokens run the recurrence itself.  Longer ones go in chunks
+// of 64 tokens, whose outputs are two products, one with the state before the
+// chunk and one inside the chunk,
+//   o_i = scale (lambda^(i+1) q_i S + sum_{j<=i} lambda^(i-j) (q_i . k_j) v_j),
+//   S' = lambda^n S + sum_j lambda^(n-1-j) k_j v_j^T,
+// all of them MFMA work.  Where there are too few heads to fill the chip a
+// sequence is cut into segments: their contributions to the state first (one
+// pass over k and v), then a scan over the segments, then the outputs.
+#include <algorithm>
+
 #include "tokens.hpp"
 
 namespace nc {
@@ -87,6 +98,486 @@ __global__ __launch_bounds__(256) void k_tok_decay_recur(DecayArgs a) {
   }
 }
 
+// ---- chunks -------------------------------------------------------------------
+constexpr int kChunk = 64;
+
+template <class E, int DP_, int NV_>
+struct Chunk {
+  static constexpr int DP = DP_, NV = NV_, VP = 32 * NV_;  // padded head and value width; a wave per 32 values
+  static constexpr int DT = DP / 32;
+  static constexpr int QB = kChunk * DP * 2, VB = kChunk * VP * 2;
+  static constexpr int STAGE = 2 * QB + VB;  // q, k, v of a chunk
+  static constexpr uint32_t INF = __is_same(E, F16) ? 0x7c00 : 0x7f80;
+  static constexpr int OPITCH = 80;          // a token's 32 outputs of a wave, padded
+  static constexpr int LDS = 2 * STAGE + NV * 32 * OPITCH;
+};
+
+// Slot of 16-byte unit u of a row of W elements: 16 consecutive rows of one
+// unit, and four consecutive rows of four units (a transposed read), each
+// touch every LDS bank once.
+template <int W>
+__device__ __forceinline__ int unit_slot(int row, int u) {
+  if (W == 128) return u ^ (((row & 3) << 2) | ((row >> 2) & 3));
+  if (W == 64) return u ^ ((((row >> 1) & 1) << 2) | ((row >> 2) & 3));
+  return u ^ ((row >> 2) & 3);
+}
+
+__device__ __align__(16) uint32_t decay_zero16[4];
+
+// Stage 64 rows of a tensor (d valid elements of W, n valid rows, zeros
+// elsewhere) into LDS.
+template <class E, int W, int NW>
+__device__ __forceinline__ void stage_rows(char* lds, const typename E::T* base, int64_t stride, int n, int d, bool dma,
+                                           int wave, int lane) {
+  typedef typename E::T T;
+  typedef typename E::V8 V8;
+  constexpr int U = W / 8, R = 64 / U, LOADS = kChunk / R;
+#pragma unroll
+  for (int i0 = 0; i0 < (LOADS + NW - 1) / NW; ++i0) {
+    const int i = wave + NW * i0;
+    if (LOADS % NW && i >= LOADS) break;
+    const int row = R * i + lane / U, u = unit_slot<W>(row, lane % U);
+    const T* p = base + row * stride + 8 * u;
+    if (dma) {
+      dma16(row < n && 8 * u < d ? (const void*)p : (const void*)decay_zero16, lds + 1024 * i);
+    } else {
+      V8 v = {};
+      if (row < n) {
+        if (8 * u + 8 <= d)
+          __builtin_memcpy(&v, p, 16);
+        else
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (8 * u + e < d) v[e] = p[e];
+      }
+      *(V8*)(lds + 1024 * i + 16 * lane) = v;
+    }
+  }
+}
+
+template <class E, int W>
+__device__ __forceinline__ typename E::V8 read_row8(const char* lds, int row, int u) {
+  return *(const typename E::V8*)(lds + row * (2 * W) + 16 * unit_slot<W>(row, u));
+}
+
+// Transposed read of four rows x 16 columns per 16 lanes: lane i of the 16
+// passes the address of element (i / 4, 4 (i % 4)) and receives column i of the
+// four rows.
+__device__ __forceinline__ half4 read_tr(const char* p, F16) {
+  typedef __fp16 H4 __attribute__((vector_size(8)));
+  typedef H4 __attribute__((address_space(3))) L;
+  return __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((L*)p));
+}
+__device__ __forceinline__ bhalf4 read_tr(const char* p, BF16) {
+  typedef bhalf4 __attribute__((address_space(3))) L;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((L*)p);
+}
+// MFMA fragment of 32 columns c0.. of an LDS tile as rows, contraction over its
+// rows ("tokens") in the order of an accumulator: lane half h, element e holds
+// token 16 s + 8 (e / 4) + 4 h + e % 4.  With PI the columns of each 16 are taken
+// as 0-3, 8-11, 4-7, 12-15, so that a lane of the resulting accumulator holds
+// eight consecutive columns in eight registers.
+template <class E, int W, bool PI>
+__device__ __forceinline__ typename E::V8 read_cols(const char* lds, int s, int c0, int lane) {
+  const int h = lane >> 5, c = (lane >> 4) & 1, i = lane & 15, k = i & 3;
+  const int col = c0 + 16 * c + 4 * (PI ? ((k & 1) << 1 | k >> 1) : k);
+  typename E::V8 v;
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const int row = 16 * s + 8 * p + 4 * h + (i >> 2);
+    const auto x = read_tr(lds + row * (2 * W) + 16 * unit_slot<W>(row, col >> 3) + 2 * (col & 7), E{});
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[4 * p + e] = x[e];
+  }
+  return v;
+}
+
+// max over all lanes
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  v = max(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(b[0], b[1]);
+#define NC_ROR(N) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + N, 0xf, 0xf, false));
+  NC_ROR(8) NC_ROR(4) NC_ROR(2) NC_ROR(1)
+#undef NC_ROR
+  return __builtin_amdgcn_readfirstlane(v);
+}
+// of a value >= 0 that is no NaN: its bits order it
+__device__ __forceinline__ float wave_max(float v) { return __uint_as_float(wave_max(__float_as_uint(v))); }
+template <class V8>
+__device__ __forceinline__ uint32_t max_bits(V8 v) {  // of eight 16-bit magnitudes
+  typedef unsigned short US8 __attribute__((ext_vector_type(8)));
+  typedef unsigned short US2 __attribute__((ext_vector_type(2)));
+  const US8 u = __builtin_bit_cast(US8, v) & (unsigned short)0x7fff;
+  US2 m = __builtin_elementwise_max(__builtin_elementwise_max(u.s01, u.s23), __builtin_elementwise_max(u.s45, u.s67));
+  return max((uint32_t)m.x, (uint32_t)m.y);
+}
+__device__ __forceinline__ float half_max(float v) {  // over the two lanes l, l + 32
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+// Power of two that takes a largest magnitude m into [2^14, 2^15), and its
+// inverse: fp16 operands are brought there, so that no sum of magnitudes and no
+// small scale leaves the range in which fp16 has its 11 bits.
+__device__ __forceinline__ float scale_up(float m, float* inverse) {
+  const uint32_t e = max((__float_as_uint(m) >> 23) & 255u, 15u);
+  *inverse = __uint_as_float((e - 14) << 23);
+  return __uint_as_float((268 - e) << 23);
+}
+
+struct Decay64 {  // lambda^n in two floats, so that long products of it lose nothing
+  float hi, lo;
+};
+__device__ __forceinline__ Decay64 decay_pow(float log_decay, int64_t n) {
+  const double l = fmax(fmin((double)log_decay, 0.0), -1e30);
+  const double f = exp((double)n * l);
+  const float hi = (float)f;
+  return {hi, (float)(f - (double)hi)};
+}
+
+struct SegArgs {
+  DecayArgs a;
+  int seg_chunks;  // chunks of a segment
+  int nseg;
+  bool dma;
+};
+
+// One segment of one sequence and head.  OUT: the outputs, from the state before
+// the segment (and the sequence's last state); otherwise only what the segment
+// adds to the state, into the workspace.  Wave w holds the state's columns
+// 32 w .. 32 w + 31 in its accumulators: register r of tile a and lane (h, c) is
+// row 32 a + 16 (r / 8) + 8 h + r % 8, column 32 w + c.
+template <class E, int DP, int NV, bool OUT>
+__global__ __launch_bounds__(64 * NV) void k_tok_decay_chunk(SegArgs sa) {
+  typedef Chunk<E, DP, NV> C;
+  typedef typename E::T T;
+  typedef typename E::V8 V8;
+  typedef typename E::V4 V4;
+  constexpr bool F = __is_same(E, F16);
+  constexpr int DT = C::DT, VP = C::VP, NT = F ? 2 : 3;  // NT: 16-bit terms of a weighted value
+  __shared__ __align__(1024) char lds[OUT ? C::LDS : 2 * (C::QB + C::VB)];
+  const DecayArgs& a = sa.a;
+  const ncodec_decay_shape& s = a.s;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, l32 = lane & 31;
+  const int nsg = OUT ? sa.nseg : sa.nseg - 1;
+  const int64_t bh = blockIdx.x / nsg;
+  const int seg = blockIdx.x % nsg;
+  const int64_t b = bh / s.heads, hd = bh % s.heads, hk = hd / (s.heads / s.kv_heads);
+  const int D = s.head_dim, V = s.value_dim;
+  const int64_t len = a.lengths ? min(max((int64_t)a.lengths[b], (int64_t)0), s.tokens) : s.tokens;
+  const int64_t SL = (int64_t)sa.seg_chunks * kChunk, t0 = seg * SL;
+  const int64_t tend = min(t0 + SL, len);  // tokens [t0, tend) are computed
+  const float log_decay = a.log_decay[hd];
+  const float l2 = log2_decay(log_decay);
+  const T* q = (const T*)a.q + b * s.q_batch_stride + hd * s.q_head_stride;
+  const T* k = (const T*)a.k + b * s.k_batch_stride + hk * s.k_head_stride;
+  const T* v = (const T*)a.v + b * s.v_batch_stride + hk * s.v_head_stride;
+  T* o = (T*)a.o + b * s.o_batch_stride + hd * s.o_head_stride;
+  const int64_t sdv = (int64_t)D * V;
+  const int col = 32 * wave + l32;
+
+  if (!OUT && t0 + SL >= len) return;  // no later segment reads it
+  if (OUT) {
+    // outputs past the sequence's end
+    const int64_t z0 = max(t0, len), z1 = min(t0 + SL, s.tokens);
+    for (int64_t t = z0 + (threadIdx.x / VP); t < z1; t += 64 * NV / VP)
+      if ((int)(threadIdx.x % VP) < V) o[t * s.o_token_stride + threadIdx.x % VP] = (T)0.f;
+    if (t0 >= len && seg > 0) return;
+  }
+
+  floatx16 S[DT];
+  const float* sin = !OUT ? nullptr : seg == 0 ? a.state_in : (const float*)a.ws + (bh * (sa.nseg - 1) + seg - 1) * sdv;
+  if (seg == 0 && sin) sin += bh * sdv;
+#pragma unroll
+  for (int x = 0; x < DT; ++x)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int d = 32 * x + 16 * (r >> 3) + 8 * h + (r & 7);
+      S[x][r] = sin && d < D && col < V ? sin[(int64_t)d * V + col] : 0.f;
+    }
+
+  // decays: inside a diagonal 32 x 32 tile lambda^(i - j) for j <= i (i this lane's
+  // token, j the register's), one tile below it lambda^(32 + i - j), and of
+  // token j at the end of a full chunk lambda^(63 - j)
+  float mdiag[OUT ? 16 : 1], mlow[OUT ? 16 : 1];
+  if (OUT) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int lag = l32 - drow(r, h);
+      mdiag[r] = lag >= 0 ? __builtin_amdgcn_exp2f(lag * l2) : 0.f;
+      mlow[r] = __builtin_amdgcn_exp2f((32 + lag) * l2);
+    }
+  }
+  const float di0 = __builtin_amdgcn_exp2f((l32 + 1) * l2), di1 = __builtin_amdgcn_exp2f((l32 + 33) * l2);
+  const Decay64 full = decay_pow(log_decay, kChunk);
+
+  const int nch = tend > t0 ? (int)((tend - t0 + kChunk - 1) / kChunk) : 0;
+  auto stage = [&](int c, int buf) {
+    const int64_t t = t0 + (int64_t)c * kChunk;
+    const int n = (int)min(tend - t, (int64_t)kChunk);
+    char* base = lds + buf * (OUT ? C::STAGE : C::QB + C::VB);
+    stage_rows<E, DP, NV>(base, k + t * s.k_token_stride, s.k_token_stride, n, D, sa.dma, wave, lane);
+    stage_rows<E, VP, NV>(base + C::QB, v + t * s.v_token_stride, s.v_token_stride, n, V, sa.dma, wave, lane);
+    if (OUT)
+      stage_rows<E, DP, NV>(base + C::QB + C::VB, q + t * s.q_token_stride, s.q_token_stride, n, D, sa.dma, wave, lane);
+  };
+  if (nch) stage(0, 0);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+
+  for (int c = 0; c < nch; ++c) {
+    // every wave's loads of chunk c have landed (each waited for its own), and
+    // every wave is done with the other buffer
+    lds_barrier();
+    if (c + 1 < nch) stage(c + 1, (c + 1) & 1);
+    const char* base = lds + (c & 1) * (OUT ? C::STAGE : C::QB + C::VB);
+    const char *ks = base, *vs = base + C::QB, *qs = base + C::QB + C::VB;
+    const int64_t t = t0 + (int64_t)c * kChunk;
+    const int n = (int)min(tend - t, (int64_t)kChunk);
+
+    V8 vf[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) vf[x] = read_cols<E, VP, false>(vs, x, 32 * wave, lane);
+    // largest magnitude, by its bits, which order finite values, infinities and NaN
+    uint32_t mb = 0;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) mb = max(mb, max_bits(vf[x]));
+    mb = wave_max(mb);
+    int bad = kChunk;  // first token of this lane's column that is not finite
+    if (mb >= C::INF) {
+      // a product would carry it to earlier tokens too (0 times NaN): it is taken
+      // out here and put into the outputs and the state that it reaches
+      mb = 0;
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t u = (uint32_t)__builtin_bit_cast(uint16_t, (T)vf[x][e]) & 0x7fffu;
+          if (u >= C::INF) {
+            bad = min(bad, 16 * x + 8 * (e >> 2) + 4 * h + (e & 3));
+            vf[x][e] = (T)0.f;
+          } else {
+            mb = max(mb, u);
+          }
+        }
+      mb = wave_max(mb);
+      bad = min(bad, __shfl_xor(bad, 32, 64));
+    }
+    float vinv = 1.f;
+    if (F) {  // a power of two, exact in fp16: what is lost lies 2^-24 below 2^14
+      const float m = fmaxf((float)__builtin_bit_cast(f16, (uint16_t)mb), 0.5f);
+      const float up = scale_up(m, &vinv);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) vf[x] = vf[x] * (T)up;
+    }
+
+    floatx16 out[2];
+    if (OUT) {
+      float sinv = 1.f, sup = 1.f;
+      if (F) {
+        float m = 0.f;
+#pragma unroll
+        for (int x = 0; x < DT; ++x)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) m = fmaxf(m, fabsf(S[x][r]));
+        m = wave_max(m);
+        if (m == __builtin_huge_valf()) {  // the finite ones keep their scale
+          m = 0.f;
+#pragma unroll
+          for (int x = 0; x < DT; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (fabsf(S[x][r]) < __builtin_huge_valf()) m = fmaxf(m, fabsf(S[x][r]));
+          m = wave_max(m);
+        }
+        sup = scale_up(m, &sinv);
+      }
+      V8 sf[2 * DT];
+#pragma unroll
+      for (int x = 0; x < 2 * DT; ++x)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sf[x][e] = (T)(S[x >> 1][8 * (x & 1) + e] * sup);
+#pragma unroll
+      for (int it = 0; it < 2; ++it) {
+        floatx16 p[2] = {}, inter = {};
+#pragma unroll
+        for (int x = 0; x < 2 * DT; ++x) {
+          const V8 qf = read_row8<E, DP>(qs, 32 * it + l32, 2 * x + h);
+#pragma unroll
+          for (int jt = 0; jt <= it; ++jt) p[jt] = E::mfma(read_row8<E, DP>(ks, 32 * jt + l32, 2 * x + h), qf, p[jt]);
+          inter = E::mfma(sf[x], qf, inter);
+        }
+        // pairs above the diagonal count nothing, whatever their product is
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (drow(r, h) > l32) p[it][r] = 0.f;
+        float pinv = 1.f, pup = 1.f;
+        if (F) {
+          float m = 0.f;
+#pragma unroll
+          for (int jt = 0; jt <= it; ++jt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) m = fmaxf(m, fabsf(p[jt][r]));
+          pup = scale_up(half_max(m), &pinv);
+        }
+        floatx16 intra = {};
+#pragma unroll
+        for (int jt = 0; jt <= it; ++jt) {
+          V8 pf[2];
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float w = jt == it ? mdiag[r] : mlow[r];
+            pf[r >> 3][r & 7] = (T)(p[jt][r] * pup * w);
+          }
+          intra = E::mfma(vf[2 * jt], pf[0], intra);
+          intra = E::mfma(vf[2 * jt + 1], pf[1], intra);
+        }
+        const float ci = s.scale * (it ? di1 : di0) * sinv, cp = s.scale * pinv * vinv;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) out[it][r] = fmaf(inter[r], ci, intra[r] * cp);
+      }
+      if (__any(bad < kChunk)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int from = __shfl(bad, drow(r, h), 64);
+#pragma unroll
+          for (int it = 0; it < 2; ++it)
+            if (32 * it + l32 >= from) out[it][r] = __builtin_nanf("");
+        }
+      }
+    }
+
+    // the state: v weighted by its age, as a sum of 16-bit terms that holds 22 (fp16)
+    // or 24 (bf16) bits, because the state is an fp32 output
+    const Decay64 keep = n == kChunk ? full : decay_pow(log_decay, n);
+    floatx16 add[DT] = {};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      V8 term[NT];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int age = n - 1 - (16 * x + 8 * (e >> 2) + 4 * h + (e & 3));
+        float w = (float)vf[x][e] * (age >= 0 ? __builtin_amdgcn_exp2f(age * l2) : 0.f);
+        // one value of the product for all terms: formed anew for a term (fused,
+        // rounded once instead of twice) it could differ from the one subtracted
+        asm("" : "+v"(w));
+#pragma unroll
+        for (int y = 0; y < NT; ++y) {
+          term[y][e] = (T)w;
+          w -= (float)term[y][e];
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const V8 kf = read_cols<E, DP, true>(ks, x, 32 * d, lane);
+#pragma unroll
+        for (int y = NT - 1; y >= 0; --y) add[d] = E::mfma(kf, term[y], add[d]);
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) S[d][r] = fmaf(S[d][r], keep.hi, fmaf(S[d][r], keep.lo, add[d][r] * vinv));
+    if (bad < kChunk) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[d][r] = __builtin_nanf("");
+    }
+
+    // the next chunk has landed before this one's stores are sent, so that
+    // nothing waits for them
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (OUT) {
+      char* mine = lds + 2 * C::STAGE + wave * 32 * C::OPITCH;
+#pragma unroll
+      for (int it = 0; it < 2; ++it) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          V4 x;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = (T)out[it][4 * g + j];
+          *(V4*)(mine + l32 * C::OPITCH + 16 * g + 8 * h) = x;
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int row = 16 * y + (lane >> 2), u = lane & 3;
+          const V8 x = *(const V8*)(mine + row * C::OPITCH + 16 * u);
+          const int left = V - (32 * wave + 8 * u);
+          if (32 * it + row < n && left > 0) {
+            T* p = o + (t + 32 * it + row) * s.o_token_stride + 32 * wave + 8 * u;
+            if (left >= 8)
+              __builtin_memcpy(p, &x, 16);
+            else
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (e < left) p[e] = x[e];
+          }
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+  }
+
+  float* sout = !OUT ? (float*)a.ws + (bh * (sa.nseg - 1) + seg) * sdv
+                : a.state_out && t0 + SL >= len ? a.state_out + bh * sdv : nullptr;
+  if (sout) {
+#pragma unroll
+    for (int x = 0; x < DT; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int d = 32 * x + 16 * (r >> 3) + 8 * h + (r & 7);
+        if (d < D && col < V) sout[(int64_t)d * V + col] = S[x][r];
+      }
+  }
+}
+
+// Over the segments of a sequence and head: what each adds becomes the state
+// after it (slot g: the state before segment g + 1).
+__global__ __launch_bounds__(256) void k_tok_decay_scan(SegArgs sa) {
+  const DecayArgs& a = sa.a;
+  const ncodec_decay_shape& s = a.s;
+  const int64_t sdv = (int64_t)s.head_dim * s.value_dim;
+  const int blocks = (int)((sdv + 255) / 256);
+  const int64_t bh = blockIdx.x / blocks, e = (int64_t)(blockIdx.x % blocks) * 256 + threadIdx.x;
+  if (e >= sdv) return;
+  const int64_t b = bh / s.heads;
+  const int64_t len = a.lengths ? min(max((int64_t)a.lengths[b], (int64_t)0), s.tokens) : s.tokens;
+  const int64_t SL = (int64_t)sa.seg_chunks * kChunk;
+  const Decay64 keep = decay_pow(a.log_decay[bh % s.heads], SL);
+  const int last = (int)min((len + SL - 1) / SL, (int64_t)sa.nseg) - 1;  // segment 0 .. last have tokens
+  float* ws = (float*)a.ws + bh * (sa.nseg - 1) * sdv + e;
+  float S = a.state_in ? a.state_in[bh * sdv + e] : 0.f;
+  for (int g = 0; g < last; ++g) {
+    S = fmaf(S, keep.hi, fmaf(S, keep.lo, ws[g * sdv]));
+    ws[g * sdv] = S;
+  }
+}
+
+// Sequences shorter than this run the recurrence (few workgroups, no chunk to fill).
+constexpr int64_t kRecurTokens = 8;
+
+struct Plan {
+  bool chunked;
+  int seg_chunks, nseg;
+};
+
+// Segments so that about kTargetWGs workgroups share the work.
+Plan plan_of(const ncodec_decay_shape& s) {
+  Plan p{s.tokens >= kRecurTokens, 0, 1};
+  const int64_t chunks = (s.tokens + kChunk - 1) / kChunk, bh = s.batch * s.heads;
+  if (!p.chunked || bh == 0) return p;
+  const int64_t target = s.head_dim > 64 || s.value_dim > 64 ? 256 : 512;
+  int64_t nseg = std::max<int64_t>(1, std::min(chunks, target / bh));
+  const int64_t per = (chunks + nseg - 1) / nseg;
+  p.seg_chunks = (int)per;
+  p.nseg = (int)((chunks + per - 1) / per);
+  return p;
+}
+
 template <class E>
 hipError_t recur(const DecayArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)(a.s.batch * a.s.heads), (unsigned)((a.s.value_dim + 63) / 64));
@@ -99,12 +590,53 @@ hipError_t recur(const DecayArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <class E, int DP, int NV>
+hipError_t chunked(const SegArgs& sa, hipStream_t st) {
+  const ncodec_decay_shape& s = sa.a.s;
+  const int64_t bh = s.batch * s.heads;
+  if (sa.nseg > 1) {
+    launch(k_tok_decay_chunk<E, DP, NV, false>, dim3((unsigned)(bh * (sa.nseg - 1))), dim3(64 * NV), st, sa);
+    const int64_t sdv = (int64_t)s.head_dim * s.value_dim;
+    launch(k_tok_decay_scan, dim3((unsigned)(bh * ((sdv + 255) / 256))), dim3(256), st, sa);
+  }
+  launch(k_tok_decay_chunk<E, DP, NV, true>, dim3((unsigned)(bh * sa.nseg)), dim3(64 * NV), st, sa);
+  return hipGetLastError();
+}
+
+template <class E, int DP>
+hipError_t by_value(const SegArgs& sa, hipStream_t st) {
+  if (sa.a.s.value_dim <= 32) return chunked<E, DP, 1>(sa, st);
+  if (sa.a.s.value_dim <= 64) return chunked<E, DP, 2>(sa, st);
+  return chunked<E, DP, 4>(sa, st);
+}
+
+template <class E>
+hipError_t run(const DecayArgs& a, hipStream_t st) {
+  const ncodec_decay_shape& s = a.s;
+  const Plan p = plan_of(s);
+  if (!p.chunked) return recur<E>(a, st);
+  const auto al = [](const void* x, int64_t u, int64_t v, int64_t w) {
+    return (uintptr_t)x % 16 == 0 && u % 8 == 0 && v % 8 == 0 && w % 8 == 0;
+  };
+  const bool dma = s.head_dim % 8 == 0 && s.value_dim % 8 == 0 &&
+                   al(a.q, s.q_batch_stride, s.q_token_stride, s.q_head_stride) &&
+                   al(a.k, s.k_batch_stride, s.k_token_stride, s.k_head_stride) &&
+                   al(a.v, s.v_batch_stride, s.v_token_stride, s.v_head_stride);
+  const SegArgs sa{a, p.seg_chunks, p.nseg, dma};
+  if (s.head_dim <= 32) return by_value<E, 32>(sa, st);
+  if (s.head_dim <= 64) return by_value<E, 64>(sa, st);
+  return by_value<E, 128>(sa, st);
+}
+
 }  // namespace
 
-size_t decay_workspace_bytes(const ncodec_decay_shape&) { return 0; }
+size_t decay_workspace_bytes(const ncodec_decay_shape& s) {
+  const Plan p = plan_of(s);
+  return (size_t)(s.batch * s.heads) * (size_t)(p.nseg - 1) * (size_t)(s.head_dim * s.value_dim) * 4;
+}
 
 hipError_t launch_decay_attention(const DecayArgs& a, hipStream_t st) {
-  return a.s.dtype == NCODEC_DTYPE_FP16 ? recur<F16>(a, st) : recur<BF16>(a, st);
+  return a.s.dtype == NCODEC_DTYPE_FP16 ? run<F16>(a, st) : run<BF16>(a, st);
 }
 
 }  // namespace nc

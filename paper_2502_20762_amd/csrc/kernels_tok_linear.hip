@@ -71,23 +71,23 @@ __device__ __align__(16) uint32_t zero16[4];  // what a load past the end of the
 // every bank once).  DMA: rows 16-byte aligned and K a multiple of 8, staged by
 // direct global->LDS loads two stages ahead; otherwise through registers.
 // With the gate each 64-row group holds 32 rows of W1 and the same 32 of W2.
-constexpr int kBK = 32;
-
-template <class E, bool GATED, bool DMA, int WN, int WM, int TB>
+template <class E, bool GATED, bool DMA, int WN, int WM, int TB, int BK = 32>
 struct Tile {
   static constexpr int NW = WN * WM, TN = 64 * WN, TM = 32 * TB * WM, ROWS = TN + TM;
   static constexpr int OF = GATED ? 32 : 64;       // output features of a wave
-  static constexpr int ST = DMA ? 3 : 2;
-  static constexpr int STAGE = ROWS * kBK * 2;     // bytes
-  static constexpr int LOADS = ROWS / 16 / NW;     // 1 KiB loads of a wave and stage
+  static constexpr int ST = DMA && BK == 32 ? 3 : 2;
+  static constexpr int STAGE = ROWS * BK * 2;      // bytes
+  static constexpr int U = BK / 8, RPL = 64 / U;   // units of a row, rows of a 1 KiB load
+  static constexpr int LOADS = ROWS / RPL / NW;    // 1 KiB loads of a wave and stage
+  static __device__ __forceinline__ int slot(int row, int u) { return u ^ (BK == 32 ? (row >> 2) & 3 : (row >> 1) & 7); }
   static constexpr int PITCH = OF * 2 + 16;        // bytes of a token's row in the epilogue
   static constexpr int LDS = ST * STAGE > NW * 32 * PITCH ? ST * STAGE : NW * 32 * PITCH;
-  static_assert(ROWS / 16 % NW == 0, "every wave stages the same number of rows");
+  static_assert(ROWS / RPL % NW == 0, "every wave stages the same number of rows");
 };
 
-template <class E, bool GATED, bool DMA, int WN, int WM, int TB>
+template <class E, bool GATED, bool DMA, int WN, int WM, int TB, int BK = 32>
 __global__ __launch_bounds__(64 * WN * WM, 2) void k_tok_linear(LinearArgs a) {
-  typedef Tile<E, GATED, DMA, WN, WM, TB> C;
+  typedef Tile<E, GATED, DMA, WN, WM, TB, BK> C;
   typedef typename E::T T;
   typedef typename E::V8 V8;
   typedef typename E::V4 V4;
@@ -107,8 +107,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tok_linear(LinearArgs a) {
   int kof[C::LOADS];
 #pragma unroll
   for (int i = 0; i < C::LOADS; ++i) {
-    const int row = 16 * (wave + C::NW * i) + (lane >> 2);
-    const int unit = (lane & 3) ^ ((row >> 2) & 3);
+    const int row = C::RPL * (wave + C::NW * i) + lane / C::U;
+    const int unit = C::slot(row, lane % C::U);
     if (row < C::TN) {
       int64_t n = GATED ? n0 + 32 * (row >> 6) + (row & 31) : n0 + row;
       n = min(n, a.s.n - 1);
@@ -120,13 +120,13 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tok_linear(LinearArgs a) {
     }
     kof[i] = 8 * unit;
   }
-  const int nk = (K + kBK - 1) / kBK;
+  const int nk = (K + BK - 1) / BK;
   auto stage_dma = [&](int kt, int buf) {
-    const bool tail = (kt + 1) * kBK > K;
+    const bool tail = (kt + 1) * BK > K;
 #pragma unroll
     for (int i = 0; i < C::LOADS; ++i) {
-      const void* p = src[i] + (int64_t)kt * kBK;
-      if (tail && kt * kBK + kof[i] >= K) p = zero16;
+      const void* p = src[i] + (int64_t)kt * BK;
+      if (tail && kt * BK + kof[i] >= K) p = zero16;
       dma16(p, lds + buf * C::STAGE + 1024 * (wave + C::NW * i));
     }
   };
@@ -135,17 +135,17 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tok_linear(LinearArgs a) {
   auto compute = [&](int buf) {
     const char* base = lds + buf * C::STAGE;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < BK / 16; ++s) {
       V8 fa[2], fb[TB];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int row = 64 * wn + 32 * i + l32;
-        fa[i] = *(const V8*)(base + row * 64 + (((2 * s + h) ^ ((row >> 2) & 3)) << 4));
+        fa[i] = *(const V8*)(base + row * (2 * BK) + 16 * C::slot(row, 2 * s + h));
       }
 #pragma unroll
       for (int t = 0; t < TB; ++t) {
         const int row = C::TN + 32 * (TB * wm + t) + l32;
-        fb[t] = *(const V8*)(base + row * 64 + (((2 * s + h) ^ ((row >> 2) & 3)) << 4));
+        fb[t] = *(const V8*)(base + row * (2 * BK) + 16 * C::slot(row, 2 * s + h));
       }
 #pragma unroll
       for (int t = 0; t < TB; ++t)
@@ -156,25 +156,25 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tok_linear(LinearArgs a) {
 
   if (DMA) {
     stage_dma(0, 0);
-    if (nk > 1) stage_dma(1, 1);
+    if (C::ST == 3 && nk > 1) stage_dma(1, 1);
     int buf = 0;
     for (int kt = 0; kt < nk; ++kt) {
       // this wave's loads of stage kt have landed (those of kt + 1 may be in flight) ...
-      if (kt + 1 < nk)
+      if (C::ST == 3 && kt + 1 < nk)
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(C::LOADS) : "memory");
       else
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       // ... and everyone's, and everyone is done with the buffer that stage kt + 2 goes to
       lds_barrier();
-      if (kt + 2 < nk) stage_dma(kt + 2, buf == 0 ? 2 : buf - 1);
+      if (kt + C::ST - 1 < nk) stage_dma(kt + C::ST - 1, buf == 0 ? C::ST - 1 : buf - 1);
       compute(buf);
-      buf = buf == 2 ? 0 : buf + 1;
+      buf = buf == C::ST - 1 ? 0 : buf + 1;
     }
   } else {
     V8 reg[C::LOADS];
     auto fetch = [&](int kt) {
 #pragma unroll
-      for (int i = 0; i < C::LOADS; ++i) reg[i] = load_row8<E>(src[i] + (int64_t)kt * kBK, K - kt * kBK - kof[i]);
+      for (int i = 0; i < C::LOADS; ++i) reg[i] = load_row8<E>(src[i] + (int64_t)kt * BK, K - kt * BK - kof[i]);
     };
     auto put = [&](int buf) {
 #pragma unroll
@@ -336,13 +336,13 @@ __global__ __launch_bounds__(512) void k_tok_linear_rows(LinearArgs a) {
   }
 }
 
-template <class E, bool GATED, bool DMA, int WN, int WM, int TB>
+template <class E, bool GATED, bool DMA, int WN, int WM, int TB, int BK = 32>
 hipError_t go_tile(const LinearArgs& a, hipStream_t st) {
-  typedef Tile<E, GATED, DMA, WN, WM, TB> C;
+  typedef Tile<E, GATED, DMA, WN, WM, TB, BK> C;
   int64_t grid = ((a.s.m + C::TM - 1) / C::TM) * ((a.s.n + C::OF * WN - 1) / (C::OF * WN));
   grid = (grid + kNumXCD - 1) / kNumXCD * kNumXCD;
   if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
-  launch(k_tok_linear<E, GATED, DMA, WN, WM, TB>, dim3((unsigned)grid), dim3(64 * C::NW), st, a);
+  launch(k_tok_linear<E, GATED, DMA, WN, WM, TB, BK>, dim3((unsigned)grid), dim3(64 * C::NW), st, a);
   return hipGetLastError();
 }
 
@@ -360,9 +360,9 @@ hipError_t pick(const LinearArgs& a, hipStream_t st) {
   if (s.m <= 16) return go_rows<E, GATED, 1>(a, st);
   if (s.m <= 128) return go_rows<E, GATED, 2>(a, st);
   const bool dma = s.k % 8 == 0 && s.ldx % 8 == 0 && s.ldw % 8 == 0 && (uintptr_t)a.x % 16 == 0 && (uintptr_t)a.w % 16 == 0;
-  const int64_t big = ((s.m + 255) / 256) * ((nf + 127) / 128);
-  if (big >= 256) return dma ? go_tile<E, GATED, true, 2, 2, 4>(a, st) : go_tile<E, GATED, false, 2, 2, 4>(a, st);
-  return dma ? go_tile<E, GATED, true, 2, 2, 1>(a, st) : go_tile<E, GATED, false, 2, 2, 1>(a, st);
+  const int64_t big = ((s.m + 255) / 256) * ((nf + 255) / 256);
+  if (big >= 200) return dma ? go_tile<E, GATED, true, 4, 2, 4, 64>(a, st) : go_tile<E, GATED, false, 4, 2, 4>(a, st);
+  return dma ? go_tile<E, GATED, true, 2, 2, 2>(a, st) : go_tile<E, GATED, false, 2, 2, 2>(a, st);
 }
 
 }  // namespace

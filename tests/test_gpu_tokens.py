@@ -470,6 +470,26 @@ def test_decay_nan_reaches_no_earlier_token_and_no_other_head():
     assert torch.equal(got[0, :, 0], clean[0, :, 0]) and torch.equal(got[1, :, 1], clean[1, :, 1])
     assert torch.isfinite(got[0, :64]).all() and torch.isfinite(got[1, :128]).all()
     assert torch.isnan(got[0, 100:, 1, 3]).all()
+    # to the token: what came before in the same stretch, and the other columns, are as they were
+    assert torch.equal(got[0, :100, 1], clean[0, :100, 1]) and torch.equal(got[1, :149, 0], clean[1, :149, 0])
+    other = torch.arange(64) != 3
+    assert torch.isfinite(got[0, :, 1][:, other]).all()
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("T", [5, 90])
+def test_decay_state_that_is_not_finite(T, dt):
+    # an infinity in one column of the state stays in that column
+    g = gen(24)
+    q, k, v = (rnd(g, (1, T, 1, 64), dt).to(DEV) for _ in range(3))
+    ld = torch.tensor([-0.05], device=DEV)
+    S = torch.randn((1, 1, 64, 64), generator=g).to(DEV)
+    clean = tk.decay_attention(q, k, v, ld, S).cpu()
+    S[0, 0, 5, 40] = float("inf")
+    got = tk.decay_attention(q, k, v, ld, S).cpu()
+    other = torch.arange(64) != 40
+    assert not torch.isfinite(got[0, :, 0, 40]).any()
+    assert torch.equal(got[..., other], clean[..., other])
 
 
 def test_decay_offsets_past_32_bits():
