@@ -1,11 +1,14 @@
 // RMS norm of every query and key head and the rotation by the token's
-// position, in one pass over q and k.
+// position, in one pass over q and k: each element is read once and written
+// once, so the bytes are the bound.
+#include <algorithm>
+
 #include "tokens.hpp"
 
 namespace nc {
 namespace {
 
-constexpr int kMaxPairs = 128;
+constexpr int kMaxPairs = 128, kMaxTokens = 8;  // of a workgroup's table
 
 // cos and sin of pos * freq radians.  The angle is counted in turns in 64
 // bits, where a 31-bit position times a 24-bit frequency is exact up to the
@@ -17,74 +20,179 @@ __device__ __forceinline__ float2 turn(int pos, float freq) {
   return make_float2(__builtin_amdgcn_cosf(f), __builtin_amdgcn_sinf(f));
 }
 
-__device__ __forceinline__ float wave_sum_f(float v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, false));
+}
+// Sum over the 2^log2g neighbouring lanes of a group, in every lane of it.
+__device__ __forceinline__ float group_sum(float v, int log2g) {
+  if (log2g > 0) v += dpp<0xB1>(v);   // lanes i ^ 1
+  if (log2g > 1) v += dpp<0x4E>(v);   // i ^ 2
+  if (log2g > 2) v += dpp<0x141>(v);  // mirrored in 8: the other four, which are all alike
+  if (log2g > 3) v += dpp<0x140>(v);  // mirrored in 16
+  if (log2g > 4) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  }
+  if (log2g > 5) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  }
   return v;
 }
 
-// One workgroup per token, one wave per head.
-template <class E>
-__global__ __launch_bounds__(256) void k_tok_rope(QkArgs a) {
+struct RopeArgs {
+  QkArgs a;
+  int tokens;      // of a workgroup
+  int log2g;       // lanes of a head
+  uint32_t magic;  // ceil(2^32 / heads): row / heads = row * magic >> 32 for the rows of a workgroup (heads > 1)
+};
+
+// A lane holds VEC pairs of a head (two runs of VEC elements), a group of lanes
+// the head, a workgroup all heads of a few tokens.  The sines and cosines of
+// those tokens are formed once, in LDS, for all their heads.  UPL: units a
+// lane holds (2 only where a head has more than 64 units).
+template <class E, int VEC, int UPL>
+__global__ __launch_bounds__(256) void k_tok_rope(RopeArgs ra) {
   typedef typename E::T T;
-  __shared__ float2 cs[kMaxPairs];
-  const ncodec_qk_shape& s = a.s;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int P = s.section[0] + s.section[1] + s.section[2], D = s.head_dim;
-  const int64_t t = blockIdx.x;
-  for (int p = threadIdx.x; p < P; p += 256) {
+  typedef T TV __attribute__((ext_vector_type(VEC)));
+  __shared__ __align__(16) float2 cs[kMaxTokens * kMaxPairs];
+  const ncodec_qk_shape& s = ra.a.s;
+  const int P = s.section[0] + s.section[1] + s.section[2], D = s.head_dim, H = s.q_heads + s.k_heads;
+  const int64_t tk0 = (int64_t)blockIdx.x * ra.tokens;
+  const int nt = (int)min((int64_t)ra.tokens, s.tokens - tk0);
+  const int G = 1 << ra.log2g, gl = threadIdx.x & (G - 1);
+
+  // this lane's units: rotated ones first, then the dimensions that pass
+  const int RU = (P + VEC - 1) / VEC;
+  int offa[UPL], offb[UPL];
+  bool rot[UPL];
+  TV wq[UPL][2], wk[UPL][2];
+#pragma unroll
+  for (int x = 0; x < UPL; ++x) {
+    const int u = gl + x * G;
+    rot[x] = u < RU;
+    offa[x] = !rot[x] ? 2 * P + 2 * VEC * (u - RU) : s.interleaved ? 2 * VEC * u : VEC * u;
+    offb[x] = rot[x] && !s.interleaved ? P + VEC * u : offa[x] + VEC;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const int off = y ? offb[x] : offa[x];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) wq[x][y][e] = wk[x][y][e] = (T)1.f;
+      if (s.norm && off < D) {
+        if (ra.a.wq) __builtin_memcpy(&wq[x][y], (const T*)ra.a.wq + off, sizeof(TV));
+        if (ra.a.wk) __builtin_memcpy(&wk[x][y], (const T*)ra.a.wk + off, sizeof(TV));
+      }
+    }
+  }
+  for (int i = threadIdx.x; i < nt * P; i += 256) {
+    const int t = i / P, p = i - t * P;
     const int axis = p < s.section[0] ? 0 : p < s.section[0] + s.section[1] ? 1 : 2;
-    cs[p] = turn(a.pos[t * s.axes + axis], a.freq[p]);
+    cs[t * P + p] = turn(ra.a.pos[(tk0 + t) * s.axes + axis], ra.a.freq[p]);
   }
   __syncthreads();
-  for (int h = wave; h < s.q_heads + s.k_heads; h += 4) {
-    const bool is_q = h < s.q_heads;
-    const int hh = is_q ? h : h - s.q_heads;
-    const T* x = is_q ? (const T*)a.q + t * s.q_token_stride + hh * s.q_head_stride
-                      : (const T*)a.k + t * s.k_token_stride + hh * s.k_head_stride;
-    T* y = is_q ? (T*)a.qo + t * s.qo_token_stride + hh * s.qo_head_stride
-                : (T*)a.ko + t * s.ko_token_stride + hh * s.ko_head_stride;
-    const T* w = (const T*)(is_q ? a.wq : a.wk);
-    float v[4], o[4], sq = 0.f;
+
+  const float inv_d = 1.f / (float)D;
+  for (int row = threadIdx.x >> ra.log2g; row < nt * H; row += 256 >> ra.log2g) {
+    const int t = H == 1 ? row : (int)__umulhi((uint32_t)row, ra.magic), hh = row - t * H;
+    const bool is_q = hh < s.q_heads;
+    const int64_t tok = tk0 + t, hd = is_q ? hh : hh - s.q_heads;
+    const T* x = is_q ? (const T*)ra.a.q + tok * s.q_token_stride + hd * s.q_head_stride
+                      : (const T*)ra.a.k + tok * s.k_token_stride + hd * s.k_head_stride;
+    T* y = is_q ? (T*)ra.a.qo + tok * s.qo_token_stride + hd * s.qo_head_stride
+                : (T*)ra.a.ko + tok * s.ko_token_stride + hd * s.ko_head_stride;
+    float v[UPL][2][VEC];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int d = lane + 64 * i;
-      v[i] = d < D ? (float)x[d] : 0.f;
-      sq = fmaf(v[i], v[i], sq);
-    }
-    float inv = 1.f;
-    if (s.norm) inv = 1.f / sqrtf(wave_sum_f(sq) / D + s.eps);
-    // each pair's other half, read before anything is written
+    for (int i = 0; i < UPL; ++i)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int d = lane + 64 * i;
-      if (d >= D) continue;
-      float e = v[i] * inv * (s.norm && w ? (float)w[d] : 1.f);
-      if (d < 2 * P) {
-        const int p = s.interleaved ? d >> 1 : d < P ? d : d - P;
-        const bool second = s.interleaved ? d & 1 : d >= P;
-        const int od = s.interleaved ? d ^ 1 : second ? d - P : d + P;
-        const float other = (float)x[od] * inv * (s.norm && w ? (float)w[od] : 1.f);
-        const float2 c = cs[p];
-        e = second ? fmaf(other, c.y, e * c.x) : fmaf(-other, c.y, e * c.x);
+      for (int j = 0; j < 2; ++j) {
+        const int off = j ? offb[i] : offa[i];
+        TV r = {};
+        if (off < D) __builtin_memcpy(&r, x + off, sizeof(TV));
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[i][j][e] = (float)r[e];
       }
-      o[i] = e;
+    if (s.norm) {
+      float sq = 0.f;
+#pragma unroll
+      for (int i = 0; i < UPL; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) sq = fmaf(v[i][j][e], v[i][j][e], sq);
+      const float inv = __builtin_amdgcn_rsqf(fmaf(group_sum(sq, ra.log2g), inv_d, s.eps));
+#pragma unroll
+      for (int i = 0; i < UPL; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) v[i][j][e] *= inv * (float)(is_q ? wq[i][j][e] : wk[i][j][e]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (lane + 64 * i < D) y[lane + 64 * i] = (T)o[i];
+    for (int i = 0; i < UPL; ++i) {
+      if (rot[i]) {
+        const float2* c = cs + t * P + VEC * (gl + i * G);
+        float2 tab[VEC];
+        __builtin_memcpy(tab, __builtin_assume_aligned(c, VEC == 1 ? 8 : 16), sizeof(tab));
+        if (s.interleaved && VEC > 1) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < VEC / 2; ++e) {
+              const float2 w = tab[j * (VEC / 2) + e];
+              const float a = v[i][j][2 * e], b = v[i][j][2 * e + 1];
+              v[i][j][2 * e] = fmaf(-b, w.y, a * w.x);
+              v[i][j][2 * e + 1] = fmaf(b, w.x, a * w.y);
+            }
+        } else {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            const float a = v[i][0][e], b = v[i][1][e];
+            v[i][0][e] = fmaf(-b, tab[e].y, a * tab[e].x);
+            v[i][1][e] = fmaf(b, tab[e].x, a * tab[e].y);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int off = j ? offb[i] : offa[i];
+        TV r;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) r[e] = (T)v[i][j][e];
+        if (off < D) __builtin_memcpy(y + off, &r, sizeof(TV));
+      }
+    }
   }
+}
+
+template <class E, int VEC, int UPL>
+hipError_t go(const QkArgs& a, int units, hipStream_t st) {
+  const ncodec_qk_shape& s = a.s;
+  RopeArgs ra{a, 1, 0, 0};
+  while (ra.log2g < 6 && (1 << ra.log2g) * UPL < units) ++ra.log2g;
+  const int64_t H = s.q_heads + s.k_heads;
+  // tokens of a workgroup: up to eight, as long as that leaves eight workgroups a CU
+  ra.tokens = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxTokens, s.tokens / 2048));
+  ra.magic = (uint32_t)((((uint64_t)1 << 32) + H - 1) / H);
+  launch(k_tok_rope<E, VEC, UPL>, dim3((unsigned)((s.tokens + ra.tokens - 1) / ra.tokens)), dim3(256), st, ra);
+  return hipGetLastError();
+}
+
+// Runs of eight or four elements where head_dim and the pairs are made of them
+// (16- and 8-byte accesses), single elements otherwise.
+template <class E>
+hipError_t pick(const QkArgs& a, hipStream_t st) {
+  const int P = a.s.section[0] + a.s.section[1] + a.s.section[2], D = a.s.head_dim;
+  if (D % 16 == 0 && P % 8 == 0) return go<E, 8, 1>(a, D / 16, st);
+  if (D % 8 == 0 && P % 4 == 0) return go<E, 4, 1>(a, D / 8, st);
+  if (D <= 128) return go<E, 1, 1>(a, (D + 1) / 2, st);
+  return go<E, 1, 2>(a, (D + 1) / 2, st);
 }
 
 }  // namespace
 
 hipError_t launch_qk_norm_rope(const QkArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)a.s.tokens);
-  if (a.s.dtype == NCODEC_DTYPE_FP16)
-    launch(k_tok_rope<F16>, grid, dim3(256), st, a);
-  else
-    launch(k_tok_rope<BF16>, grid, dim3(256), st, a);
-  return hipGetLastError();
+  return a.s.dtype == NCODEC_DTYPE_FP16 ? pick<F16>(a, st) : pick<BF16>(a, st);
 }
 
 }  // namespace nc
