@@ -26,29 +26,40 @@ def _need(ok, what):
 
 def _dtype(x):
     dt = _DTYPES.get(x.dtype)
-    _need(dt is not None, f"the element type must be float16 or bfloat16, not {x.dtype}")
-    _need(x.is_cuda, "tensors must be on the GPU")
+    if dt is None or not x.is_cuda:
+        raise ValueError(f"tensors must be float16 or bfloat16 on the GPU, not {x.dtype} on {x.device}")
     return dt
 
 
 def _like(t, x, what, shape=None, dtype=None):
     """t sits with x: device, type and (if given) shape, its last dimension contiguous."""
-    _need(t.device == x.device and t.dtype == (dtype or x.dtype), f"{what}: device or type differs from the input's")
-    _need(shape is None or tuple(t.shape) == shape, f"{what}: shape {tuple(t.shape)}, expected {shape}")
-    _need(t.shape[-1] <= 1 or t.stride(-1) == 1, f"{what}: the last dimension must be contiguous")
+    if t.dtype != (dtype or x.dtype) or t.get_device() != x.get_device():
+        raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {dtype or x.dtype} on {x.device}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{what}: the last dimension must be contiguous")
 
 
 def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
-def _call(fn, device, *args):
-    """fn(*args, stream) on the current stream of the tensors' device."""
-    if torch.cuda.current_device() == device.index:
-        st = fn(*args, torch.cuda.current_stream().cuda_stream)
+def _raw_stream(index):
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# the same without building a Stream object, where torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
+
+
+def _call(fn, index, *args):
+    """fn(*args, stream) on the current stream of device `index`."""
+    if torch.cuda.current_device() == index:
+        st = fn(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(device):
-            st = fn(*args, torch.cuda.current_stream().cuda_stream)
+        with torch.cuda.device(index):
+            st = fn(*args, _raw_stream(index))
     if st:
         _nc._check(st)
 
@@ -65,14 +76,15 @@ def linear(x, weight, bias=None, residual=None, act="none", gated=False, out=Non
     act: "none", "lrelu" (slope 0.1), "wsilu" (v sigmoid(4v)), "silu" or "gelu".  ``out`` may be ``residual``.
     Sums and the epilogue are float32, rounded once."""
     dt = _dtype(x)
-    _need(act in ACTS, f"act must be one of {sorted(ACTS)}")
+    if act not in ACTS:
+        raise ValueError(f"act must be one of {sorted(ACTS)}")
     _need(x.dim() >= 1 and weight.dim() == 2, "x needs a dimension, weight two")
     k, rows = x.shape[-1], weight.shape[0]
     _need(not gated or rows % 2 == 0, "a gated weight has an even number of rows")
     n = rows // 2 if gated else rows
     _like(x, x, "x")
     _like(weight, x, "weight", (rows, k))
-    lead = tuple(x.shape[:-1])
+    lead = x.shape[:-1]
     x2 = x if x.dim() == 2 else _flat(x, "x")
     if bias is not None:
         _like(bias, x, "bias", (rows,))
@@ -80,7 +92,7 @@ def linear(x, weight, bias=None, residual=None, act="none", gated=False, out=Non
         _like(residual, x, "residual", lead + (n,))
     y = out
     if y is None:
-        y = torch.empty(lead + (n,), dtype=x.dtype, device=x.device)
+        y = x.new_empty(lead + (n,))
     else:
         _like(y, x, "out", lead + (n,))
     y2 = y if y.dim() == 2 else _flat(y, "out")
@@ -88,7 +100,7 @@ def linear(x, weight, bias=None, residual=None, act="none", gated=False, out=Non
     shape = _nc.ncodec_linear_shape(dt, ACTS[act], 1 if gated else 0, 0, x2.shape[0], n, k, _row_stride(x2, 0, k),
                                     _row_stride(weight, 0, k), 0 if r2 is None else _row_stride(r2, 0, n),
                                     _row_stride(y2, 0, n))
-    _call(_nc.load_library().ncodec_linear, x.device, ctypes.byref(shape), _ptr(x), _ptr(weight), _ptr(bias),
+    _call(_nc.load_library().ncodec_linear, x.get_device(), ctypes.byref(shape), _ptr(x), _ptr(weight), _ptr(bias),
           _ptr(residual), _ptr(y))
     return y
 
@@ -139,17 +151,17 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, positions=None, freq=None, 
         _need(positions.is_contiguous(), "positions must be contiguous")
         _like(freq, q, "freq", (sum(sections),), torch.float32)
     if q_out is None:
-        q_out = torch.empty((T, hq, D), dtype=q.dtype, device=q.device)
+        q_out = q.new_empty((T, hq, D))
     else:
         _like(q_out, q, "q_out", (T, hq, D))
     if k_out is None:
-        k_out = torch.empty((T, hk, D), dtype=q.dtype, device=q.device)
+        k_out = q.new_empty((T, hk, D))
     else:
         _like(k_out, q, "k_out", (T, hk, D))
     shape = _nc.ncodec_qk_shape(dt, 1 if norm else 0, axes, tuple(sections) + (0,) * (3 - axes),
                                 1 if interleaved else 0, hq, hk, D, eps, 0, T, q.stride(0), q.stride(1), k.stride(0),
                                 k.stride(1), q_out.stride(0), q_out.stride(1), k_out.stride(0), k_out.stride(1))
-    _call(_nc.load_library().ncodec_qk_norm_rope, q.device, ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(q_weight),
+    _call(_nc.load_library().ncodec_qk_norm_rope, q.get_device(), ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(q_weight),
           _ptr(k_weight), _ptr(positions) if axes else None, _ptr(freq) if axes else None, _ptr(q_out), _ptr(k_out))
     return q_out, k_out
 
@@ -179,12 +191,12 @@ def decay_attention(q, k, v, log_decay, state=None, lengths=None, scale=None, re
         _need(state.is_contiguous(), "state must be contiguous")
     if state_out is None:
         if return_state:
-            state_out = torch.empty((B, H, D, V), dtype=torch.float32, device=q.device)
+            state_out = q.new_empty((B, H, D, V), dtype=torch.float32)
     else:
         _like(state_out, q, "state_out", (B, H, D, V), torch.float32)
         _need(state_out.is_contiguous(), "state_out must be contiguous")
     if out is None:
-        out = torch.empty((B, T, H, V), dtype=q.dtype, device=q.device)
+        out = q.new_empty((B, T, H, V))
     else:
         _like(out, q, "out", (B, T, H, V))
     shape = _nc.ncodec_decay_shape(dt, H, hk, D, V, D ** -0.5 if scale is None else scale, B, T, *q.stride()[:3],
@@ -192,7 +204,7 @@ def decay_attention(q, k, v, log_decay, state=None, lengths=None, scale=None, re
     lib = _nc.load_library()
     ref = ctypes.byref(shape)
     need = lib.ncodec_decay_attention_workspace_bytes(ref)
-    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    _call(lib.ncodec_decay_attention, q.device, ref, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lengths),
+    ws = q.new_empty(need, dtype=torch.uint8) if need else None
+    _call(lib.ncodec_decay_attention, q.get_device(), ref, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lengths),
           _ptr(state), _ptr(state_out), _ptr(out), _ptr(ws), need)
     return (out, state_out) if return_state else out
