@@ -101,15 +101,15 @@ __global__ __launch_bounds__(256) void k_tok_decay_recur(DecayArgs a) {
 // ---- chunks -------------------------------------------------------------------
 constexpr int kChunk = 64;
 
-template <class E, int DP_, int NV_>
+// LDS: two buffers of k (and q), one of v, which goes to registers first thing.
+template <class E, int DP_, int NV_, bool OUT>
 struct Chunk {
   static constexpr int DP = DP_, NV = NV_, VP = 32 * NV_;  // padded head and value width; a wave per 32 values
   static constexpr int DT = DP / 32;
-  static constexpr int QB = kChunk * DP * 2, VB = kChunk * VP * 2;
-  static constexpr int STAGE = 2 * QB + VB;  // q, k, v of a chunk
+  static constexpr int KB = kChunk * DP * 2, VB = kChunk * VP * 2;
+  static constexpr int STAGE = (OUT ? 2 : 1) * KB;  // k, then q
+  static constexpr int VOFF = 2 * STAGE, LDS = 2 * STAGE + VB;
   static constexpr uint32_t INF = __is_same(E, F16) ? 0x7c00 : 0x7f80;
-  static constexpr int OPITCH = 80;          // a token's 32 outputs of a wave, padded
-  static constexpr int LDS = 2 * STAGE + NV * 32 * OPITCH;
 };
 
 // Slot of 16-byte unit u of a row of W elements: 16 consecutive rows of one
@@ -146,11 +146,14 @@ __device__ __forceinline__ void stage_rows(char* lds, const typename E::T* base,
       rows += step;
     }
   } else {
+    int ln = lane;
+    if (DMA) asm volatile("" : "+v"(ln));  // seldom taken: nothing of it is kept in registers from chunk to chunk
+    const int r1 = ln / U, u1 = unit_slot<W>(r1, ln % U);
 #pragma unroll
     for (int i0 = 0; i0 < LOADS / NW; ++i0) {
-      const int i = wave + NW * i0, u = u0 ^ unit_slot<W>(R * i, 0);
-      const char* p = rows + r0 * stride * 2 + 16 * u;
-      const bool in = R * i + r0 >= pad && 8 * u < d;
+      const int i = wave + NW * i0, u = u1 ^ unit_slot<W>(R * i, 0);
+      const char* p = rows + r1 * stride * 2 + 16 * u;
+      const bool in = R * i + r1 >= pad && 8 * u < d;
       if (DMA) {
         dma16(in ? (const void*)p : (const void*)decay_zero16, lds + 1024 * i);
       } else {
@@ -208,8 +211,9 @@ __device__ __forceinline__ typename E::V8 read_cols(const char* p0, const char* 
   return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// max over all lanes
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+// max over all lanes of a value >= 0 that is no NaN (its bits order it)
+__device__ __forceinline__ float wave_max(float f) {
+  uint32_t v = __float_as_uint(f);
   const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
   v = max(a[0], a[1]);
   const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
@@ -217,16 +221,17 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
 #define NC_ROR(N) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + N, 0xf, 0xf, false));
   NC_ROR(8) NC_ROR(4) NC_ROR(2) NC_ROR(1)
 #undef NC_ROR
-  return __builtin_amdgcn_readfirstlane(v);
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(v));
 }
-// of a value >= 0 that is no NaN: its bits order it
-__device__ __forceinline__ float wave_max(float v) { return __uint_as_float(wave_max(__float_as_uint(v))); }
 template <class V8>
-__device__ __forceinline__ uint32_t max_bits(V8 v) {  // of eight 16-bit magnitudes
+__device__ __forceinline__ uint32_t max_bits(const V8 (&v)[4]) {  // of 16-bit magnitudes
   typedef unsigned short US8 __attribute__((ext_vector_type(8)));
   typedef unsigned short US2 __attribute__((ext_vector_type(2)));
-  const US8 u = __builtin_bit_cast(US8, v) & (unsigned short)0x7fff;
-  US2 m = __builtin_elementwise_max(__builtin_elementwise_max(u.s01, u.s23), __builtin_elementwise_max(u.s45, u.s67));
+  US8 u[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) u[x] = __builtin_bit_cast(US8, v[x]) & (unsigned short)0x7fff;
+  const US8 w = __builtin_elementwise_max(__builtin_elementwise_max(u[0], u[1]), __builtin_elementwise_max(u[2], u[3]));
+  const US2 m = __builtin_elementwise_max(__builtin_elementwise_max(w.s01, w.s23), __builtin_elementwise_max(w.s45, w.s67));
   return max((uint32_t)m.x, (uint32_t)m.y);
 }
 // max(m, |a|, |b|), NaN ignored
@@ -234,24 +239,44 @@ __device__ __forceinline__ float max3_abs(float m, float a, float b) {
   asm("v_max3_f32 %0, %0, |%1|, |%2|" : "+v"(m) : "v"(a), "v"(b));
   return m;
 }
-__device__ __forceinline__ float max_abs(float m, const floatx16& v) {
+__device__ __forceinline__ float max_abs(const floatx16& v) {
+  float m[4];  // four chains
 #pragma unroll
-  for (int r = 0; r < 16; r += 2) m = max3_abs(m, v[r], v[r + 1]);
+  for (int r = 0; r < 4; ++r) m[r] = max3_abs(fabsf(v[4 * r]), v[4 * r + 1], v[4 * r + 2]);
+  m[0] = max3_abs(m[0], v[3], v[7]);
+  m[1] = max3_abs(m[1], v[11], v[15]);
+  return max3_abs(max3_abs(m[0], m[1], m[2]), m[3], 0.f);
+}
+__device__ __forceinline__ float max_finite(float m, const floatx16& v) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    if (fabsf(v[r]) < __builtin_huge_valf()) m = fmaxf(m, fabsf(v[r]));
   return m;
 }
-__device__ __forceinline__ float half_max(float v) {  // over the two lanes l, l + 32
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
 
-// Power of two that takes a largest magnitude m into [2^14, 2^15), and its
-// inverse: fp16 operands are brought there, so that no sum of magnitudes and no
-// small scale leaves the range in which fp16 has its 11 bits.
-__device__ __forceinline__ float scale_up(float m, float* inverse) {
-  const uint32_t e = max((__float_as_uint(m) >> 23) & 255u, 15u);
-  *inverse = __uint_as_float((e - 14) << 23);
-  return __uint_as_float((268 - e) << 23);
-}
+// Units.  What becomes an fp16 operand (scores, the state, weighted values) is
+// held in a power-of-two unit of its own, so that neither large nor small
+// magnitudes leave the range in which fp16 has its 11 bits.  A unit stays
+// while the wave's largest magnitude lies in [lo, hi); else it moves to where that
+// is 2^11 (nothing else in the kernel depends on it).
+struct Unit {
+  float u = 1.f, inv = 1.f;
+  static constexpr float kHi = 0x1p15f, kLo = 0x1p5f;
+  // m: this lane's largest magnitude, times u
+  __device__ __forceinline__ static bool leaves(float m) { return __any(m >= kHi) || !__any(m >= kLo); }
+  // to the unit in which the largest finite magnitude of the wave is 2^11; returns the change
+  __device__ __forceinline__ float move(float m) {
+    const uint32_t e = (__float_as_uint(wave_max(m)) >> 23) & 255u;
+    if (e < 16u || e > 254u) return 1.f;  // nothing but zeros
+    // kept within 2^+-96, so that products of units stay numbers
+    const int want = 127 + 11 - (int)e, have = (int)((__float_as_uint(u) >> 23) & 255u) - 127;
+    const int by = min(max(want, -96 - have), 96 - have);
+    const float f = __uint_as_float((uint32_t)(127 + by) << 23);
+    u *= f;
+    inv *= __uint_as_float((uint32_t)(127 - by) << 23);
+    return f;
+  }
+};
 
 struct Decay64 {  // lambda^n in two floats, so that long products of it lose nothing
   float hi, lo;
@@ -275,15 +300,14 @@ struct SegArgs {
 // 32 w .. 32 w + 31 in its accumulators: register r of tile a and lane (h, c) is
 // row 32 a + 16 (r / 8) + 8 h + r % 8, column 32 w + c.
 template <class E, int DP, int NV, bool OUT, bool DMA>
-__global__ __launch_bounds__(64 * NV, DP <= 64 ? 2 : 1) void k_tok_decay_chunk(SegArgs sa) {
-  typedef Chunk<E, DP, NV> C;
+__global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_tok_decay_chunk(SegArgs sa) {
+  typedef Chunk<E, DP, NV, OUT> C;
   typedef typename E::T T;
   typedef typename E::V8 V8;
   typedef typename E::V4 V4;
   constexpr bool F = __is_same(E, F16);
   constexpr int DT = C::DT, VP = C::VP, NT = F ? 2 : 3;  // NT: 16-bit terms of a weighted value
-  constexpr int STAGE = OUT ? C::STAGE : C::QB + C::VB;
-  __shared__ __align__(1024) char lds[OUT ? C::LDS : 2 * STAGE];
+  __shared__ __align__(1024) char lds[C::LDS];
   const DecayArgs& a = sa.a;
   const ncodec_decay_shape& s = a.s;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -312,19 +336,31 @@ __global__ __launch_bounds__(64 * NV, DP <= 64 ? 2 : 1) void k_tok_decay_chunk(S
     if (t0 >= len && seg > 0) return;
   }
 
-  const int nch = tend > t0 ? (int)((tend - t0 + kChunk - 1) / kChunk) : 0;
   // A last chunk of n < 64 tokens sits at the end of its tile, behind 64 - n rows of
   // zeros: the ages and lags of its rows are then those of a full chunk.
-  auto stage = [&](int c) {
-    const int64_t te = min(t0 + (int64_t)(c + 1) * kChunk, tend), t = te - kChunk;  // of row 0
-    const int pad = kChunk - (int)(te - (t0 + (int64_t)c * kChunk));
-    char* base = lds + (c & 1) * STAGE;
-    stage_rows<E, DP, NV, DMA>(base, k + t * s.k_token_stride, s.k_token_stride, pad, D, wave, lane);
-    stage_rows<E, VP, NV, DMA>(base + C::QB, v + t * s.v_token_stride, s.v_token_stride, pad, V, wave, lane);
-    if (OUT)
-      stage_rows<E, DP, NV, DMA>(base + C::QB + C::VB, q + t * s.q_token_stride, s.q_token_stride, pad, D, wave, lane);
+  const int nch = tend > t0 ? (int)((tend - t0 + kChunk - 1) / kChunk) : 0;
+  const int last_pad = (int)((int64_t)nch * kChunk - (tend - t0));  // of the last chunk
+  const int64_t ks = s.k_token_stride, qs = s.q_token_stride, vs = s.v_token_stride;
+  const T *kp = k + t0 * ks, *qp = q + t0 * qs, *vp = v + t0 * vs;  // of the chunk to be staged next
+  auto stage_kq = [&](int c) {
+    const int pad = c + 1 == nch ? last_pad : 0;
+    char* base = lds + (c & 1) * C::STAGE;
+    stage_rows<E, DP, NV, DMA>(base, kp - pad * ks, ks, pad, D, wave, lane);
+    kp += kChunk * ks;
+    if (OUT) {
+      stage_rows<E, DP, NV, DMA>(base + C::KB, qp - pad * qs, qs, pad, D, wave, lane);
+      qp += kChunk * qs;
+    }
   };
-  if (nch) stage(0);
+  auto stage_v = [&](int c) {
+    const int pad = c + 1 == nch ? last_pad : 0;
+    stage_rows<E, VP, NV, DMA>(lds + C::VOFF, vp - pad * vs, vs, pad, V, wave, lane);
+    vp += kChunk * vs;
+  };
+  if (nch) {
+    stage_v(0);
+    stage_kq(0);
+  }
 
   const float log_decay = a.log_decay[hd];
   const float l2 = log2_decay(log_decay);
@@ -342,13 +378,16 @@ __global__ __launch_bounds__(64 * NV, DP <= 64 ? 2 : 1) void k_tok_decay_chunk(S
                 : a.state_out && t0 + SL >= len ? a.state_out + bh * sdv : nullptr;
 
   // Decays.  Inside a diagonal 32 x 32 tile lambda^(i - j) for j <= i (i this lane's
-  // token, j the register's), one tile below it lambda^(32 + i - j).  At the end
-  // of a chunk token 16 x + j counts lambda^(15 - j) lambda^(48 - 16 x).
+  // token, j the register's), one tile below it lambda^(32 + i - j), both in the
+  // scores' unit.  At the end of a chunk token 16 x + j counts lambda^(15 - j)
+  // lambda^(48 - 16 x), in the unit of the weighted values.
   float mdiag[OUT ? 16 : 1], mlow[OUT ? 16 : 1], wage[8], wstep[4];
+  uint32_t below = 0;  // bit r: j <= i
   if (OUT) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int lag = l32 - drow(r, h);
+      below |= lag >= 0 ? 1u << r : 0u;
       mdiag[r] = __builtin_amdgcn_exp2f(max(lag, 0) * l2);
       mlow[r] = __builtin_amdgcn_exp2f((32 + lag) * l2);
     }
@@ -357,158 +396,203 @@ __global__ __launch_bounds__(64 * NV, DP <= 64 ? 2 : 1) void k_tok_decay_chunk(S
   for (int e = 0; e < 8; ++e) wage[e] = __builtin_amdgcn_exp2f((15 - (8 * (e >> 2) + 4 * h + (e & 3))) * l2);
 #pragma unroll
   for (int x = 0; x < 4; ++x) wstep[x] = __builtin_amdgcn_exp2f((48 - 16 * x) * l2);
-  Decay64 keep = decay_pow(log_decay, kChunk);
+  const float di0 = __builtin_amdgcn_exp2f((l32 + 1) * l2), d32 = __builtin_amdgcn_exp2f(32 * l2);
+  Decay64 keep = decay_pow(log_decay, kChunk), keep_last = keep;
+  if (last_pad) keep_last = decay_pow(log_decay, kChunk - last_pad);
+  T* op = o + (t0 + l32) * s.o_token_stride + 32 * wave + 8 * h;  // this lane's first output row
+  const int64_t ostep = 32 * s.o_token_stride;
   const int ro = row_offset<DP>(lane);
   const int ck0 = col_offset<DP, true>(lane, 0), ck1 = col_offset<DP, true>(lane, 1);
-  const int cv0 = C::QB + (col_offset<VP, false>(lane, 0) ^ (64 * wave)),
-            cv1 = C::QB + (col_offset<VP, false>(lane, 1) ^ (64 * wave));
-  char* mine = lds + 2 * STAGE + wave * 32 * C::OPITCH;
+  const char *pv0 = lds + C::VOFF + (col_offset<VP, false>(lane, 0) ^ (64 * wave)),
+             *pv1 = lds + C::VOFF + (col_offset<VP, false>(lane, 1) ^ (64 * wave));
+  Unit us, up, uv;  // of the state, the scores and the weighted values (fp16 only)
+  float owed = 0.f;
+  auto settle = [&]() {
+#pragma unroll
+    for (int x = 0; x < DT; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) S[x][r] = fmaf(S[x][r], owed, S[x][r]);
+    owed = 0.f;
+  };
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
   for (int c = 0; c < nch; ++c) {
     // every wave's loads of chunk c have landed (each waited for its own), and
     // every wave is done with the other buffer
     lds_barrier();
-    if (c + 1 < nch) stage(c + 1);
-    const int buf = (c & 1) * STAGE;
-    const int64_t t = t0 + (int64_t)c * kChunk;
-    const int n = (int)min(tend - t, (int64_t)kChunk), pad = kChunk - n;
+    if (c + 1 < nch) stage_kq(c + 1);
+    const int buf = (c & 1) * C::STAGE;
+    const int pad = c + 1 == nch ? last_pad : 0;
+    if (pad) {
+      keep = keep_last;
+      op -= pad * s.o_token_stride;
+    }
 
     V8 vf[4];
-    {
-      const char *p0 = lds + (cv0 + buf), *p1 = lds + (cv1 + buf);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) vf[x] = read_cols<E>(p0 + 32 * VP * x, p1 + 32 * VP * x);
-    }
-    // largest magnitude, by its bits, which order finite values, infinities and NaN
-    uint32_t mb = max(max(max_bits(vf[0]), max_bits(vf[1])), max(max_bits(vf[2]), max_bits(vf[3])));
-    mb = wave_max(mb);
+    for (int x = 0; x < 4; ++x) vf[x] = read_cols<E>(pv0 + 32 * VP * x, pv1 + 32 * VP * x);
+    lds_barrier();  // v is in registers: its buffer takes the next chunk's
+    if (c + 1 < nch) stage_v(c + 1);
+
     int bad = kChunk;  // first row of this lane's column that is not finite
-    const bool any_bad = mb >= C::INF;
+    uint32_t mb = max_bits(vf);  // magnitudes by their bits, which order finite values, infinities and NaN
+    const bool any_bad = __any(mb >= C::INF);
     if (any_bad) {
       // a product would carry it to earlier tokens too (0 times NaN): it is taken
       // out here and put into the outputs and the state that it reaches
       mb = 0;
+      int h4 = 4 * h;
+      asm volatile("" : "+v"(h4));  // nothing of this rare path is computed, and kept, before the loop
 #pragma unroll
       for (int x = 0; x < 4; ++x)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const uint32_t u = (uint32_t)__builtin_bit_cast(uint16_t, (T)vf[x][e]) & 0x7fffu;
           if (u >= C::INF) {
-            bad = min(bad, 16 * x + 8 * (e >> 2) + 4 * h + (e & 3));
+            bad = min(bad, 16 * x + 8 * (e >> 2) + h4 + (e & 3));
             vf[x][e] = (T)0.f;
           } else {
             mb = max(mb, u);
           }
         }
-      mb = wave_max(mb);
       bad = min(bad, __shfl_xor(bad, 32, 64));
     }
-    float vinv = 1.f;
-    if (F) {  // a power of two, exact in fp16: what is lost lies 2^-24 below 2^14
-      const float m = fmaxf((float)__builtin_bit_cast(f16, (uint16_t)mb), 0.5f);
-      const float up = scale_up(m, &vinv);
+    if (F) {
+      const float m = (float)__builtin_bit_cast(f16, (uint16_t)mb) * uv.u;
+      if (Unit::leaves(m)) {
+        const float f = uv.move(m);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) vf[x] = vf[x] * (T)up;
+        for (int e = 0; e < 8; ++e) wage[e] *= f;
+      }
     }
 
     if (OUT) {
-      float sinv = 1.f, sup = 1.f;
       if (F) {
-        float m = 0.f;
+        float m = max_abs(S[0]);
 #pragma unroll
-        for (int x = 0; x < DT; ++x) m = max_abs(m, S[x]);
-        m = wave_max(m);
-        if (m == __builtin_huge_valf()) {  // the finite ones keep their scale
-          m = 0.f;
+        for (int x = 1; x < DT; ++x) m = fmaxf(m, max_abs(S[x]));
+        if (Unit::leaves(m)) {
+          if (__any(m == __builtin_huge_valf())) {  // the finite ones keep their unit
+            m = 0.f;
+#pragma unroll
+            for (int x = 0; x < DT; ++x) m = max_finite(m, S[x]);
+          }
+          const float f = us.move(m);
 #pragma unroll
           for (int x = 0; x < DT; ++x)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (fabsf(S[x][r]) < __builtin_huge_valf()) m = fmaxf(m, fabsf(S[x][r]));
-          m = wave_max(m);
+            for (int r = 0; r < 16; ++r) S[x][r] *= f;
         }
-        sup = scale_up(m, &sinv);
       }
+      // scores of a 32 x 32 tile as an operand: p holds k_j . q_i
+      auto scores = [&](floatx16& p, bool diag, V8(&pf)[2]) {
+        if (diag) {  // pairs above the diagonal count nothing, whatever their product is
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            p[r] = __int_as_float(__float_as_int(p[r]) & ((int)(below << (31 - r)) >> 31));
+        }
+        if (F) {
+          float m = max_abs(p) * up.u;
+          if (Unit::leaves(m)) {
+            if (__any(m == __builtin_huge_valf())) m = max_finite(0.f, p) * up.u;
+            const float f = up.move(m);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              mdiag[r] *= f;
+              mlow[r] *= f;
+            }
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) pf[r >> 3][r & 7] = (T)(p[r] * (diag ? mdiag[r] : mlow[r]));
+      };
 #pragma unroll
       for (int it = 0; it < 2; ++it) {  // 32 queries
-        __builtin_amdgcn_sched_barrier(0);
-        floatx16 p[2] = {}, inter = {};
+        floatx16 inter = {}, intra = {};
         const int rb = ro + buf;
+        if (it) {  // the keys before them
+          floatx16 p = {};
 #pragma unroll
-        for (int x = 0; x < 2 * DT; ++x) {
-          const char* r = lds + (rb ^ (32 * x));
-          const V8 qf = *(const V8*)(r + (C::QB + C::VB + 64 * DP * it));
-#pragma unroll
-          for (int jt = 0; jt <= it; ++jt) p[jt] = E::mfma(*(const V8*)(r + 64 * DP * jt), qf, p[jt]);
-          V8 sf;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sf[e] = (T)(F ? S[x >> 1][8 * (x & 1) + e] * sup : S[x >> 1][8 * (x & 1) + e]);
-          inter = E::mfma(sf, qf, inter);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        // pairs above the diagonal count nothing, whatever their product is
-        int tok = l32;
-        asm volatile("" : "+v"(tok));  // compared here and not before the loop, where 16 masks would have to be kept
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[it][r] = drow(r, h) > tok ? 0.f : p[it][r];
-        float pinv = 1.f, pup = 1.f;
-        if (F) {
-          float m = max_abs(0.f, p[0]);
-          if (it) m = max_abs(m, p[1]);
-          pup = scale_up(half_max(m), &pinv);
-        }
-        floatx16 intra = {};
-#pragma unroll
-        for (int jt = 0; jt <= it; ++jt) {
-          V8 pf[2];
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float w = jt == it ? mdiag[r] : mlow[r];
-            pf[r >> 3][r & 7] = (T)(F ? p[jt][r] * pup * w : p[jt][r] * w);
+          for (int x = 0; x < 2 * DT; ++x) {
+            const char* r = lds + (rb ^ (32 * x));
+            p = E::mfma(*(const V8*)r, *(const V8*)(r + (C::KB + 64 * DP)), p);
           }
-          intra = E::mfma(vf[2 * jt], pf[0], intra);
-          intra = E::mfma(vf[2 * jt + 1], pf[1], intra);
+          V8 pf[2];
+          scores(p, false, pf);
+          intra = E::mfma(vf[0], pf[0], intra);
+          intra = E::mfma(vf[1], pf[1], intra);
+        }
+        const float was = up.inv;
+        {
+          floatx16 p = {};
+#pragma unroll
+          for (int x = 0; x < 2 * DT; ++x) {
+            const char* r = lds + (rb ^ (32 * x)) + 64 * DP * it;
+            const V8 qf = *(const V8*)(r + C::KB);
+            p = E::mfma(*(const V8*)r, qf, p);
+            V8 sf;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sf[e] = (T)S[x >> 1][8 * (x & 1) + e];
+            inter = E::mfma(sf, qf, inter);
+          }
+          V8 pf[2];
+          scores(p, true, pf);
+          if (F && it && was != up.inv) {  // the unit moved between the two tiles
+            const float f = was * up.u;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) intra[r] *= f;
+          }
+          intra = E::mfma(vf[2 * it], pf[0], intra);
+          intra = E::mfma(vf[2 * it + 1], pf[1], intra);
         }
         // row i is token i - pad of the chunk; rows of the padding are not stored
-        const float di = __builtin_amdgcn_exp2f(max(32 * it + l32 + 1 - pad, 0) * l2);
-        const float ci = s.scale * di * sinv, cp = s.scale * pinv * vinv;
+        float di = it ? di0 * d32 : di0;
+        if (pad) di = __builtin_amdgcn_exp2f(max(32 * it + l32 + 1 - pad, 0) * l2);
+        const float ci = s.scale * di * us.inv, cp = s.scale * up.inv;
 #pragma unroll
         for (int r = 0; r < 16; ++r) inter[r] = fmaf(inter[r], ci, intra[r] * cp);
         if (any_bad) {
+          int h2 = h;
+          asm volatile("" : "+v"(h2));
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (32 * it + l32 >= __shfl(bad, drow(r, h), 64)) inter[r] = __builtin_nanf("");
+            if (32 * it + l32 >= __shfl(bad, drow(r, h2), 64)) inter[r] = __builtin_nanf("");
         }
+        // a lane has four consecutive values eight times, its neighbour l ^ 32 the
+        // four after them: exchanged, each has eight, a 16-byte unit of the row
+        const bool row_in = 32 * it + l32 >= pad;
+        T* row = op;
+        op += ostep;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          V4 x;
+        for (int g = 0; g < 2; ++g) {
+          V4 lo, hi;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] = (T)inter[4 * g + j];
-          *(V4*)(mine + l32 * C::OPITCH + 16 * g + 8 * h) = x;
-        }
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const int row = 16 * y + (lane >> 2), u = lane & 3;
-          const V8 x = *(const V8*)(mine + row * C::OPITCH + 16 * u);
-          const int left = V - (32 * wave + 8 * u);
-          if (32 * it + row >= pad && left > 0) {
-            T* p = o + (t + 32 * it + row - pad) * s.o_token_stride + 32 * wave + 8 * u;
-            if (left >= 8)
-              __builtin_memcpy(p, &x, 16);
-            else
+          for (int j = 0; j < 4; ++j) {
+            lo[j] = (T)inter[8 * g + j];
+            hi[j] = (T)inter[8 * g + 4 + j];
+          }
+          typedef uint32_t U2 __attribute__((ext_vector_type(2)));
+          typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+          const U2 x = __builtin_bit_cast(U2, lo), y = __builtin_bit_cast(U2, hi);
+          const auto w0 = __builtin_amdgcn_permlane32_swap(x.x, y.x, false, false);
+          const auto w1 = __builtin_amdgcn_permlane32_swap(x.y, y.y, false, false);
+          const U4 w = {w0[0], w1[0], w0[1], w1[1]};
+          const int left = V - (32 * wave + 16 * g + 8 * h);
+          if (row_in && left > 0) {
+            if (left >= 8) {
+              __builtin_memcpy(row + 16 * g, &w, 16);
+            } else {
+              const V8 z = __builtin_bit_cast(V8, w);
 #pragma unroll
               for (int e = 0; e < 8; ++e)
-                if (e < left) p[e] = x[e];
+                if (e < left) row[16 * g + e] = z[e];
+            }
           }
         }
-        __builtin_amdgcn_wave_barrier();
       }
     }
 
     if (!OUT || c + 1 < nch || sout) {
-      __builtin_amdgcn_sched_barrier(0);
       // the state: v weighted by its age, as a sum of 16-bit terms that holds 22 (fp16)
       // or 24 (bf16) bits, because the state is an fp32 output
       V8 term[4][NT];
@@ -526,8 +610,7 @@ __global__ __launch_bounds__(64 * NV, DP <= 64 ? 2 : 1) void k_tok_decay_chunk(S
             w -= (float)term[x][y][e];
           }
         }
-      __builtin_amdgcn_sched_barrier(0);
-      if (pad) keep = decay_pow(log_decay, n);
+      const float gain = uv.inv * us.u;
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const char *p0 = lds + ((ck0 + buf) ^ (64 * d)), *p1 = lds + ((ck1 + buf) ^ (64 * d));
@@ -539,13 +622,17 @@ __global__ __launch_bounds__(64 * NV, DP <= 64 ? 2 : 1) void k_tok_decay_chunk(S
           for (int y = NT - 1; y >= 0; --y) add = E::mfma(kf, term[x][y], add);
         }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) S[d][r] = fmaf(S[d][r], keep.hi, fmaf(S[d][r], keep.lo, F ? add[r] * vinv : add[r]));
+        for (int r = 0; r < 16; ++r) S[d][r] = F ? fmaf(add[r], gain, S[d][r] * keep.hi) : fmaf(S[d][r], keep.hi, add[r]);
       }
-      if (any_bad && bad < kChunk) {
+      // what rounding lambda^n to keep.hi left out, made up for every sixteenth chunk
+      owed += keep.hi > 0.f ? keep.lo / keep.hi : 0.f;
+      if ((c & 15) == 15) settle();
+      if (any_bad) {
+        asm volatile("");  // a branch, not a select for each register
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) S[d][r] = __builtin_nanf("");
+          for (int r = 0; r < 16; ++r) S[d][r] = bad < kChunk ? __builtin_nanf("") : S[d][r];
       }
     }
     // this wave's part of the next chunk has landed (and its stores, long sent)
@@ -553,12 +640,13 @@ __global__ __launch_bounds__(64 * NV, DP <= 64 ? 2 : 1) void k_tok_decay_chunk(S
   }
 
   if (sout) {
+    settle();
 #pragma unroll
     for (int x = 0; x < DT; ++x)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int d = 32 * x + 16 * (r >> 3) + 8 * h + (r & 7);
-        if (d < D && col < V) sout[(int64_t)d * V + col] = S[x][r];
+        if (d < D && col < V) sout[(int64_t)d * V + col] = S[x][r] * us.inv;
       }
   }
 }
