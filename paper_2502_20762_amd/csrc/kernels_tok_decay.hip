@@ -260,7 +260,7 @@ __device__ __forceinline__ float max_finite(float m, const floatx16& v) {
 // while the wave's largest magnitude lies in [lo, hi); else it moves to where that
 // is 2^11 (nothing else in the kernel depends on it).
 struct Unit {
-  float u = 1.f, inv = 1.f;
+  float u, inv;
   static constexpr float kHi = 0x1p15f, kLo = 0x1p5f;
   // m: this lane's largest magnitude, times u
   __device__ __forceinline__ static bool leaves(float m) { return __any(m >= kHi) || !__any(m >= kLo); }
@@ -315,7 +315,8 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int nsg = OUT ? sa.nseg : sa.nseg - 1;
   const int64_t bh = blockIdx.x / nsg;
   const int seg = blockIdx.x % nsg;
-  const int64_t b = bh / s.heads, hd = bh % s.heads, hk = hd / (s.heads / s.kv_heads);
+  const uint32_t b = (uint32_t)bh / (uint32_t)s.heads, hd = (uint32_t)bh - b * s.heads,
+                 hk = hd / ((uint32_t)s.heads / (uint32_t)s.kv_heads);  // batch * heads < 2^24
   const int D = s.head_dim, V = s.value_dim;
   const int64_t len = a.lengths ? min(max((int64_t)a.lengths[b], (int64_t)0), s.tokens) : s.tokens;
   const int64_t SL = (int64_t)sa.seg_chunks * kChunk, t0 = seg * SL;
@@ -370,13 +371,24 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
   for (int x = 0; x < DT; ++x)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int d = 32 * x + 16 * (r >> 3) + 8 * h + (r & 7);
-      S[x][r] = sin && d < D && col < V ? sin[(int64_t)d * V + col] : 0.f;
-    }
+    for (int r = 0; r < 16; ++r) S[x][r] = 0.f;
+  if (sin) {  // from inside the state whatever the padding, so that no load hangs on a condition
+    const float* from = sin + min(col, V - 1);
+#pragma unroll
+    for (int x = 0; x < DT; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int d = 32 * x + 16 * (r >> 3) + 8 * h + (r & 7);
+        S[x][r] = from[min(d, D - 1) * V];
+      }
+  }
   float* sout = !OUT ? (float*)a.ws + (bh * (sa.nseg - 1) + seg) * sdv
                 : a.state_out && t0 + SL >= len ? a.state_out + bh * sdv : nullptr;
 
+  // Of the state, the scores and the weighted values (fp16 only; first such that
+  // values of about one do not move them).
+  Unit us = {F ? 0x1p5f : 1.f, F ? 0x1p-5f : 1.f}, up = {F ? 0x1p6f : 1.f, F ? 0x1p-6f : 1.f},
+       uv = {F ? 0x1p9f : 1.f, F ? 0x1p-9f : 1.f};
   // Decays.  Inside a diagonal 32 x 32 tile lambda^(i - j) for j <= i (i this lane's
   // token, j the register's), one tile below it lambda^(32 + i - j), both in the
   // scores' unit.  At the end of a chunk token 16 x + j counts lambda^(15 - j)
@@ -388,12 +400,12 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
     for (int r = 0; r < 16; ++r) {
       const int lag = l32 - drow(r, h);
       below |= lag >= 0 ? 1u << r : 0u;
-      mdiag[r] = __builtin_amdgcn_exp2f(max(lag, 0) * l2);
-      mlow[r] = __builtin_amdgcn_exp2f((32 + lag) * l2);
+      mdiag[r] = __builtin_amdgcn_exp2f(max(lag, 0) * l2) * up.u;
+      mlow[r] = __builtin_amdgcn_exp2f((32 + lag) * l2) * up.u;
     }
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) wage[e] = __builtin_amdgcn_exp2f((15 - (8 * (e >> 2) + 4 * h + (e & 3))) * l2);
+  for (int e = 0; e < 8; ++e) wage[e] = __builtin_amdgcn_exp2f((15 - (8 * (e >> 2) + 4 * h + (e & 3))) * l2) * uv.u;
 #pragma unroll
   for (int x = 0; x < 4; ++x) wstep[x] = __builtin_amdgcn_exp2f((48 - 16 * x) * l2);
   const float di0 = __builtin_amdgcn_exp2f((l32 + 1) * l2), d32 = __builtin_amdgcn_exp2f(32 * l2);
@@ -405,7 +417,6 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int ck0 = col_offset<DP, true>(lane, 0), ck1 = col_offset<DP, true>(lane, 1);
   const char *pv0 = lds + C::VOFF + (col_offset<VP, false>(lane, 0) ^ (64 * wave)),
              *pv1 = lds + C::VOFF + (col_offset<VP, false>(lane, 1) ^ (64 * wave));
-  Unit us, up, uv;  // of the state, the scores and the weighted values (fp16 only)
   float owed = 0.f;
   auto settle = [&]() {
 #pragma unroll
@@ -414,6 +425,17 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
       for (int r = 0; r < 16; ++r) S[x][r] = fmaf(S[x][r], owed, S[x][r]);
     owed = 0.f;
   };
+  if (sin) {
+    const bool whole = D == DP && V == VP;
+#pragma unroll
+    for (int x = 0; x < DT; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        asm volatile("" : "+v"(S[x][r]));  // or the load would move behind the condition
+        const int d = 32 * x + 16 * (r >> 3) + 8 * h + (r & 7);
+        S[x][r] = whole || (d < D && col < V) ? S[x][r] * us.u : 0.f;  // zeros in the padding
+      }
+  }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
   for (int c = 0; c < nch; ++c) {
@@ -615,12 +637,14 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
       for (int d = 0; d < DT; ++d) {
         const char *p0 = lds + ((ck0 + buf) ^ (64 * d)), *p1 = lds + ((ck1 + buf) ^ (64 * d));
         floatx16 add = {};
+        V8 kf[4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const V8 kf = read_cols<E>(p0 + 32 * DP * x, p1 + 32 * DP * x);
+        for (int x = 0; x < 4; ++x) kf[x] = read_cols<E>(p0 + 32 * DP * x, p1 + 32 * DP * x);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int y = NT - 1; y >= 0; --y) add = E::mfma(kf, term[x][y], add);
-        }
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int y = NT - 1; y >= 0; --y) add = E::mfma(kf[x], term[x][y], add);
 #pragma unroll
         for (int r = 0; r < 16; ++r) S[d][r] = F ? fmaf(add[r], gain, S[d][r] * keep.hi) : fmaf(S[d][r], keep.hi, add[r]);
       }
@@ -641,26 +665,35 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
   if (sout) {
     settle();
+    sout += col;
+    if (D == DP && V == VP) {
 #pragma unroll
-    for (int x = 0; x < DT; ++x)
+      for (int x = 0; x < DT; ++x)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int d = 32 * x + 16 * (r >> 3) + 8 * h + (r & 7);
-        if (d < D && col < V) sout[(int64_t)d * V + col] = S[x][r] * us.inv;
-      }
+        for (int r = 0; r < 16; ++r) sout[(32 * x + 16 * (r >> 3) + 8 * h + (r & 7)) * VP] = S[x][r] * us.inv;
+    } else if (col < V) {
+#pragma unroll
+      for (int x = 0; x < DT; ++x)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int d = 32 * x + 16 * (r >> 3) + 8 * h + (r & 7);
+          if (d < D) sout[d * V] = S[x][r] * us.inv;
+        }
+    }
   }
 }
 
 // Over the segments of a sequence and head: what each adds becomes the state
 // after it (slot g: the state before segment g + 1).
-__global__ __launch_bounds__(256) void k_tok_decay_scan(SegArgs sa) {
+__global__ __launch_bounds__(64) void k_tok_decay_scan(SegArgs sa) {
   const DecayArgs& a = sa.a;
   const ncodec_decay_shape& s = a.s;
   const int64_t sdv = (int64_t)s.head_dim * s.value_dim;
-  const int blocks = (int)((sdv + 255) / 256);
-  const int64_t bh = blockIdx.x / blocks, e = (int64_t)(blockIdx.x % blocks) * 256 + threadIdx.x;
+  const int blocks = (int)((sdv + 63) / 64);
+  const uint32_t bh = blockIdx.x / blocks;
+  const int64_t e = (int64_t)(blockIdx.x % blocks) * 64 + threadIdx.x;
   if (e >= sdv) return;
-  const int64_t b = bh / s.heads;
+  const uint32_t b = bh / (uint32_t)s.heads;
   const int64_t len = a.lengths ? min(max((int64_t)a.lengths[b], (int64_t)0), s.tokens) : s.tokens;
   const int64_t SL = (int64_t)sa.seg_chunks * kChunk;
   const Decay64 keep = decay_pow(a.log_decay[bh % s.heads], SL);
@@ -690,13 +723,18 @@ struct Plan {
   int seg_chunks, nseg;
 };
 
-// Segments so that about kTargetWGs workgroups share the work.
+// A chunk takes a workgroup some 4 us whether or not it has the SIMDs to itself, and
+// one wave a SIMD (1,024 of them) is where splitting a sequence stops to pay for
+// the second pass over k and v: 512 heads of 8 chunks take 44 us whole and 76 us in
+// halves.  Below that the sequences are cut so that two waves share a SIMD, into
+// segments of two chunks at least (8 heads of 128 chunks: 50 us in twos, 53 us singly).
 Plan plan_of(const ncodec_decay_shape& s) {
   Plan p{s.tokens >= kRecurTokens, 0, 1};
   const int64_t chunks = (s.tokens + kChunk - 1) / kChunk, bh = s.batch * s.heads;
   if (!p.chunked || bh == 0) return p;
-  const int64_t target = s.head_dim > 64 || s.value_dim > 64 ? 256 : 512;
-  int64_t nseg = std::max<int64_t>(1, std::min(chunks, target / bh));
+  const int64_t waves = s.value_dim <= 32 ? 1 : s.value_dim <= 64 ? 2 : 4;
+  int64_t nseg = 1;
+  if (bh * waves < 1024) nseg = std::max<int64_t>(1, std::min(chunks / 2, 2048 / (bh * waves)));
   const int64_t per = (chunks + nseg - 1) / nseg;
   p.seg_chunks = (int)per;
   p.nseg = (int)((chunks + per - 1) / per);
@@ -722,7 +760,7 @@ hipError_t chunked(const SegArgs& sa, hipStream_t st) {
   if (sa.nseg > 1) {
     launch(k_tok_decay_chunk<E, DP, NV, false, DMA>, dim3((unsigned)(bh * (sa.nseg - 1))), dim3(64 * NV), st, sa);
     const int64_t sdv = (int64_t)s.head_dim * s.value_dim;
-    launch(k_tok_decay_scan, dim3((unsigned)(bh * ((sdv + 255) / 256))), dim3(256), st, sa);
+    launch(k_tok_decay_scan, dim3((unsigned)(bh * ((sdv + 63) / 64))), dim3(64), st, sa);
   }
   launch(k_tok_decay_chunk<E, DP, NV, true, DMA>, dim3((unsigned)(bh * sa.nseg)), dim3(64 * NV), st, sa);
   return hipGetLastError();
