@@ -11,16 +11,27 @@ namespace {
 
 // Activations in fp32.  The logistic is 1 / (1 + exp(-v)) with the hardware
 // exponential and reciprocal (relative error below 2^-21, far below the
-// rounding of y); v Phi(v) goes through erfc, whose fit is relative, so the
-// tail keeps its digits.
+// rounding of y).  v Phi(v) = max(v, 0) - |v| Phi(-|v|), and Phi(-a) =
+// exp(-a^2 / 2) M(a) with M fitted on [0, 14] as t times a polynomial of degree 6
+// in t = 1 / (1 + 0.36 a) by iteratively reweighted least squares of the relative
+// error, which stays below 9e-7, so the tail keeps its digits.
 template <int ACT>
 __device__ __forceinline__ float act1(float v) {
   if (ACT == NCODEC_ACT_LRELU) return v >= 0.f ? v : 0.1f * v;
   if (ACT == NCODEC_ACT_WSILU) return v * __builtin_amdgcn_rcpf(1.f + __expf(-4.f * v));
   if (ACT == NCODEC_ACT_SILU) return v * __builtin_amdgcn_rcpf(1.f + __expf(-v));
   if (ACT == NCODEC_ACT_GELU) {
-    const float e = 0.5f * erfc_pos(0.70710678118654752f * fabsf(v));
-    return v * (v >= 0.f ? 1.f - e : e);
+    const float a = fminf(fabsf(v), 64.f);  // Phi(-64) is 0: an infinity times it would be no number
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.36f, a, 1.f));
+    float p = 0.047059200f;
+    p = fmaf(p, t, -0.179774719f);
+    p = fmaf(p, t, 0.180967717f);
+    p = fmaf(p, t, 0.0265398683f);
+    p = fmaf(p, t, 0.139722717f);
+    p = fmaf(p, t, 0.141771825f);
+    p = fmaf(p, t, 0.143713090f);
+    const float e = p * t * __builtin_amdgcn_exp2f(-0.72134752f * a * a);
+    return fmaf(-a, e, fmaxf(v, 0.f));
   }
   return v;
 }
@@ -65,29 +76,35 @@ __device__ __forceinline__ typename E::V8 load_row8(const typename E::T* p, int6
 __device__ __align__(16) uint32_t zero16[4];  // what a load past the end of the contraction reads
 
 // ---- tiles ------------------------------------------------------------------
-// WN x WM waves of 64 weight rows x 32 TB tokens each.  K streams through LDS
-// in stages of 32 (a row's stage is 64 bytes, four 16-byte units; unit u of row
-// r lies at slot u ^ (r / 4 % 4), so that 16 consecutive rows of one unit touch
-// every bank once).  DMA: rows 16-byte aligned and K a multiple of 8, staged by
-// direct global->LDS loads two stages ahead; otherwise through registers.
-// With the gate each 64-row group holds 32 rows of W1 and the same 32 of W2.
-template <class E, bool GATED, bool DMA, int WN, int WM, int TB, int BK = 32>
+// WN x WM waves of 64 weight rows x 32 TB tokens each.  K streams through LDS in
+// stages of BK = 32 or 64 (unit u, 16 bytes, of row r lies at a slot such that 16
+// consecutive rows of one unit touch every bank once).  DMA: rows 16-byte
+// aligned and K a multiple of 8, staged by direct global->LDS loads ST - 1
+// stages ahead; otherwise through registers.  With the gate each 64-row group
+// holds 32 rows of W1 and the same 32 of W2, so that both halves of an output
+// are in one lane.  A wave reads 2 + TB fragments from LDS for 2 TB MFMAs: with
+// TB = 4 the LDS takes 1.5 KiB for every two MFMAs, which its 128 B a clock just
+// carry, and the products set the pace (8192 x 4096 -> 4096 bf16 251 us, 1.10 PFLOP/s
+// of the 1.49 that the library reaches on 8192^3; 32640 x 2048 -> 512 64 us, 54.5 the
+// library).
+template <class E, bool GATED, bool DMA, int WN, int WM, int TB, int BK, int ST_>
 struct Tile {
   static constexpr int NW = WN * WM, TN = 64 * WN, TM = 32 * TB * WM, ROWS = TN + TM;
   static constexpr int OF = GATED ? 32 : 64;       // output features of a wave
-  static constexpr int ST = DMA && BK == 32 ? 3 : 2;
+  static constexpr int ST = DMA ? ST_ : 2;
   static constexpr int STAGE = ROWS * BK * 2;      // bytes
   static constexpr int U = BK / 8, RPL = 64 / U;   // units of a row, rows of a 1 KiB load
   static constexpr int LOADS = ROWS / RPL / NW;    // 1 KiB loads of a wave and stage
   static __device__ __forceinline__ int slot(int row, int u) { return u ^ (BK == 32 ? (row >> 2) & 3 : (row >> 1) & 7); }
   static constexpr int PITCH = OF * 2 + 16;        // bytes of a token's row in the epilogue
   static constexpr int LDS = ST * STAGE > NW * 32 * PITCH ? ST * STAGE : NW * 32 * PITCH;
+  static_assert(ST >= 2 && ST <= 4, "the waits in the loop count one to three stages in flight");
   static_assert(ROWS / RPL % NW == 0, "every wave stages the same number of rows");
 };
 
-template <class E, bool GATED, bool DMA, int WN, int WM, int TB, int BK = 32>
+template <class E, bool GATED, bool DMA, int WN, int WM, int TB, int BK, int ST_>
 __global__ __launch_bounds__(64 * WN * WM, 2) void k_tok_linear(LinearArgs a) {
-  typedef Tile<E, GATED, DMA, WN, WM, TB, BK> C;
+  typedef Tile<E, GATED, DMA, WN, WM, TB, BK, ST_> C;
   typedef typename E::T T;
   typedef typename E::V8 V8;
   typedef typename E::V4 V4;
@@ -155,16 +172,19 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tok_linear(LinearArgs a) {
   };
 
   if (DMA) {
-    stage_dma(0, 0);
-    if (C::ST == 3 && nk > 1) stage_dma(1, 1);
+#pragma unroll
+    for (int i = 0; i < C::ST - 1; ++i)
+      if (i < nk) stage_dma(i, i);
     int buf = 0;
     for (int kt = 0; kt < nk; ++kt) {
-      // this wave's loads of stage kt have landed (those of kt + 1 may be in flight) ...
-      if (C::ST == 3 && kt + 1 < nk)
+      // this wave's loads of stage kt have landed (those of later stages may be in flight) ...
+      if (C::ST > 3 && kt + 2 < nk)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * C::LOADS) : "memory");
+      else if (C::ST > 2 && kt + 1 < nk)
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(C::LOADS) : "memory");
       else
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      // ... and everyone's, and everyone is done with the buffer that stage kt + 2 goes to
+      // ... and everyone's, and everyone is done with the buffer that the next load goes to
       lds_barrier();
       if (kt + C::ST - 1 < nk) stage_dma(kt + C::ST - 1, buf == 0 ? C::ST - 1 : buf - 1);
       compute(buf);
@@ -205,10 +225,22 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tok_linear(LinearArgs a) {
   const T* bias = (const T*)a.b;
   const T* res = (const T*)a.r;
   T* y = (T*)a.y;
-  auto get_bias = [&](int64_t n, int64_t half, float (&v)[4]) {
+  V4 bq[2][4] = {};  // the lane's features: 32 i + 8 q + 4 h, with the gate i is the half
+  if (bias) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = bias && n + j < a.s.n ? (float)bias[half + n + j] : 0.f;
-  };
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t n = nw0 + (GATED ? 0 : 32 * i) + 8 * q + 4 * h;
+        const T* p = bias + (GATED && i ? a.s.n : 0) + n;
+        if (n + 4 <= a.s.n)
+          bq[i][q] = load_any<V4>(p);
+        else
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (n + j < a.s.n) bq[i][q][j] = p[j];
+      }
+  }
 #pragma unroll
   for (int t = 0; t < TB; ++t) {
     const int64_t mt = mw0 + 32 * t;
@@ -227,15 +259,13 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tok_linear(LinearArgs a) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int f = 32 * i + 8 * q + 4 * h;  // first of the lane's four features
-        float v[4], bv[4];
-        get_bias(nw0 + f, 0, bv);
+        float v[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = acc[i][t][4 * q + j] + bv[j];
+        for (int j = 0; j < 4; ++j) v[j] = acc[i][t][4 * q + j] + (float)bq[i][q][j];
         activate(v, a.s.act);
         if (GATED) {
-          get_bias(nw0 + f, a.s.n, bv);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] *= acc[1][t][4 * q + j] + bv[j];
+          for (int j = 0; j < 4; ++j) v[j] *= acc[1][t][4 * q + j] + (float)bq[1][q][j];
         }
         V4* slot = (V4*)(mine + l32 * C::PITCH + 2 * f);
         if (res) {
@@ -336,13 +366,13 @@ __global__ __launch_bounds__(512) void k_tok_linear_rows(LinearArgs a) {
   }
 }
 
-template <class E, bool GATED, bool DMA, int WN, int WM, int TB, int BK = 32>
+template <class E, bool GATED, bool DMA, int WN, int WM, int TB, int BK, int ST_>
 hipError_t go_tile(const LinearArgs& a, hipStream_t st) {
-  typedef Tile<E, GATED, DMA, WN, WM, TB, BK> C;
+  typedef Tile<E, GATED, DMA, WN, WM, TB, BK, ST_> C;
   int64_t grid = ((a.s.m + C::TM - 1) / C::TM) * ((a.s.n + C::OF * WN - 1) / (C::OF * WN));
   grid = (grid + kNumXCD - 1) / kNumXCD * kNumXCD;
   if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
-  launch(k_tok_linear<E, GATED, DMA, WN, WM, TB, BK>, dim3((unsigned)grid), dim3(64 * C::NW), st, a);
+  launch(k_tok_linear<E, GATED, DMA, WN, WM, TB, BK, ST_>, dim3((unsigned)grid), dim3(64 * C::NW), st, a);
   return hipGetLastError();
 }
 
@@ -353,16 +383,37 @@ hipError_t go_rows(const LinearArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Which kernel, by the size alone (times in us, bf16, both sides; m x k -> n, n the
+// weight rows).
+//  - Few outputs go to the rows kernel, whose waves share K: 130 x 2048 -> 1024
+//    10.4 there and 19.5 on the smallest tile; the two meet at about 2^19 outputs
+//    (512 x 1024 -> 1024: 11.9 and 11.7; 1000 x 256 -> 1024: 7.9 and 5.9).
+//    Its own token blocks grow with the outputs: 64 x 1024 -> 1024 4.1 / 5.0 / 7.1 with
+//    16 / 32 / 64 tokens, 512 x 256 -> 256 4.0 / 3.1 / 3.8, 1000 x 1024 -> 256 9.5 / 7.9 / 7.3.
+//  - 128 x 64 tiles (features x tokens) until they are about three a CU: 3000 x 1024 ->
+//    2048 22.0, 23.1 in 128 x 128; 6000 x 1024 -> 2048 39.1 and 36.7.
+//  - 256 x 256 from 200 of them on, where L2 traffic is what counts (8192 x 4096 -> 4096 251,
+//    288 in 256 x 128, 364 in 128 x 128), unless K is short: two workgroups of 256 x 128 a CU
+//    then hide one's epilogue behind the other's products (32640 x 512 -> 2048 with GELU,
+//    fp16: 123, 139 in 256 x 256).
+// Rows that are not 16-byte aligned go through registers; tiles of two sizes.
 template <class E, bool GATED>
 hipError_t pick(const LinearArgs& a, hipStream_t st) {
   const ncodec_linear_shape& s = a.s;
-  const int64_t nf = s.n * (GATED ? 2 : 1);
-  if (s.m <= 16) return go_rows<E, GATED, 1>(a, st);
-  if (s.m <= 128) return go_rows<E, GATED, 2>(a, st);
+  const int64_t nf = s.n * (GATED ? 2 : 1), outs = s.m * nf;
+  if (s.m <= 16 || outs <= ((int64_t)1 << 19)) {
+    if (s.m <= 16 || outs <= 96 * 1024) return go_rows<E, GATED, 1>(a, st);
+    if (s.m <= 32 || outs <= 192 * 1024) return go_rows<E, GATED, 2>(a, st);
+    return go_rows<E, GATED, 4>(a, st);
+  }
+  const auto tiles = [&](int64_t f, int64_t tok) { return ((s.m + tok - 1) / tok) * ((nf + f - 1) / f); };
   const bool dma = s.k % 8 == 0 && s.ldx % 8 == 0 && s.ldw % 8 == 0 && (uintptr_t)a.x % 16 == 0 && (uintptr_t)a.w % 16 == 0;
-  const int64_t big = ((s.m + 255) / 256) * ((nf + 255) / 256);
-  if (big >= 200) return dma ? go_tile<E, GATED, true, 4, 2, 4, 64>(a, st) : go_tile<E, GATED, false, 4, 2, 4>(a, st);
-  return dma ? go_tile<E, GATED, true, 2, 2, 2>(a, st) : go_tile<E, GATED, false, 2, 2, 2>(a, st);
+  const bool large = tiles(256, 256) >= 200;
+  if (!dma) return large ? go_tile<E, GATED, false, 4, 2, 4, 32, 2>(a, st) : go_tile<E, GATED, false, 2, 2, 2, 32, 2>(a, st);
+  if (tiles(128, 64) <= 768) return go_tile<E, GATED, true, 2, 2, 1, 64, 2>(a, st);
+  if (!large) return go_tile<E, GATED, true, 2, 2, 2, 32, 3>(a, st);
+  if (s.k >= 1024) return go_tile<E, GATED, true, 4, 2, 4, 64, 2>(a, st);
+  return go_tile<E, GATED, true, 4, 2, 2, 32, 3>(a, st);
 }
 
 }  // namespace
