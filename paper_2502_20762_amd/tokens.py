@@ -31,13 +31,13 @@ def _dtype(x):
     return dt
 
 
-def _like(t, x, what, shape=None, dtype=None):
-    """t sits with x: device, type and (if given) shape, its last dimension contiguous."""
-    if t.dtype != (dtype or x.dtype) or t.get_device() != x.get_device():
-        raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {dtype or x.dtype} on {x.device}")
-    if shape is not None and t.shape != shape:
+def _like(t, dtype, device, shape, what):
+    """t has this type, device (index) and shape, its last dimension contiguous."""
+    if t.dtype != dtype or t.get_device() != device:
+        raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {dtype} on cuda:{device}")
+    if t.shape != shape:
         raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
+    if t.stride(-1) != 1 and shape[-1] > 1:
         raise ValueError(f"{what}: the last dimension must be contiguous")
 
 
@@ -64,11 +64,6 @@ def _call(fn, index, *args):
         _nc._check(st)
 
 
-def _row_stride(t, i, width):
-    """Stride of dimension i, or the packed one where the dimension has one entry (its stride means nothing)."""
-    return t.stride(i) if t.shape[i] > 1 else max(t.stride(i), width)
-
-
 def linear(x, weight, bias=None, residual=None, act="none", gated=False, out=None):
     """``act(x W^T + b) + residual``; gated, with W = [W1; W2]: ``act(x W1^T + b1) * (x W2^T + b2) + residual``.
 
@@ -76,32 +71,41 @@ def linear(x, weight, bias=None, residual=None, act="none", gated=False, out=Non
     act: "none", "lrelu" (slope 0.1), "wsilu" (v sigmoid(4v)), "silu" or "gelu".  ``out`` may be ``residual``.
     Sums and the epilogue are float32, rounded once."""
     dt = _dtype(x)
-    if act not in ACTS:
+    act_code = ACTS.get(act)
+    if act_code is None:
         raise ValueError(f"act must be one of {sorted(ACTS)}")
-    _need(x.dim() >= 1 and weight.dim() == 2, "x needs a dimension, weight two")
-    k, rows = x.shape[-1], weight.shape[0]
+    xs, ws = x.shape, weight.shape
+    _need(len(xs) >= 1 and len(ws) == 2, "x needs a dimension, weight two")
+    k, rows = xs[-1], ws[0]
     _need(not gated or rows % 2 == 0, "a gated weight has an even number of rows")
     n = rows // 2 if gated else rows
-    _like(x, x, "x")
-    _like(weight, x, "weight", (rows, k))
-    lead = x.shape[:-1]
-    x2 = x if x.dim() == 2 else _flat(x, "x")
+    dtype, device = x.dtype, x.get_device()
+    if x.stride(-1) != 1 and k > 1:
+        raise ValueError("x: the last dimension must be contiguous")
+    _like(weight, dtype, device, (rows, k), "weight")
     if bias is not None:
-        _like(bias, x, "bias", (rows,))
-    if residual is not None:
-        _like(residual, x, "residual", lead + (n,))
-    y = out
-    if y is None:
-        y = x.new_empty(lead + (n,))
+        _like(bias, dtype, device, (rows,), "bias")
+    ys = (*xs[:-1], n)
+    if out is None:
+        y = x.new_empty(ys)
     else:
-        _like(y, x, "out", lead + (n,))
-    y2 = y if y.dim() == 2 else _flat(y, "out")
-    r2 = None if residual is None else residual if residual.dim() == 2 else _flat(residual, "residual")
-    shape = _nc.ncodec_linear_shape(dt, ACTS[act], 1 if gated else 0, 0, x2.shape[0], n, k, _row_stride(x2, 0, k),
-                                    _row_stride(weight, 0, k), 0 if r2 is None else _row_stride(r2, 0, n),
-                                    _row_stride(y2, 0, n))
-    _call(_nc.load_library().ncodec_linear, x.get_device(), ctypes.byref(shape), _ptr(x), _ptr(weight), _ptr(bias),
-          _ptr(residual), _ptr(y))
+        y = out
+        _like(y, dtype, device, ys, "out")
+    flat = len(xs) == 2
+    x2, y2 = (x, y) if flat else (_flat(x, "x"), _flat(y, "out"))
+    ldr = 0
+    if residual is not None:
+        _like(residual, dtype, device, ys, "residual")
+        ldr = (residual if flat else _flat(residual, "residual")).stride(0)
+    m = x2.shape[0]
+    if m == 1:  # the stride of a dimension with one entry means nothing
+        ldx, ldy, ldr = k, n, n
+    else:
+        ldx, ldy = x2.stride(0), y2.stride(0)
+    shape = _nc.ncodec_linear_shape(dt, act_code, 1 if gated else 0, 0, m, n, k, ldx,
+                                    weight.stride(0) if rows > 1 else k, ldr, ldy)
+    _call(_nc.load_library().ncodec_linear, device, ctypes.byref(shape), x.data_ptr(), weight.data_ptr(), _ptr(bias),
+          _ptr(residual), y.data_ptr())
     return y
 
 
@@ -134,35 +138,40 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, positions=None, freq=None, 
     float32 radians per step (:func:`rope_frequencies`).  Without sections there is no rotation.  ``q_out`` and
     ``k_out`` may be q and k themselves."""
     dt = _dtype(q)
-    _need(q.dim() == 3 and k.dim() == 3, "q and k must be (tokens, heads, dim)")
-    T, hq, D = q.shape
-    hk = k.shape[1]
-    _like(q, q, "q")
-    _like(k, q, "k", (T, hk, D))
-    for w in (q_weight, k_weight):
-        if w is not None:
-            _need(norm, "weights without a norm")
-            _like(w, q, "norm weight", (D,))
+    qs, ks = q.shape, k.shape
+    _need(len(qs) == 3 and len(ks) == 3, "q and k must be (tokens, heads, dim)")
+    T, hq, D = qs
+    hk = ks[1]
+    dtype, device = q.dtype, q.get_device()
+    _like(q, dtype, device, qs, "q")
+    _like(k, dtype, device, (T, hk, D), "k")
+    _need(norm or (q_weight is None and k_weight is None), "weights without a norm")
+    if q_weight is not None:
+        _like(q_weight, dtype, device, (D,), "q_weight")
+    if k_weight is not None:
+        _like(k_weight, dtype, device, (D,), "k_weight")
     axes = len(sections)
-    _need(axes <= 3, "at most three axes")
+    pos = fr = None
     if axes:
+        _need(axes <= 3, "at most three axes")
         _need(positions is not None and freq is not None, "a rotation needs positions and freq")
-        _like(positions, q, "positions", (T, axes), torch.int32)
+        _like(positions, torch.int32, device, (T, axes), "positions")
         _need(positions.is_contiguous(), "positions must be contiguous")
-        _like(freq, q, "freq", (sum(sections),), torch.float32)
+        _like(freq, torch.float32, device, (sum(sections),), "freq")
+        pos, fr = positions.data_ptr(), freq.data_ptr()
     if q_out is None:
         q_out = q.new_empty((T, hq, D))
     else:
-        _like(q_out, q, "q_out", (T, hq, D))
+        _like(q_out, dtype, device, qs, "q_out")
     if k_out is None:
         k_out = q.new_empty((T, hk, D))
     else:
-        _like(k_out, q, "k_out", (T, hk, D))
-    shape = _nc.ncodec_qk_shape(dt, 1 if norm else 0, axes, tuple(sections) + (0,) * (3 - axes),
-                                1 if interleaved else 0, hq, hk, D, eps, 0, T, q.stride(0), q.stride(1), k.stride(0),
-                                k.stride(1), q_out.stride(0), q_out.stride(1), k_out.stride(0), k_out.stride(1))
-    _call(_nc.load_library().ncodec_qk_norm_rope, q.get_device(), ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(q_weight),
-          _ptr(k_weight), _ptr(positions) if axes else None, _ptr(freq) if axes else None, _ptr(q_out), _ptr(k_out))
+        _like(k_out, dtype, device, ks, "k_out")
+    a, b, c, d = q.stride(), k.stride(), q_out.stride(), k_out.stride()
+    shape = _nc.ncodec_qk_shape(dt, 1 if norm else 0, axes, (*sections, 0, 0, 0)[:3], 1 if interleaved else 0, hq, hk, D,
+                                eps, 0, T, a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1])
+    _call(_nc.load_library().ncodec_qk_norm_rope, device, ctypes.byref(shape), q.data_ptr(), k.data_ptr(),
+          _ptr(q_weight), _ptr(k_weight), pos, fr, q_out.data_ptr(), k_out.data_ptr())
     return q_out, k_out
 
 
@@ -176,35 +185,36 @@ def decay_attention(q, k, v, log_decay, state=None, lengths=None, scale=None, re
     dim^-0.5.  Returns o (batch, tokens, heads, value_dim), with return_state (o, state after the last token).
     ``state_out`` may be ``state`` itself: one token per call is the recurrent form."""
     dt = _dtype(q)
-    _need(q.dim() == 4 and k.dim() == 4 and v.dim() == 4, "q, k and v must be (batch, tokens, heads, dim)")
-    B, T, H, D = q.shape
-    hk, V = k.shape[2], v.shape[3]
+    qs, ks, vs = q.shape, k.shape, v.shape
+    _need(len(qs) == 4 and len(ks) == 4 and len(vs) == 4, "q, k and v must be (batch, tokens, heads, dim)")
+    B, T, H, D = qs
+    hk, V = ks[2], vs[3]
     _need(D >= 1, "q needs a head dimension")
-    _like(q, q, "q")
-    _like(k, q, "k", (B, T, hk, D))
-    _like(v, q, "v", (B, T, hk, V))
-    _like(log_decay, q, "log_decay", (H,), torch.float32)
+    dtype, device = q.dtype, q.get_device()
+    _like(q, dtype, device, qs, "q")
+    _like(k, dtype, device, (B, T, hk, D), "k")
+    _like(v, dtype, device, (B, T, hk, V), "v")
+    _like(log_decay, torch.float32, device, (H,), "log_decay")
     if lengths is not None:
-        _like(lengths, q, "lengths", (B,), torch.int32)
+        _like(lengths, torch.int32, device, (B,), "lengths")
     if state is not None:
-        _like(state, q, "state", (B, H, D, V), torch.float32)
+        _like(state, torch.float32, device, (B, H, D, V), "state")
         _need(state.is_contiguous(), "state must be contiguous")
-    if state_out is None:
-        if return_state:
-            state_out = q.new_empty((B, H, D, V), dtype=torch.float32)
-    else:
-        _like(state_out, q, "state_out", (B, H, D, V), torch.float32)
+    if state_out is not None:
+        _like(state_out, torch.float32, device, (B, H, D, V), "state_out")
         _need(state_out.is_contiguous(), "state_out must be contiguous")
+    elif return_state:
+        state_out = q.new_empty((B, H, D, V), dtype=torch.float32)
     if out is None:
         out = q.new_empty((B, T, H, V))
     else:
-        _like(out, q, "out", (B, T, H, V))
+        _like(out, dtype, device, (B, T, H, V), "out")
     shape = _nc.ncodec_decay_shape(dt, H, hk, D, V, D ** -0.5 if scale is None else scale, B, T, *q.stride()[:3],
                                    *k.stride()[:3], *v.stride()[:3], *out.stride()[:3])
     lib = _nc.load_library()
     ref = ctypes.byref(shape)
     need = lib.ncodec_decay_attention_workspace_bytes(ref)
     ws = q.new_empty(need, dtype=torch.uint8) if need else None
-    _call(lib.ncodec_decay_attention, q.get_device(), ref, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lengths),
-          _ptr(state), _ptr(state_out), _ptr(out), _ptr(ws), need)
+    _call(lib.ncodec_decay_attention, device, ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(),
+          _ptr(lengths), _ptr(state), _ptr(state_out), out.data_ptr(), _ptr(ws), need)
     return (out, state_out) if return_state else out
