@@ -7,7 +7,14 @@
 
 namespace {
 
-using nc::set_error;
+// Records the message; nothing is thrown across the C entry.
+ncodec_status set_error(ncodec_status st, const char* where, const char* why, size_t bytes = 0) noexcept {
+  try {
+    return nc::set_error(st, std::string(where) + ": " + why + (bytes ? std::to_string(bytes) + " bytes" : ""));
+  } catch (...) {
+    return st;
+  }
+}
 
 constexpr int64_t kMaxRows = (int64_t)1 << 31;
 constexpr int64_t kMaxStride = (int64_t)1 << 40;
@@ -18,7 +25,7 @@ bool stride_ok(int64_t s) { return s >= 0 && s <= kMaxStride; }
 
 ncodec_status finish(hipError_t e, const char* where) {
   if (e == hipSuccess) return NCODEC_OK;
-  return set_error(NCODEC_EHIP, std::string(where) + ": " + hipGetErrorString(e));
+  return set_error(NCODEC_EHIP, where, hipGetErrorString(e));
 }
 
 // Why a shape is refused, or NULL.
@@ -90,34 +97,34 @@ const char* decay_fault(const ncodec_decay_shape& s, ncodec_status* st) {
 
 extern "C" ncodec_status ncodec_linear(const ncodec_linear_shape* shape, const void* d_x, const void* d_w,
                                        const void* d_b, const void* d_r, void* d_y, void* hip_stream) {
-  if (!shape) return set_error(NCODEC_EINVAL, "linear: shape is NULL");
+  if (!shape) return set_error(NCODEC_EINVAL, "linear", "shape is NULL");
   ncodec_status st;
-  if (const char* why = linear_fault(*shape, &st)) return set_error(st, std::string("linear: ") + why);
+  if (const char* why = linear_fault(*shape, &st)) return set_error(st, "linear", why);
   if (d_r && (shape->ldr < shape->n || !stride_ok(shape->ldr)))
-    return set_error(NCODEC_ESHAPE, "linear: ldr is below n or above 2^40");
+    return set_error(NCODEC_ESHAPE, "linear", "ldr is below n or above 2^40");
   if (shape->m == 0) return NCODEC_OK;
-  if (!d_x || !d_w || !d_y) return set_error(NCODEC_EINVAL, "linear: d_x, d_w and d_y must be non-NULL");
+  if (!d_x || !d_w || !d_y) return set_error(NCODEC_EINVAL, "linear", "d_x, d_w and d_y must be non-NULL");
   if (!aligned(d_x, 2) || !aligned(d_w, 2) || !aligned(d_y, 2) || !aligned(d_b, 2) || !aligned(d_r, 2))
-    return set_error(NCODEC_EINVAL, "linear: a pointer is not aligned to an element");
+    return set_error(NCODEC_EINVAL, "linear", "a pointer is not aligned to an element");
   if (d_r == d_y && d_r && shape->ldr != shape->ldy)
-    return set_error(NCODEC_EINVAL, "linear: d_y is d_r, but ldy is not ldr");
+    return set_error(NCODEC_EINVAL, "linear", "d_y is d_r, but ldy is not ldr");
   return finish(nc::launch_linear({*shape, d_x, d_w, d_b, d_r, d_y}, (hipStream_t)hip_stream), "linear");
 }
 
 extern "C" ncodec_status ncodec_qk_norm_rope(const ncodec_qk_shape* shape, const void* d_q, const void* d_k,
                                              const void* d_wq, const void* d_wk, const int32_t* d_pos,
                                              const float* d_freq, void* d_qo, void* d_ko, void* hip_stream) {
-  if (!shape) return set_error(NCODEC_EINVAL, "qk_norm_rope: shape is NULL");
+  if (!shape) return set_error(NCODEC_EINVAL, "qk_norm_rope", "shape is NULL");
   ncodec_status st;
-  if (const char* why = qk_fault(*shape, &st)) return set_error(st, std::string("qk_norm_rope: ") + why);
+  if (const char* why = qk_fault(*shape, &st)) return set_error(st, "qk_norm_rope", why);
   if (shape->tokens == 0 || shape->q_heads + shape->k_heads == 0) return NCODEC_OK;
-  if (shape->q_heads && (!d_q || !d_qo)) return set_error(NCODEC_EINVAL, "qk_norm_rope: d_q and d_qo must be non-NULL");
-  if (shape->k_heads && (!d_k || !d_ko)) return set_error(NCODEC_EINVAL, "qk_norm_rope: d_k and d_ko must be non-NULL");
+  if (shape->q_heads && (!d_q || !d_qo)) return set_error(NCODEC_EINVAL, "qk_norm_rope", "d_q and d_qo must be non-NULL");
+  if (shape->k_heads && (!d_k || !d_ko)) return set_error(NCODEC_EINVAL, "qk_norm_rope", "d_k and d_ko must be non-NULL");
   const bool rot = shape->section[0] + shape->section[1] + shape->section[2] > 0;
-  if (rot && (!d_pos || !d_freq)) return set_error(NCODEC_EINVAL, "qk_norm_rope: d_pos and d_freq must be non-NULL");
+  if (rot && (!d_pos || !d_freq)) return set_error(NCODEC_EINVAL, "qk_norm_rope", "d_pos and d_freq must be non-NULL");
   if (!aligned(d_q, 2) || !aligned(d_k, 2) || !aligned(d_qo, 2) || !aligned(d_ko, 2) || !aligned(d_wq, 2) ||
       !aligned(d_wk, 2) || (rot && (!aligned(d_pos, 4) || !aligned(d_freq, 4))))
-    return set_error(NCODEC_EINVAL, "qk_norm_rope: a pointer is not aligned to an element");
+    return set_error(NCODEC_EINVAL, "qk_norm_rope", "a pointer is not aligned to an element");
   return finish(nc::launch_qk_norm_rope({*shape, d_q, d_k, d_wq, d_wk, d_pos, d_freq, d_qo, d_ko},
                                         (hipStream_t)hip_stream),
                 "qk_norm_rope");
@@ -133,20 +140,19 @@ extern "C" ncodec_status ncodec_decay_attention(const ncodec_decay_shape* shape,
                                                 const void* d_v, const float* d_log_decay, const int32_t* d_lengths,
                                                 const float* d_state_in, float* d_state_out, void* d_o,
                                                 void* d_workspace, size_t ws_bytes, void* hip_stream) {
-  if (!shape) return set_error(NCODEC_EINVAL, "decay_attention: shape is NULL");
+  if (!shape) return set_error(NCODEC_EINVAL, "decay_attention", "shape is NULL");
   ncodec_status st;
-  if (const char* why = decay_fault(*shape, &st)) return set_error(st, std::string("decay_attention: ") + why);
+  if (const char* why = decay_fault(*shape, &st)) return set_error(st, "decay_attention", why);
   if (shape->batch == 0) return NCODEC_OK;
-  if (!d_log_decay) return set_error(NCODEC_EINVAL, "decay_attention: d_log_decay is NULL");
+  if (!d_log_decay) return set_error(NCODEC_EINVAL, "decay_attention", "d_log_decay is NULL");
   if (shape->tokens > 0 && (!d_q || !d_k || !d_v || !d_o))
-    return set_error(NCODEC_EINVAL, "decay_attention: d_q, d_k, d_v and d_o must be non-NULL");
+    return set_error(NCODEC_EINVAL, "decay_attention", "d_q, d_k, d_v and d_o must be non-NULL");
   if (!aligned(d_q, 2) || !aligned(d_k, 2) || !aligned(d_v, 2) || !aligned(d_o, 2) || !aligned(d_log_decay, 4) ||
       !aligned(d_lengths, 4) || !aligned(d_state_in, 4) || !aligned(d_state_out, 4))
-    return set_error(NCODEC_EINVAL, "decay_attention: a pointer is not aligned to an element");
+    return set_error(NCODEC_EINVAL, "decay_attention", "a pointer is not aligned to an element");
   const size_t need = nc::decay_workspace_bytes(*shape);
   if (need && (!d_workspace || ws_bytes < need || !aligned(d_workspace, 256)))
-    return set_error(NCODEC_ENOMEM, "decay_attention: the workspace must be 256-byte aligned and hold " +
-                                        std::to_string(need) + " bytes");
+    return set_error(NCODEC_ENOMEM, "decay_attention", "the workspace must be 256-byte aligned and hold ", need);
   return finish(nc::launch_decay_attention({*shape, d_q, d_k, d_v, d_log_decay, d_lengths, d_state_in, d_state_out,
                                             d_o, d_workspace},
                                            (hipStream_t)hip_stream),

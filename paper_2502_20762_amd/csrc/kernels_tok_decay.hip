@@ -22,35 +22,54 @@ __device__ __forceinline__ float log2_decay(float log_decay) {
   return fmaxf(fminf(log_decay, 0.f), -1e30f) * 1.44269504088896341f;
 }
 
+struct Decay64 {  // lambda^n in two floats, so that long products of it lose nothing
+  float hi, lo;
+};
+__device__ __forceinline__ Decay64 decay_pow(float log_decay, int64_t n) {
+  const double l = fmax(fmin((double)log_decay, 0.0), -1e30);
+  const double f = exp((double)n * l);
+  const float hi = (float)f;
+  return {hi, (float)(f - (double)hi)};
+}
+
 // The recurrence itself, token by token.  A workgroup holds 64 columns of one
 // sequence's and head's state in registers: thread (g, c) the rows g + 16 r and
-// the columns 4 c .. 4 c + 3.
-template <class E, int R>
+// the columns 4 c .. 4 c + 3.  For one token it reads and writes the state once and is
+// bound by that.  VEC: value_dim a multiple of 4 and states 16-byte aligned.
+template <class E, int R, bool VEC>
 __global__ __launch_bounds__(256) void k_tok_decay_recur(DecayArgs a) {
   typedef typename E::T T;
   __shared__ float qs[16 * R], ks[16 * R], part[4][64];
   const ncodec_decay_shape& s = a.s;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c = lane & 15, g = wave * 4 + (lane >> 4);
-  const int64_t b = blockIdx.x / s.heads, h = blockIdx.x % s.heads, hk = h / (s.heads / s.kv_heads);
+  const uint32_t b = blockIdx.x / (uint32_t)s.heads, h = blockIdx.x - b * s.heads,
+                 hk = h / ((uint32_t)s.heads / (uint32_t)s.kv_heads);
   const int D = s.head_dim, V = s.value_dim, v0 = blockIdx.y * 64 + 4 * c;
-  const float lam = exp2f(log2_decay(a.log_decay[h]));
   const int64_t len = a.lengths ? min(max((int64_t)a.lengths[b], (int64_t)0), s.tokens) : s.tokens;
   const T* q = (const T*)a.q + b * s.q_batch_stride + h * s.q_head_stride;
   const T* k = (const T*)a.k + b * s.k_batch_stride + hk * s.k_head_stride;
   const T* v = (const T*)a.v + b * s.v_batch_stride + hk * s.v_head_stride;
   T* o = (T*)a.o + b * s.o_batch_stride + h * s.o_head_stride;
-  const int64_t sbase = (b * s.heads + h) * (int64_t)D * V;
+  const int64_t sbase = (int64_t)blockIdx.x * D * V;
   float S[R][4];
 #pragma unroll
-  for (int r = 0; r < R; ++r)
+  for (int r = 0; r < R; ++r) {
+    const int d = g + 16 * r;
+    const float* p = a.state_in + sbase + d * V + v0;
+    if (VEC && a.state_in && d < D && v0 < V) {
+      const floatx4 f = *(const floatx4*)p;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int d = g + 16 * r;
-      S[r][j] = a.state_in && d < D && v0 + j < V ? a.state_in[sbase + d * V + v0 + j] : 0.f;
+      for (int j = 0; j < 4; ++j) S[r][j] = f[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) S[r][j] = !VEC && a.state_in && d < D && v0 + j < V ? p[j] : 0.f;
     }
+  }
+  // lambda in two floats: it multiplies the state once a token, call after call
+  const Decay64 lam = decay_pow(a.log_decay[h], 1);
   for (int64_t t = 0; t < len; ++t) {
-    __syncthreads();
+    if (t) __syncthreads();
     if (threadIdx.x < 16 * R) {
       const int d = threadIdx.x;
       qs[d] = d < D ? (float)q[t * s.q_token_stride + d] * s.scale : 0.f;
@@ -65,7 +84,7 @@ __global__ __launch_bounds__(256) void k_tok_decay_recur(DecayArgs a) {
       const float kd = ks[g + 16 * r], qd = qs[g + 16 * r];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        S[r][j] = fmaf(kd, vv[j], lam * S[r][j]);
+        S[r][j] = fmaf(S[r][j], lam.hi, fmaf(S[r][j], lam.lo, kd * vv[j]));
         ov[j] = fmaf(qd, S[r][j], ov[j]);
       }
     }
@@ -89,12 +108,17 @@ __global__ __launch_bounds__(256) void k_tok_decay_recur(DecayArgs a) {
   }
   if (a.state_out) {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) {
+      const int d = g + 16 * r;
+      float* p = a.state_out + sbase + d * V + v0;
+      if (VEC) {
+        if (d < D && v0 < V) *(floatx4*)p = floatx4{S[r][0], S[r][1], S[r][2], S[r][3]};
+      } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int d = g + 16 * r;
-        if (d < D && v0 + j < V) a.state_out[sbase + d * V + v0 + j] = S[r][j];
+        for (int j = 0; j < 4; ++j)
+          if (d < D && v0 + j < V) p[j] = S[r][j];
       }
+    }
   }
 }
 
@@ -278,16 +302,6 @@ struct Unit {
   }
 };
 
-struct Decay64 {  // lambda^n in two floats, so that long products of it lose nothing
-  float hi, lo;
-};
-__device__ __forceinline__ Decay64 decay_pow(float log_decay, int64_t n) {
-  const double l = fmax(fmin((double)log_decay, 0.0), -1e30);
-  const double f = exp((double)n * l);
-  const float hi = (float)f;
-  return {hi, (float)(f - (double)hi)};
-}
-
 struct SegArgs {
   DecayArgs a;
   int seg_chunks;  // chunks of a segment
@@ -366,8 +380,13 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const float log_decay = a.log_decay[hd];
   const float l2 = log2_decay(log_decay);
   floatx16 S[DT];
-  const float* sin = !OUT ? nullptr : seg == 0 ? a.state_in : (const float*)a.ws + (bh * (sa.nseg - 1) + seg - 1) * sdv;
-  if (seg == 0 && sin) sin += bh * sdv;
+  // With segments the scan has put the state before each into the workspace, the
+  // caller's too: state_out, which may be the same memory, is written while other
+  // segments still begin.
+  const float* sin = !OUT ? nullptr
+                     : sa.nseg > 1 ? (const float*)a.ws + (bh * sa.nseg + seg) * sdv
+                     : a.state_in  ? a.state_in + bh * sdv
+                                   : nullptr;
 #pragma unroll
   for (int x = 0; x < DT; ++x)
 #pragma unroll
@@ -382,7 +401,7 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
         S[x][r] = from[min(d, D - 1) * V];
       }
   }
-  float* sout = !OUT ? (float*)a.ws + (bh * (sa.nseg - 1) + seg) * sdv
+  float* sout = !OUT ? (float*)a.ws + (bh * sa.nseg + seg + 1) * sdv
                 : a.state_out && t0 + SL >= len ? a.state_out + bh * sdv : nullptr;
 
   // Of the state, the scores and the weighted values (fp16 only; first such that
@@ -683,35 +702,56 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
 }
 
-// Over the segments of a sequence and head: what each adds becomes the state
-// after it (slot g: the state before segment g + 1).
-__global__ __launch_bounds__(64) void k_tok_decay_scan(SegArgs sa) {
+// Over the segments of a sequence and head: slot g + 1, what segment g adds, becomes
+// the state before segment g + 1; slot 0 the state before the first.  A workgroup
+// has 64 VEC elements of the state and a wave for every M segments (eight at
+// most): wave j takes segments j M .. j M + M - 1, all its loads in flight, first alone,
+// then from the state that the waves before it give.  VEC: 4 where the state is a
+// multiple of 4, which also forms the decays (64-bit exponentials) for four elements
+// at a time.
+constexpr int kScanM = 8;
+template <int VEC>
+__global__ __launch_bounds__(512) void k_tok_decay_scan(SegArgs sa) {
+  typedef float FV __attribute__((ext_vector_type(VEC)));
+  __shared__ FV part[8][64];
   const DecayArgs& a = sa.a;
   const ncodec_decay_shape& s = a.s;
   const int64_t sdv = (int64_t)s.head_dim * s.value_dim;
-  const int blocks = (int)((sdv + 63) / 64);
-  const uint32_t bh = blockIdx.x / blocks;
-  const int64_t e = (int64_t)(blockIdx.x % blocks) * 64 + threadIdx.x;
-  if (e >= sdv) return;
-  const uint32_t b = bh / (uint32_t)s.heads;
+  const int blocks = (int)((sdv + 64 * VEC - 1) / (64 * VEC));
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const uint32_t bh = blockIdx.x / blocks, b = bh / (uint32_t)s.heads;
+  const int64_t e = ((int64_t)(blockIdx.x % blocks) * 64 + lane) * VEC;
+  const bool in = e < sdv;
   const int64_t len = a.lengths ? min(max((int64_t)a.lengths[b], (int64_t)0), s.tokens) : s.tokens;
   const int64_t SL = (int64_t)sa.seg_chunks * kChunk;
-  const Decay64 keep = decay_pow(a.log_decay[bh % s.heads], SL);
-  const int last = (int)min((len + SL - 1) / SL, (int64_t)sa.nseg) - 1;  // segment 0 .. last have tokens
-  float* ws = (float*)a.ws + bh * (sa.nseg - 1) * sdv + e;
-  float S = a.state_in ? a.state_in[bh * sdv + e] : 0.f;
-  // the loads do not depend on each other: sixteen in flight
-  constexpr int N = 16;
-  for (int g0 = 0; g0 < last; g0 += N) {
-    float add[N];
+  const int last = (int)min((len + SL - 1) / SL, (int64_t)sa.nseg) - 1;  // segments 0 .. last have tokens
+  float* ws = (float*)a.ws + (int64_t)bh * sa.nseg * sdv + (in ? e : 0);
+  FV S = {};
+  if (in && a.state_in) __builtin_memcpy(&S, a.state_in + bh * sdv + e, sizeof(FV));
+  if (in && wave == 0) *(FV*)ws = S;
+  const float ld = a.log_decay[bh % (uint32_t)s.heads];
+  const Decay64 keep = decay_pow(ld, SL), all = decay_pow(ld, kScanM * SL);
+  const auto step = [](FV x, const Decay64& f, FV add) { return x * f.hi + (x * f.lo + add); };
+  for (int g0 = 0; g0 < last; g0 += waves * kScanM) {
+    const int first = g0 + wave * kScanM;
+    FV add[kScanM], mine = {};
 #pragma unroll
-    for (int i = 0; i < N; ++i) add[i] = g0 + i < last ? ws[(g0 + i) * sdv] : 0.f;
+    for (int i = 0; i < kScanM; ++i) add[i] = first + i < last ? *(const FV*)(ws + (first + i + 1) * sdv) : FV{};
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (g0 + i >= last) break;
-      S = fmaf(S, keep.hi, fmaf(S, keep.lo, add[i]));
-      ws[(g0 + i) * sdv] = S;
+    for (int i = 0; i < kScanM; ++i) mine = step(mine, keep, add[i]);
+    part[wave][lane] = mine;
+    __syncthreads();
+    FV P = S;
+    for (int j = 0; j < waves; ++j) {
+      if (j == wave) P = S;
+      S = step(S, all, part[j][lane]);
     }
+#pragma unroll
+    for (int i = 0; i < kScanM; ++i) {
+      P = step(P, keep, add[i]);
+      if (in && first + i < last) *(FV*)(ws + (first + i + 1) * sdv) = P;
+    }
+    __syncthreads();
   }
 }
 
@@ -741,15 +781,15 @@ Plan plan_of(const ncodec_decay_shape& s) {
   return p;
 }
 
-template <class E>
+template <class E, bool VEC>
 hipError_t recur(const DecayArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)(a.s.batch * a.s.heads), (unsigned)((a.s.value_dim + 63) / 64));
   if (a.s.head_dim <= 32)
-    launch(k_tok_decay_recur<E, 2>, grid, dim3(256), st, a);
+    launch(k_tok_decay_recur<E, 2, VEC>, grid, dim3(256), st, a);
   else if (a.s.head_dim <= 64)
-    launch(k_tok_decay_recur<E, 4>, grid, dim3(256), st, a);
+    launch(k_tok_decay_recur<E, 4, VEC>, grid, dim3(256), st, a);
   else
-    launch(k_tok_decay_recur<E, 8>, grid, dim3(256), st, a);
+    launch(k_tok_decay_recur<E, 8, VEC>, grid, dim3(256), st, a);
   return hipGetLastError();
 }
 
@@ -760,7 +800,11 @@ hipError_t chunked(const SegArgs& sa, hipStream_t st) {
   if (sa.nseg > 1) {
     launch(k_tok_decay_chunk<E, DP, NV, false, DMA>, dim3((unsigned)(bh * (sa.nseg - 1))), dim3(64 * NV), st, sa);
     const int64_t sdv = (int64_t)s.head_dim * s.value_dim;
-    launch(k_tok_decay_scan, dim3((unsigned)(bh * ((sdv + 63) / 64))), dim3(64), st, sa);
+    const unsigned waves = (unsigned)std::min(8, (sa.nseg - 2) / kScanM + 1);
+    if (sdv % 4 == 0)
+      launch(k_tok_decay_scan<4>, dim3((unsigned)(bh * ((sdv + 255) / 256))), dim3(64 * waves), st, sa);
+    else
+      launch(k_tok_decay_scan<1>, dim3((unsigned)(bh * ((sdv + 63) / 64))), dim3(64 * waves), st, sa);
   }
   launch(k_tok_decay_chunk<E, DP, NV, true, DMA>, dim3((unsigned)(bh * sa.nseg)), dim3(64 * NV), st, sa);
   return hipGetLastError();
@@ -783,7 +827,10 @@ template <class E>
 hipError_t run(const DecayArgs& a, hipStream_t st) {
   const ncodec_decay_shape& s = a.s;
   const Plan p = plan_of(s);
-  if (!p.chunked) return recur<E>(a, st);
+  if (!p.chunked) {
+    const bool vec = s.value_dim % 4 == 0 && (uintptr_t)a.state_in % 16 == 0 && (uintptr_t)a.state_out % 16 == 0;
+    return vec ? recur<E, true>(a, st) : recur<E, false>(a, st);
+  }
   const auto direct = [](const void* x, int64_t batch, int64_t token, int64_t head) {
     return (uintptr_t)x % 16 == 0 && batch % 8 == 0 && token % 8 == 0 && head % 8 == 0 && token < (1 << 26);
   };
@@ -799,7 +846,8 @@ hipError_t run(const DecayArgs& a, hipStream_t st) {
 
 size_t decay_workspace_bytes(const ncodec_decay_shape& s) {
   const Plan p = plan_of(s);
-  return (size_t)(s.batch * s.heads) * (size_t)(p.nseg - 1) * (size_t)(s.head_dim * s.value_dim) * 4;
+  if (p.nseg == 1) return 0;
+  return (size_t)(s.batch * s.heads) * (size_t)p.nseg * (size_t)(s.head_dim * s.value_dim) * 4;
 }
 
 hipError_t launch_decay_attention(const DecayArgs& a, hipStream_t st) {

@@ -417,6 +417,18 @@ def test_decay_state_options(T):
         assert bool((S == 0).all())
 
 
+@pytest.mark.parametrize("B,T,H,D", [(1, 1, 2, 64), (1, 5, 1, 32), (2, 64, 2, 64), (1, 2000, 1, 64), (1, 900, 3, 128)])
+def test_decay_state_in_place_is_the_state_apart(B, T, H, D):
+    # also where a sequence is cut into segments, which begin and end at different times
+    g = gen(25)
+    q, k, v = (rnd(g, (B, T, H, D), "fp16").to(DEV) for _ in range(3))
+    ld = torch.full((H,), -0.01, device=DEV)
+    S = torch.randn((B, H, D, D), generator=g).to(DEV)
+    o, S1 = tk.decay_attention(q, k, v, ld, S, return_state=True)
+    o2, S2 = tk.decay_attention(q, k, v, ld, S, return_state=True, state_out=S)
+    assert S2.data_ptr() == S.data_ptr() and torch.equal(o, o2) and torch.equal(S1, S2)
+
+
 @pytest.mark.parametrize("T", [1, 50, 400])
 @pytest.mark.parametrize("mag", [2.0 ** -7, 40.0])
 def test_decay_magnitudes(mag, T):
