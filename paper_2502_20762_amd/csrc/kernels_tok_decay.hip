@@ -436,6 +436,9 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int ck0 = col_offset<DP, true>(lane, 0), ck1 = col_offset<DP, true>(lane, 1);
   const char *pv0 = lds + C::VOFF + (col_offset<VP, false>(lane, 0) ^ (64 * wave)),
              *pv1 = lds + C::VOFF + (col_offset<VP, false>(lane, 1) ^ (64 * wave));
+  // what rounding lambda^n to its hi part leaves out of a state, relative to it
+  const float rest = keep.hi > 0.f ? keep.lo / keep.hi : 0.f;
+  const float rest_last = keep_last.hi > 0.f ? keep_last.lo / keep_last.hi : 0.f;
   float owed = 0.f;
   auto settle = [&]() {
 #pragma unroll
@@ -667,8 +670,8 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
         for (int r = 0; r < 16; ++r) S[d][r] = F ? fmaf(add[r], gain, S[d][r] * keep.hi) : fmaf(S[d][r], keep.hi, add[r]);
       }
-      // what rounding lambda^n to keep.hi left out, made up for every sixteenth chunk
-      owed += keep.hi > 0.f ? keep.lo / keep.hi : 0.f;
+      // made up for every sixteenth chunk
+      owed += pad ? rest_last : rest;
       if ((c & 15) == 15) settle();
       if (any_bad) {
         asm volatile("");  // a branch, not a select for each register

@@ -84,8 +84,8 @@ __device__ __align__(16) uint32_t zero16[4];  // what a load past the end of the
 // holds 32 rows of W1 and the same 32 of W2, so that both halves of an output
 // are in one lane.  A wave reads 2 + TB fragments from LDS for 2 TB MFMAs: with
 // TB = 4 the LDS takes 1.5 KiB for every two MFMAs, which its 128 B a clock just
-// carry, and the products set the pace (8192 x 4096 -> 4096 bf16 251 us, 1.10 PFLOP/s
-// of the 1.49 that the library reaches on 8192^3; 32640 x 2048 -> 512 64 us, 54.5 the
+// carry, and the products set the pace (8192 x 4096 -> 4096 bf16 231 us, 1.19 PFLOP/s
+// of the 1.49 that the library reaches on 8192^3; 32640 x 2048 -> 512 63 us, 54.5 the
 // library).
 template <class E, bool GATED, bool DMA, int WN, int WM, int TB, int BK, int ST_>
 struct Tile {
@@ -149,25 +149,43 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tok_linear(LinearArgs a) {
   };
 
   floatx16 acc[2][TB] = {};
+  // The fragments of a step of 16 are read between the MFMAs of the step before, one
+  // after each (8192 x 4096 -> 4096 bf16: 243 us with the reads right before their
+  // use, 231 so).
   auto compute = [&](int buf) {
     const char* base = lds + buf * C::STAGE;
-#pragma unroll
-    for (int s = 0; s < BK / 16; ++s) {
-      V8 fa[2], fb[TB];
+    constexpr int S = BK / 16;
+    V8 fa[2][2], fb[2][TB];
+    auto get = [&](int s) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int row = 64 * wn + 32 * i + l32;
-        fa[i] = *(const V8*)(base + row * (2 * BK) + 16 * C::slot(row, 2 * s + h));
+        fa[s & 1][i] = *(const V8*)(base + row * (2 * BK) + 16 * C::slot(row, 2 * s + h));
       }
 #pragma unroll
       for (int t = 0; t < TB; ++t) {
         const int row = C::TN + 32 * (TB * wm + t) + l32;
-        fb[t] = *(const V8*)(base + row * (2 * BK) + 16 * C::slot(row, 2 * s + h));
+        fb[s & 1][t] = *(const V8*)(base + row * (2 * BK) + 16 * C::slot(row, 2 * s + h));
       }
+    };
+    get(0);
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      if (s + 1 < S) get(s + 1);
 #pragma unroll
       for (int t = 0; t < TB; ++t)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) acc[i][t] = E::mfma(fa[i], fb[t], acc[i][t]);
+        for (int i = 0; i < 2; ++i) acc[i][t] = E::mfma(fa[s & 1][i], fb[s & 1][t], acc[i][t]);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 + TB, 0);
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+#pragma unroll
+      for (int x = 0; x < 2 + TB; ++x) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (s + 1 < S) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, TB - 2, 0);
     }
   };
 
@@ -392,10 +410,10 @@ hipError_t go_rows(const LinearArgs& a, hipStream_t st) {
 //    16 / 32 / 64 tokens, 512 x 256 -> 256 4.0 / 3.1 / 3.8, 1000 x 1024 -> 256 9.5 / 7.9 / 7.3.
 //  - 128 x 64 tiles (features x tokens) until they are about three a CU: 3000 x 1024 ->
 //    2048 22.0, 23.1 in 128 x 128; 6000 x 1024 -> 2048 39.1 and 36.7.
-//  - 256 x 256 from 200 of them on, where L2 traffic is what counts (8192 x 4096 -> 4096 251,
-//    288 in 256 x 128, 364 in 128 x 128), unless K is short: two workgroups of 256 x 128 a CU
+//  - 256 x 256 from 200 of them on, where L2 traffic is what counts (8192 x 4096 -> 4096 231,
+//    295 in 256 x 128, 354 in 128 x 128), unless K is short: two workgroups of 256 x 128 a CU
 //    then hide one's epilogue behind the other's products (32640 x 512 -> 2048 with GELU,
-//    fp16: 123, 139 in 256 x 256).
+//    fp16: 121 to 127, 133 to 139 in 256 x 256).
 // Rows that are not 16-byte aligned go through registers; tiles of two sizes.
 template <class E, bool GATED>
 hipError_t pick(const LinearArgs& a, hipStream_t st) {
