@@ -372,11 +372,7 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
     stage_rows<E, VP, NV, DMA>(lds + C::VOFF, vp - pad * vs, vs, pad, V, wave, lane);
     vp += kChunk * vs;
   };
-  if (nch) {
-    stage_v(0);
-    stage_kq(0);
-  }
-
+  // The state's loads before the tiles': behind those they would stand in the queue.
   const float log_decay = a.log_decay[hd];
   const float l2 = log2_decay(log_decay);
   floatx16 S[DT];
@@ -401,6 +397,11 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
         S[x][r] = from[min(d, D - 1) * V];
       }
   }
+  if (nch) {
+    stage_v(0);
+    stage_kq(0);
+  }
+
   float* sout = !OUT ? (float*)a.ws + (bh * sa.nseg + seg + 1) * sdv
                 : a.state_out && t0 + SL >= len ? a.state_out + bh * sdv : nullptr;
 
