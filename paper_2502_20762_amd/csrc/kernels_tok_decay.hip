@@ -169,30 +169,48 @@ __device__ __forceinline__ void stage_rows(char* lds, const typename E::T* base,
       dma16s(rows, voff + 16 * (u0 ^ unit_slot<W>(R * i, 0)), lds + 1024 * i);
       rows += step;
     }
-  } else {
+  } else if (DMA) {
     int ln = lane;
-    if (DMA) asm volatile("" : "+v"(ln));  // seldom taken: nothing of it is kept in registers from chunk to chunk
+    asm volatile("" : "+v"(ln));  // seldom taken: nothing of it is kept in registers from chunk to chunk
     const int r1 = ln / U, u1 = unit_slot<W>(r1, ln % U);
 #pragma unroll
     for (int i0 = 0; i0 < LOADS / NW; ++i0) {
       const int i = wave + NW * i0, u = u1 ^ unit_slot<W>(R * i, 0);
       const char* p = rows + r1 * stride * 2 + 16 * u;
       const bool in = R * i + r1 >= pad && 8 * u < d;
-      if (DMA) {
-        dma16(in ? (const void*)p : (const void*)decay_zero16, lds + 1024 * i);
-      } else {
-        V8 v = {};
-        if (in) {
-          if (8 * u + 8 <= d)
-            __builtin_memcpy(&v, p, 16);
-          else
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (8 * u + e < d) v[e] = ((const typename E::T*)p)[e];
-        }
-        *(V8*)(lds + 1024 * i + 16 * lane) = v;
-      }
+      dma16(in ? (const void*)p : (const void*)decay_zero16, lds + 1024 * i);
       rows += step;
+    }
+  } else {
+    // through registers: the loads of whole units hang on no condition (what has
+    // none reads zeros), so that four are on their way at a time
+    constexpr int N = LOADS / NW < 4 ? LOADS / NW : 4;
+#pragma unroll
+    for (int j = 0; j < LOADS / NW; j += N) {
+      V8 v[N];
+      const char* p[N];
+      bool in[N];
+#pragma unroll
+      for (int x = 0; x < N; ++x) {
+        const int i = wave + NW * (j + x), u = u0 ^ unit_slot<W>(R * i, 0);
+        p[x] = rows + r0 * stride * 2 + 16 * u;
+        in[x] = R * i + r0 >= pad && 8 * u < d;
+        const void* from = in[x] && 8 * u + 8 <= d ? (const void*)p[x] : (const void*)decay_zero16;
+        __builtin_memcpy(&v[x], from, 16);
+        rows += step;
+      }
+      if (d & 7) {  // the last unit of a row, element by element
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+          const int i = wave + NW * (j + x), u = u0 ^ unit_slot<W>(R * i, 0);
+          if (in[x] && 8 * u + 8 > d)
+#pragma unroll
+            for (int e = 0; e < 7; ++e)
+              if (8 * u + e < d) v[x][e] = ((const typename E::T*)p[x])[e];
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < N; ++x) *(V8*)(lds + 1024 * (wave + NW * (j + x)) + 16 * lane) = v[x];
     }
   }
 }

@@ -408,13 +408,16 @@ hipError_t go_rows(const LinearArgs& a, hipStream_t st) {
 //    (512 x 1024 -> 1024: 11.9 and 11.7; 1000 x 256 -> 1024: 7.9 and 5.9).
 //    Its own token blocks grow with the outputs: 64 x 1024 -> 1024 4.1 / 5.0 / 7.1 with
 //    16 / 32 / 64 tokens, 512 x 256 -> 256 4.0 / 3.1 / 3.8, 1000 x 1024 -> 256 9.5 / 7.9 / 7.3.
-//  - 128 x 64 tiles (features x tokens) until they are about three a CU: 3000 x 1024 ->
-//    2048 22.0, 23.1 in 128 x 128; 6000 x 1024 -> 2048 39.1 and 36.7.
-//  - 256 x 256 from 200 of them on, where L2 traffic is what counts (8192 x 4096 -> 4096 231,
-//    295 in 256 x 128, 354 in 128 x 128), unless K is short: two workgroups of 256 x 128 a CU
-//    then hide one's epilogue behind the other's products (32640 x 512 -> 2048 with GELU,
-//    fp16: 121 to 127, 133 to 139 in 256 x 256).
-// Rows that are not 16-byte aligned go through registers; tiles of two sizes.
+//  - Then the largest tile (features x tokens) that still leaves work for most CUs: 256 x 256
+//    from 150 of them on (14793 x 2048 -> 712 64 us, 69 in 256 x 128, 68 in 128 x 128; with 128 of
+//    them, 8160 x 1024 -> 1024, 31.5 against 24.1), 256 x 128 in stages of 64 from 150 of those (8160
+//    x 2048 -> 1024 41.5, 50 in 128 x 128; with 128 of them, 8160 x 2048 -> 512, 33 against 28),
+//    128 x 64 up to three a CU (3000 x 1024 -> 1024 15.0, 18 in 128 x 128), else 128 x 128.
+//  - Short contractions, K < 512, are mostly epilogue and stay with the small tiles (6000 x
+//    256 -> 1024 9.9 in 128 x 64, 11.4 in 256 x 128), and up to K = 512 a large product takes
+//    256 x 128 in stages of 32: two workgroups a CU, one's epilogue behind the other's
+//    products (32640 x 512 -> 2048 with GELU, fp16: 121 to 127, 133 to 139 in 256 x 256).
+// Rows that are not 16-byte aligned go through registers; tiles of three sizes.
 template <class E, bool GATED>
 hipError_t pick(const LinearArgs& a, hipStream_t st) {
   const ncodec_linear_shape& s = a.s;
@@ -426,12 +429,15 @@ hipError_t pick(const LinearArgs& a, hipStream_t st) {
   }
   const auto tiles = [&](int64_t f, int64_t tok) { return ((s.m + tok - 1) / tok) * ((nf + f - 1) / f); };
   const bool dma = s.k % 8 == 0 && s.ldx % 8 == 0 && s.ldw % 8 == 0 && (uintptr_t)a.x % 16 == 0 && (uintptr_t)a.w % 16 == 0;
-  const bool large = tiles(256, 256) >= 200;
-  if (!dma) return large ? go_tile<E, GATED, false, 4, 2, 4, 32, 2>(a, st) : go_tile<E, GATED, false, 2, 2, 2, 32, 2>(a, st);
-  if (tiles(128, 64) <= 768) return go_tile<E, GATED, true, 2, 2, 1, 64, 2>(a, st);
-  if (!large) return go_tile<E, GATED, true, 2, 2, 2, 32, 3>(a, st);
-  if (s.k >= 1024) return go_tile<E, GATED, true, 4, 2, 4, 64, 2>(a, st);
-  return go_tile<E, GATED, true, 4, 2, 2, 32, 3>(a, st);
+  const bool small = tiles(128, 64) <= 768;
+  if (!dma) {
+    if (tiles(256, 256) >= 150) return go_tile<E, GATED, false, 4, 2, 4, 32, 2>(a, st);
+    return small ? go_tile<E, GATED, false, 2, 2, 1, 32, 2>(a, st) : go_tile<E, GATED, false, 2, 2, 2, 32, 2>(a, st);
+  }
+  if (s.k <= 512 && tiles(256, 256) >= 512) return go_tile<E, GATED, true, 4, 2, 2, 32, 3>(a, st);
+  if (s.k >= 512 && tiles(256, 256) >= 150) return go_tile<E, GATED, true, 4, 2, 4, 64, 2>(a, st);
+  if (s.k >= 512 && tiles(256, 128) >= 150) return go_tile<E, GATED, true, 4, 2, 2, 64, 2>(a, st);
+  return small ? go_tile<E, GATED, true, 2, 2, 1, 64, 2>(a, st) : go_tile<E, GATED, true, 2, 2, 2, 32, 3>(a, st);
 }
 
 }  // namespace
