@@ -203,10 +203,17 @@ __device__ __forceinline__ void stage_rows(char* lds, const typename E::T* base,
 #pragma unroll
         for (int x = 0; x < N; ++x) {
           const int i = wave + NW * (j + x), u = u0 ^ unit_slot<W>(R * i, 0);
-          if (in[x] && 8 * u + 8 > d)
+          const bool part = in[x] && 8 * u + 8 > d;
+          const uint16_t* from = (const uint16_t*)(part ? (const void*)p[x] : (const void*)decay_zero16);
+          const int top = part ? d - 8 * u - 1 : 0;
+          uint32_t el[7];
 #pragma unroll
-            for (int e = 0; e < 7; ++e)
-              if (8 * u + e < d) v[x][e] = ((const typename E::T*)p[x])[e];
+          for (int e = 0; e < 7; ++e) el[e] = from[min(e, top)];
+#pragma unroll
+          for (int e = 0; e < 7; ++e) {
+            asm volatile("" : "+v"(el[e]));  // or the load would move behind the condition
+            if (part && e <= top) v[x][e] = __builtin_bit_cast(typename E::T, (uint16_t)el[e]);
+          }
         }
       }
 #pragma unroll
