@@ -784,8 +784,11 @@ __global__ __launch_bounds__(512) void k_tok_decay_scan(SegArgs sa) {
   }
 }
 
-// Sequences shorter than this run the recurrence (few workgroups, no chunk to fill).
-constexpr int64_t kRecurTokens = 8;
+// Sequences shorter than this run the recurrence, which takes a step of 1 to 2 us for
+// every token where a chunk takes the same time for 1 and 64.  us there / in a chunk: 4
+// tokens 7.4 / 8.4 with 8 heads of 64 x 64, 8.5 / 10.0 with 8 of 128 x 128, 15.6 / 17.0 with
+// 512 of these; 6 tokens 9.5 / 8.4, 11.1 / 10.1, 19.4 / 17.1.
+constexpr int64_t kRecurTokens = 6;
 
 struct Plan {
   bool chunked;
