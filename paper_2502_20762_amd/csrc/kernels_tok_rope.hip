@@ -1,6 +1,9 @@
 // RMS norm of every query and key head and the rotation by the token's
 // position, in one pass over q and k: each element is read once and written
-// once, so the bytes are the bound.
+// once, so the bytes are the bound: 130,560 tokens of 10 + 10 heads of 128, 1.34 GB, take
+// 226 us (5.9 TB/s; a large copy reaches 5.0 and one inside the last-level cache 6.6),
+// 8,160 tokens of 8 + 8 heads of 64, 33 MB, 7.6 us (4.4 TB/s).  A few tokens take the 2.5 to
+// 3 us of a launch.
 #include <algorithm>
 
 #include "tokens.hpp"
@@ -8,7 +11,7 @@
 namespace nc {
 namespace {
 
-constexpr int kMaxPairs = 128, kMaxTokens = 8;  // of a workgroup's table
+constexpr int kTable = 1024;  // pairs of a workgroup's tokens: 8 tokens of the largest head
 
 // cos and sin of pos * freq radians.  The angle is counted in turns in 64
 // bits, where a 31-bit position times a 24-bit frequency is exact up to the
@@ -56,7 +59,7 @@ template <class E, int VEC, int UPL>
 __global__ __launch_bounds__(256) void k_tok_rope(RopeArgs ra) {
   typedef typename E::T T;
   typedef T TV __attribute__((ext_vector_type(VEC)));
-  __shared__ __align__(16) float2 cs[kMaxTokens * kMaxPairs];
+  __shared__ __align__(16) float2 cs[kTable];
   const ncodec_qk_shape& s = ra.a.s;
   const int P = s.section[0] + s.section[1] + s.section[2], D = s.head_dim, H = s.q_heads + s.k_heads;
   const int64_t tk0 = (int64_t)blockIdx.x * ra.tokens;
@@ -171,15 +174,22 @@ hipError_t go(const QkArgs& a, int units, hipStream_t st) {
   RopeArgs ra{a, 1, 0, 0};
   while (ra.log2g < 6 && (1 << ra.log2g) * UPL < units) ++ra.log2g;
   const int64_t H = s.q_heads + s.k_heads;
-  // tokens of a workgroup: up to eight, as long as that leaves eight workgroups a CU
-  ra.tokens = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxTokens, s.tokens / 2048));
+  // Tokens of a workgroup: 16 KiB of values (two rounds of its lanes), so that the sines
+  // and the start are spread over enough of them (130,560 tokens, 8 + 8 heads of 64: 8 tokens
+  // 95 us, one 179; 1 + 1 heads: 32 tokens 17 us, 8 tokens 24) and one round's loads run
+  // beside the other's stores (16 + 16 heads of 128: 2 tokens 354 us, 1 or 8 390 to 399), and
+  // no more than leaves three workgroups a CU (2,048 tokens of 8 + 8 heads of 64: 2 tokens 3.9
+  // us, one 4.7, eight 4.4; 256 tokens 2.9 with one, 3.9 with eight).
+  const int64_t bytes = 2 * H * s.head_dim, pairs = std::max(1, s.section[0] + s.section[1] + s.section[2]);
+  ra.tokens = (int)std::max<int64_t>(1, std::min({kTable / pairs, 16384 / bytes, s.tokens / 768}));
   ra.magic = (uint32_t)((((uint64_t)1 << 32) + H - 1) / H);
   launch(k_tok_rope<E, VEC, UPL>, dim3((unsigned)((s.tokens + ra.tokens - 1) / ra.tokens)), dim3(256), st, ra);
   return hipGetLastError();
 }
 
 // Runs of eight or four elements where head_dim and the pairs are made of them
-// (16- and 8-byte accesses), single elements otherwise.
+// (16- and 8-byte accesses), single elements otherwise: 130,560 tokens of 16 + 16 heads of
+// 128 take 356, 403 and 656 us so.
 template <class E>
 hipError_t pick(const QkArgs& a, hipStream_t st) {
   const int P = a.s.section[0] + a.s.section[1] + a.s.section[2], D = a.s.head_dim;
