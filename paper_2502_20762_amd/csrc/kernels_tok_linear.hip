@@ -4,6 +4,8 @@
 // the MFMA A operand, the tokens are the columns, and a lane of the
 // accumulator holds one token and four consecutive features at a time.
 // Operands are read as they lie in memory: nothing is packed beforehand.
+#include <algorithm>
+
 #include "tokens.hpp"
 
 namespace nc {
@@ -390,7 +392,6 @@ hipError_t go_tile(const LinearArgs& a, hipStream_t st) {
   typedef Tile<E, GATED, DMA, WN, WM, TB, BK, ST_> C;
   int64_t grid = ((a.s.m + C::TM - 1) / C::TM) * ((a.s.n + C::OF * WN - 1) / (C::OF * WN));
   grid = (grid + kNumXCD - 1) / kNumXCD * kNumXCD;
-  if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
   launch(k_tok_linear<E, GATED, DMA, WN, WM, TB, BK, ST_>, dim3((unsigned)grid), dim3(64 * C::NW), st, a);
   return hipGetLastError();
 }
@@ -443,9 +444,21 @@ hipError_t pick(const LinearArgs& a, hipStream_t st) {
 
 }  // namespace
 
+// A launch counts its threads in 32 bits: rows past 2^22 of the smallest tiles go in further launches.
 hipError_t launch_linear(const LinearArgs& a, hipStream_t st) {
-  if (a.s.dtype == NCODEC_DTYPE_FP16) return a.s.gated ? pick<F16, true>(a, st) : pick<F16, false>(a, st);
-  return a.s.gated ? pick<BF16, true>(a, st) : pick<BF16, false>(a, st);
+  const int64_t nf = a.s.n * (a.s.gated ? 2 : 1), rows = (((int64_t)1 << 22) / ((nf + 127) / 128)) * 64;
+  for (int64_t m0 = 0; m0 < a.s.m; m0 += rows) {
+    LinearArgs p = a;
+    p.s.m = std::min(rows, a.s.m - m0);
+    p.x = (const char*)a.x + 2 * m0 * a.s.ldx;
+    p.y = (char*)a.y + 2 * m0 * a.s.ldy;
+    if (a.r) p.r = (const char*)a.r + 2 * m0 * a.s.ldr;
+    const hipError_t e = a.s.dtype == NCODEC_DTYPE_FP16
+                             ? (a.s.gated ? pick<F16, true>(p, st) : pick<F16, false>(p, st))
+                             : (a.s.gated ? pick<BF16, true>(p, st) : pick<BF16, false>(p, st));
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace nc

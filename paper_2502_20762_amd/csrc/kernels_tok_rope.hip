@@ -183,8 +183,20 @@ hipError_t go(const QkArgs& a, int units, hipStream_t st) {
   const int64_t bytes = 2 * H * s.head_dim, pairs = std::max(1, s.section[0] + s.section[1] + s.section[2]);
   ra.tokens = (int)std::max<int64_t>(1, std::min({kTable / pairs, 16384 / bytes, s.tokens / 768}));
   ra.magic = (uint32_t)((((uint64_t)1 << 32) + H - 1) / H);
-  launch(k_tok_rope<E, VEC, UPL>, dim3((unsigned)((s.tokens + ra.tokens - 1) / ra.tokens)), dim3(256), st, ra);
-  return hipGetLastError();
+  // a launch counts its threads in 32 bits: tokens past 2^22 workgroups go in further ones
+  const int64_t most = ((int64_t)1 << 22) * ra.tokens;
+  for (int64_t t0 = 0; t0 < s.tokens; t0 += most) {
+    ra.a.s.tokens = std::min(most, s.tokens - t0);
+    ra.a.q = (const char*)a.q + 2 * t0 * s.q_token_stride;
+    ra.a.k = (const char*)a.k + 2 * t0 * s.k_token_stride;
+    ra.a.qo = (char*)a.qo + 2 * t0 * s.qo_token_stride;
+    ra.a.ko = (char*)a.ko + 2 * t0 * s.ko_token_stride;
+    if (a.pos) ra.a.pos = a.pos + t0 * s.axes;
+    launch(k_tok_rope<E, VEC, UPL>, dim3((unsigned)((ra.a.s.tokens + ra.tokens - 1) / ra.tokens)), dim3(256), st, ra);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // Runs of eight or four elements where head_dim and the pairs are made of them

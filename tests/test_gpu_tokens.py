@@ -169,6 +169,16 @@ def test_linear_rows_past_32_bit_offsets():
     assert torch.equal(tk.linear(x.contiguous(), w, out=y), tk.linear(x.contiguous(), w))
 
 
+def test_linear_more_rows_than_a_launch_takes():
+    m = (1 << 28) + 1000  # one product an output: the rounding of an exact fp32 value
+    x = torch.arange(m, device=DEV, dtype=torch.int32).remainder_(1999).to(torch.float16).view(m, 1)
+    w = torch.tensor([[0.375]], dtype=torch.float16, device=DEV)
+    y = tk.linear(x, w, residual=x)
+    for lo in range(0, m, 1 << 26):  # 1.375 x is 11 x / 8: fp32 holds it, fp16 rounds it once
+        part = x[lo:lo + (1 << 26)].float()
+        assert torch.equal(y[lo:lo + (1 << 26)], (part * 0.375 + part).half()), lo
+
+
 def test_linear_is_repeatable_and_takes_the_current_stream():
     g = gen(7)
     x, w = rnd(g, (900, 512), "bf16").to(DEV), rnd(g, (300, 512), "bf16").to(DEV)
@@ -514,6 +524,21 @@ def test_decay_offsets_past_32_bits():
     a = tk.decay_attention(q, k, v, lam, return_state=True)
     b = tk.decay_attention(q.contiguous(), k.contiguous(), v.contiguous(), lam, return_state=True)
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_rope_more_tokens_than_a_launch_takes():
+    T, last = (1 << 25) + 777, 2000  # eight tokens of 256 a workgroup, 17 GB
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    q = torch.ones((T, 1, 256), dtype=torch.float16, device=DEV)
+    rows = rnd(gen(44), (last, 1, 256), "fp16").to(DEV)
+    q[-last:] = rows
+    pos = torch.arange(T, dtype=torch.int32, device=DEV).view(T, 1)
+    freq = tk.rope_frequencies((128,), device=DEV)
+    none = q[:, :0]
+    tk.qk_norm_rope(q, none, None, None, pos, freq, (128,), q_out=q, k_out=none)
+    want, _ = tk.qk_norm_rope(rows, rows[:, :0], None, None, pos[-last:].contiguous(), freq, (128,))
+    assert torch.equal(q[-last:], want)
 
 
 # ---------------------------------------------------------------- streams, graphs, refusals
