@@ -313,9 +313,31 @@ __device__ __forceinline__ float max_finite(float m, const floatx16& v) {
   return m;
 }
 
-// Units.  What becomes an fp16 operand (scores, the state, weighted values) is
-// held in a power-of-two unit of its own, so that neither large nor small
-// magnitudes leave the range in which fp16 has its 11 bits.  A unit stays
+// Operands.  Scores, the state and weighted values are fp32; MFMA operands have 16
+// bits.  They go in as sums of 16-bit terms, each the rest of the one before: two
+// hold 22 bits in fp16 and 16 in bf16, where an output keeps 11 and 8, so that the
+// outputs' own rounding is the only one that counts (with one term, as many bits as
+// the output, the error of the outputs was 1.4 times that of their rounding).
+template <class T>
+__device__ __forceinline__ void two_terms(float x, T& hi, T& lo) {
+  hi = (T)x;
+  lo = (T)(x - (float)hi);
+}
+
+// Units.  What becomes an fp16 operand is held in a power-of-two unit, so that
+// neither large nor small magnitudes leave the range in which its terms have
+// their bits.
+// The unit in which m >= 0 is in [2^14, 2^15), and its inverse; m below 2^-112, zero
+// too, counts as 2^-112.
+struct Fresh {
+  float u, inv;
+};
+__device__ __forceinline__ Fresh fresh_unit(float m) {
+  const uint32_t e = max(__float_as_uint(m) >> 23, 15u);  // m >= 0: 15 .. 255
+  return {__uint_as_float((268u - e) << 23), __uint_as_float((e - 14u) << 23)};
+}
+
+// A unit that lasts: of the state and of the weighted values.  It stays
 // while the wave's largest magnitude lies in [lo, hi); else it moves to where that
 // is 2^11 (nothing else in the kernel depends on it).
 struct Unit {
@@ -440,30 +462,29 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
   float* sout = !OUT ? (float*)a.ws + (bh * sa.nseg + seg + 1) * sdv
                 : a.state_out && t0 + SL >= len ? a.state_out + bh * sdv : nullptr;
 
-  // Of the state, the scores and the weighted values (fp16 only; first such that
-  // values of about one do not move them).
-  Unit us = {F ? 0x1p5f : 1.f, F ? 0x1p-5f : 1.f}, up = {F ? 0x1p6f : 1.f, F ? 0x1p-6f : 1.f},
-       uv = {F ? 0x1p9f : 1.f, F ? 0x1p-9f : 1.f};
+  // Of the state and the weighted values (fp16 only; first such that values of about
+  // one do not move them).
+  Unit us = {F ? 0x1p5f : 1.f, F ? 0x1p-5f : 1.f}, uv = {F ? 0x1p9f : 1.f, F ? 0x1p-9f : 1.f};
   // Decays.  Inside a diagonal 32 x 32 tile lambda^(i - j) for j <= i (i this lane's
-  // token, j the register's), one tile below it lambda^(32 + i - j), both in the
-  // scores' unit.  At the end of a chunk token 16 x + j counts lambda^(15 - j)
-  // lambda^(48 - 16 x), in the unit of the weighted values.
-  float mdiag[OUT ? 16 : 1], mlow[OUT ? 16 : 1], wage[8], wstep[4];
+  // token, j the register's).  At the end of a chunk token 16 x + j counts
+  // lambda^(15 - j) lambda^(48 - 16 x).  One tile below the diagonal lambda^(32 + i - j)
+  // is lambda^(i + 1) lambda^(31 - j), whose second factor is that age again.
+  float mdiag[OUT ? 16 : 1], wage[8], wstep[4];
   uint32_t below = 0;  // bit r: j <= i
   if (OUT) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int lag = l32 - drow(r, h);
       below |= lag >= 0 ? 1u << r : 0u;
-      mdiag[r] = __builtin_amdgcn_exp2f(max(lag, 0) * l2) * up.u;
-      mlow[r] = __builtin_amdgcn_exp2f((32 + lag) * l2) * up.u;
+      mdiag[r] = __builtin_amdgcn_exp2f(max(lag, 0) * l2);
     }
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) wage[e] = __builtin_amdgcn_exp2f((15 - (8 * (e >> 2) + 4 * h + (e & 3))) * l2) * uv.u;
+  for (int e = 0; e < 8; ++e) wage[e] = __builtin_amdgcn_exp2f((15 - (8 * (e >> 2) + 4 * h + (e & 3))) * l2);
 #pragma unroll
   for (int x = 0; x < 4; ++x) wstep[x] = __builtin_amdgcn_exp2f((48 - 16 * x) * l2);
-  const float di0 = __builtin_amdgcn_exp2f((l32 + 1) * l2), d32 = __builtin_amdgcn_exp2f(32 * l2);
+  const float di0 = __builtin_amdgcn_exp2f((l32 + 1) * l2), di16 = __builtin_amdgcn_exp2f((l32 + 17) * l2),
+              d32 = __builtin_amdgcn_exp2f(32 * l2);
   Decay64 keep = decay_pow(log_decay, kChunk), keep_last = keep;
   if (last_pad) keep_last = decay_pow(log_decay, kChunk - last_pad);
   T* op = o + (t0 + l32) * s.o_token_stride + 32 * wave + 8 * h;  // this lane's first output row
@@ -539,11 +560,7 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
     if (F) {
       const float m = (float)__builtin_bit_cast(f16, (uint16_t)mb) * uv.u;
-      if (Unit::leaves(m)) {
-        const float f = uv.move(m);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) wage[e] *= f;
-      }
+      if (Unit::leaves(m)) uv.move(m);
     }
 
     if (OUT) {
@@ -564,67 +581,62 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
             for (int r = 0; r < 16; ++r) S[x][r] *= f;
         }
       }
-      // scores of a 32 x 32 tile as an operand: p holds k_j . q_i
-      auto scores = [&](floatx16& p, bool diag, V8(&pf)[2]) {
-        if (diag) {  // pairs above the diagonal count nothing, whatever their product is
+      // Products of the 64 queries with the state, and the scores: keys against queries
+      // in the tiles (0, 0), (0, 1) and (1, 1), p holds k_j . q_i.
+      floatx16 inter2[2] = {}, p[3] = {};
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            p[r] = __int_as_float(__float_as_int(p[r]) & ((int)(below << (31 - r)) >> 31));
+      for (int x = 0; x < 2 * DT; ++x) {
+        const char* r = lds + ((ro + buf) ^ (32 * x));
+        const V8 k0 = *(const V8*)r, k1 = *(const V8*)(r + 64 * DP);
+        const V8 q0 = *(const V8*)(r + C::KB), q1 = *(const V8*)(r + (C::KB + 64 * DP));
+        p[0] = E::mfma(k0, q0, p[0]);
+        p[1] = E::mfma(k0, q1, p[1]);
+        p[2] = E::mfma(k1, q1, p[2]);
+        V8 sh, sl;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          T hi, lo;
+          two_terms(S[x >> 1][8 * (x & 1) + e], hi, lo);
+          sh[e] = hi;
+          sl[e] = lo;
         }
-        if (F) {
-          float m = max_abs(p) * up.u;
-          if (Unit::leaves(m)) {
-            if (__any(m == __builtin_huge_valf())) m = max_finite(0.f, p) * up.u;
-            const float f = up.move(m);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              mdiag[r] *= f;
-              mlow[r] *= f;
-            }
-          }
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) pf[r >> 3][r & 7] = (T)(p[r] * (diag ? mdiag[r] : mlow[r]));
-      };
+        inter2[0] = E::mfma(sh, q0, inter2[0]);
+        inter2[1] = E::mfma(sh, q1, inter2[1]);
+        inter2[0] = E::mfma(sl, q0, inter2[0]);
+        inter2[1] = E::mfma(sl, q1, inter2[1]);
+      }
 #pragma unroll
       for (int it = 0; it < 2; ++it) {  // 32 queries
-        floatx16 inter = {}, intra = {};
-        const int rb = ro + buf;
-        if (it) {  // the keys before them
-          floatx16 p = {};
+        floatx16 &inter = inter2[it], intra = {}, &diag = p[2 * it], &below0 = p[1];
+        // weighted scores: pairs above the diagonal count nothing, whatever their product is
 #pragma unroll
-          for (int x = 0; x < 2 * DT; ++x) {
-            const char* r = lds + (rb ^ (32 * x));
-            p = E::mfma(*(const V8*)r, *(const V8*)(r + (C::KB + 64 * DP)), p);
-          }
-          V8 pf[2];
-          scores(p, false, pf);
-          intra = E::mfma(vf[0], pf[0], intra);
-          intra = E::mfma(vf[1], pf[1], intra);
+        for (int r = 0; r < 16; ++r) {
+          diag[r] = __int_as_float(__float_as_int(diag[r]) & ((int)(below << (31 - r)) >> 31)) * mdiag[r];
+          if (it) below0[r] *= wage[r & 7] * (r < 8 ? di16 : di0);
         }
-        const float was = up.inv;
-        {
-          floatx16 p = {};
-#pragma unroll
-          for (int x = 0; x < 2 * DT; ++x) {
-            const char* r = lds + (rb ^ (32 * x)) + 64 * DP * it;
-            const V8 qf = *(const V8*)(r + C::KB);
-            p = E::mfma(*(const V8*)r, qf, p);
-            V8 sf;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sf[e] = (T)S[x >> 1][8 * (x & 1) + e];
-            inter = E::mfma(sf, qf, inter);
-          }
-          V8 pf[2];
-          scores(p, true, pf);
-          if (F && it && was != up.inv) {  // the unit moved between the two tiles
-            const float f = was * up.u;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) intra[r] *= f;
-          }
-          intra = E::mfma(vf[2 * it], pf[0], intra);
-          intra = E::mfma(vf[2 * it + 1], pf[1], intra);
+        Fresh up = {1.f, 1.f};  // of this lane's query
+        if (F) {
+          float m = max_abs(diag);
+          if (it) m = fmaxf(m, max_abs(below0));
+          const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+          up = fresh_unit(__uint_as_float(max(both[0], both[1])));
         }
+        const auto add_values = [&](const floatx16& w, int x) {  // values 16 x .. 16 x + 31
+          V8 wh[2], wl[2];
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            T hi, lo;
+            two_terms(F ? w[r] * up.u : w[r], hi, lo);
+            wh[r >> 3][r & 7] = hi;
+            wl[r >> 3][r & 7] = lo;
+          }
+          intra = E::mfma(vf[x], wl[0], intra);
+          intra = E::mfma(vf[x + 1], wl[1], intra);
+          intra = E::mfma(vf[x], wh[0], intra);
+          intra = E::mfma(vf[x + 1], wh[1], intra);
+        };
+        if (it) add_values(below0, 0);
+        add_values(diag, 2 * it);
         // row i is token i - pad of the chunk; rows of the padding are not stored
         float di = it ? di0 * d32 : di0;
         if (pad) di = __builtin_amdgcn_exp2f(max(32 * it + l32 + 1 - pad, 0) * l2);
@@ -680,7 +692,7 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
       for (int x = 0; x < 4; ++x)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          float w = (float)vf[x][e] * (wage[e] * wstep[x]);
+          float w = (float)vf[x][e] * (wage[e] * (wstep[x] * uv.u));
           // one value of the product for all terms: formed anew for a term (fused,
           // rounded once instead of twice) it could differ from the one subtracted
           asm("" : "+v"(w));
