@@ -270,7 +270,12 @@ __device__ __forceinline__ typename E::V8 read_cols(const char* p0, const char* 
   return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// max over all lanes of a value >= 0 that is no NaN (its bits order it)
+// max over a lane and the other of its column, l ^ 32, of a value >= 0 that is no NaN (its bits order it)
+__device__ __forceinline__ float half_max(float f) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(f), __float_as_uint(f), false, false);
+  return __uint_as_float(max(a[0], a[1]));
+}
+// max over all lanes
 __device__ __forceinline__ float wave_max(float f) {
   uint32_t v = __float_as_uint(f);
   const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
@@ -337,7 +342,7 @@ __device__ __forceinline__ Fresh fresh_unit(float m) {
   return {__uint_as_float((268u - e) << 23), __uint_as_float((e - 14u) << 23)};
 }
 
-// A unit that lasts: of the state and of the weighted values.  It stays
+// A unit that lasts, of the state.  It stays
 // while the wave's largest magnitude lies in [lo, hi); else it moves to where that
 // is 2^11 (nothing else in the kernel depends on it).
 struct Unit {
@@ -462,9 +467,7 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
   float* sout = !OUT ? (float*)a.ws + (bh * sa.nseg + seg + 1) * sdv
                 : a.state_out && t0 + SL >= len ? a.state_out + bh * sdv : nullptr;
 
-  // Of the state and the weighted values (fp16 only; first such that values of about
-  // one do not move them).
-  Unit us = {F ? 0x1p5f : 1.f, F ? 0x1p-5f : 1.f}, uv = {F ? 0x1p9f : 1.f, F ? 0x1p-9f : 1.f};
+  Unit us = {F ? 0x1p5f : 1.f, F ? 0x1p-5f : 1.f};  // fp16 only; first such that values of about one do not move it
   // Decays.  Inside a diagonal 32 x 32 tile lambda^(i - j) for j <= i (i this lane's
   // token, j the register's).  At the end of a chunk token 16 x + j counts
   // lambda^(15 - j) lambda^(48 - 16 x).  One tile below the diagonal lambda^(32 + i - j)
@@ -536,12 +539,10 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
     if (c + 1 < nch) stage_v(c + 1);
 
     int bad = kChunk;  // first row of this lane's column that is not finite
-    uint32_t mb = max_bits(vf);  // magnitudes by their bits, which order finite values, infinities and NaN
-    const bool any_bad = __any(mb >= C::INF);
+    const bool any_bad = __any(max_bits(vf) >= C::INF);  // bits order finite values, infinities and NaN
     if (any_bad) {
       // a product would carry it to earlier tokens too (0 times NaN): it is taken
       // out here and put into the outputs and the state that it reaches
-      mb = 0;
       int h4 = 4 * h;
       asm volatile("" : "+v"(h4));  // nothing of this rare path is computed, and kept, before the loop
 #pragma unroll
@@ -552,15 +553,9 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
           if (u >= C::INF) {
             bad = min(bad, 16 * x + 8 * (e >> 2) + h4 + (e & 3));
             vf[x][e] = (T)0.f;
-          } else {
-            mb = max(mb, u);
           }
         }
       bad = min(bad, __shfl_xor(bad, 32, 64));
-    }
-    if (F) {
-      const float m = (float)__builtin_bit_cast(f16, (uint16_t)mb) * uv.u;
-      if (Unit::leaves(m)) uv.move(m);
     }
 
     if (OUT) {
@@ -618,8 +613,7 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
         if (F) {
           float m = max_abs(diag);
           if (it) m = fmaxf(m, max_abs(below0));
-          const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
-          up = fresh_unit(__uint_as_float(max(both[0], both[1])));
+          up = fresh_unit(half_max(m));
         }
         const auto add_values = [&](const floatx16& w, int x) {  // values 16 x .. 16 x + 31
           V8 wh[2], wl[2];
@@ -686,20 +680,46 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
     if (!OUT || c + 1 < nch || sout) {
       // the state: v weighted by its age, as a sum of 16-bit terms that holds 22 (fp16)
-      // or 24 (bf16) bits, because the state is an fp32 output
+      // or 24 (bf16) bits, because the state is an fp32 output.  fp16 terms are in a unit
+      // of this lane's column, from its largest weighted value: a quiet column keeps its
+      // bits beside a loud one, and a late value behind a loud one that has decayed.
+      float w[4][8];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        float ws = wstep[x];
+        asm volatile("" : "+v"(ws));  // or the 32 weights would be formed, and kept, before the loop
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[x][e] = fmaf((float)vf[x][e], wage[e] * ws, 0.f);
+      }
+      Fresh uv = {1.f, 1.f};
+      if (F) {
+        float m[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          m[x] = max3_abs(fabsf(w[x][0]), w[x][1], w[x][2]);
+          m[x] = max3_abs(max3_abs(m[x], w[x][3], w[x][4]), w[x][5], w[x][6]);
+        }
+        m[0] = max3_abs(max3_abs(m[0], w[0][7], w[1][7]), w[2][7], w[3][7]);
+        m[0] = fmaxf(max3_abs(m[0], m[1], m[2]), m[3]);
+        uv = fresh_unit(half_max(m[0]));
+      }
       V8 term[4][NT];
 #pragma unroll
       for (int x = 0; x < 4; ++x)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          float w = (float)vf[x][e] * (wage[e] * (wstep[x] * uv.u));
-          // one value of the product for all terms: formed anew for a term (fused,
-          // rounded once instead of twice) it could differ from the one subtracted
-          asm("" : "+v"(w));
+          float t = w[x][e];
+          if (F) {  // the unit is a power of two: the product is as exact formed twice
+            T hi, lo;
+            two_terms(t * uv.u, hi, lo);
+            term[x][0][e] = hi;
+            term[x][1][e] = lo;
+          } else {
 #pragma unroll
-          for (int y = 0; y < NT; ++y) {
-            term[x][y][e] = (T)w;
-            w -= (float)term[x][y][e];
+            for (int y = 0; y < NT; ++y) {
+              term[x][y][e] = (T)t;
+              t -= (float)term[x][y][e];
+            }
           }
         }
       const float gain = uv.inv * us.u;

@@ -67,3 +67,37 @@ def test_quiet_keys_after_loud_ones_that_have_decayed(loud, dt):
     k *= 2.0 ** -9
     k[:, loud - 10:loud] *= 2.0 ** 18
     attend(*(x.to(DT[dt]) for x in (q, k, v)), (-2.0, -2.5), None, 1.0, dt, (loud, dt))
+
+
+def state_check(S, wS, mS, T, what):
+    # terms to 2^-22 of a weighted value, their weights to a few 2^-24, fp32 sums
+    check(S, wS, ((T + 16) * F32 + 2.0 ** -21) * mS + 1e-37, (what, "state"))
+
+
+@pytest.mark.parametrize("T", [3, 64, 150, 700])
+@pytest.mark.parametrize("quiet", [2.0 ** -12, 2.0 ** -16, 2.0 ** -20])
+def test_quiet_columns_keep_the_bits_of_the_state(quiet, T):
+    # columns of very different magnitude in one head: each as exact as if it were alone
+    say("decay, quiet columns", quiet, T)
+    g = gen(4)
+    q, k, v = (torch.randn((1, T, 2, 64), generator=g) for _ in range(3))
+    v[..., 1::2] *= quiet
+    v *= 2.0 ** 6
+    o, S, want, wS, mag, mS = attend(*(x.half() for x in (q, k, v)), (-0.02, -0.3), None, 1.0, "fp16", (quiet, T))
+    state_check(S, wS, mS, T, (quiet, T))
+
+
+@pytest.mark.parametrize("loud", [5, 40, 100])
+def test_quiet_values_after_loud_ones_that_have_decayed_keep_the_bits_of_the_state(loud):
+    say("decay, quiet values", loud)
+    g = gen(5)
+    q, k, v = (torch.randn((1, 128, 2, 64), generator=g) for _ in range(3))
+    v *= 2.0 ** -9
+    v[:, loud - 5:loud] *= 2.0 ** 20
+    q, k, v = (x.half() for x in (q, k, v))
+    ld = torch.tensor([-2.0, -1.5])
+    # the state alone: the loud tokens' own outputs are beyond fp16
+    _, S = tk.decay_attention(*(x.to(DEV) for x in (q, k, v)), ld.to(DEV), return_state=True)
+    _, wS = ref.decay_attention(f64(q), f64(k), f64(v), f64(ld))
+    _, mS = ref.decay_attention(f64(q), np.abs(f64(k)), np.abs(f64(v)), f64(ld))
+    state_check(S, wS, mS, 128, loud)
