@@ -323,10 +323,19 @@ __device__ __forceinline__ float max_finite(float m, const floatx16& v) {
 // hold 22 bits in fp16 and 16 in bf16, where an output keeps 11 and 8, so that the
 // outputs' own rounding is the only one that counts (with one term, as many bits as
 // the output, the error of the outputs was 1.4 times that of their rounding).
-template <class T>
-__device__ __forceinline__ void two_terms(float x, T& hi, T& lo) {
-  hi = (T)x;
-  lo = (T)(x - (float)hi);
+template <class E>
+__device__ __forceinline__ void two_terms(const float (&x)[8], float u, typename E::V8& hi, typename E::V8& lo) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const float a = x[i] * u, b = x[i + 1] * u;  // u a power of two: exact, however often it is formed
+    typename E::V2 h = {(typename E::T)a, (typename E::T)b};
+    asm("" : "+v"(h));  // or each half would be formed anew for its rest
+    const typename E::V2 l = {(typename E::T)(a - (float)h.x), (typename E::T)(b - (float)h.y)};
+    hi[i] = h.x;
+    hi[i + 1] = h.y;
+    lo[i] = l.x;
+    lo[i + 1] = l.y;
+  }
 }
 
 // Units.  What becomes an fp16 operand is held in a power-of-two unit, so that
@@ -341,28 +350,6 @@ __device__ __forceinline__ Fresh fresh_unit(float m) {
   const uint32_t e = max(__float_as_uint(m) >> 23, 15u);  // m >= 0: 15 .. 255
   return {__uint_as_float((268u - e) << 23), __uint_as_float((e - 14u) << 23)};
 }
-
-// A unit that lasts, of the state.  It stays
-// while the wave's largest magnitude lies in [lo, hi); else it moves to where that
-// is 2^11 (nothing else in the kernel depends on it).
-struct Unit {
-  float u, inv;
-  static constexpr float kHi = 0x1p15f, kLo = 0x1p5f;
-  // m: this lane's largest magnitude, times u
-  __device__ __forceinline__ static bool leaves(float m) { return __any(m >= kHi) || !__any(m >= kLo); }
-  // to the unit in which the largest finite magnitude of the wave is 2^11; returns the change
-  __device__ __forceinline__ float move(float m) {
-    const uint32_t e = (__float_as_uint(wave_max(m)) >> 23) & 255u;
-    if (e < 16u || e > 254u) return 1.f;  // nothing but zeros
-    // kept within 2^+-96, so that products of units stay numbers
-    const int want = 127 + 11 - (int)e, have = (int)((__float_as_uint(u) >> 23) & 255u) - 127;
-    const int by = min(max(want, -96 - have), 96 - have);
-    const float f = __uint_as_float((uint32_t)(127 + by) << 23);
-    u *= f;
-    inv *= __uint_as_float((uint32_t)(127 - by) << 23);
-    return f;
-  }
-};
 
 struct SegArgs {
   DecayArgs a;
@@ -467,7 +454,6 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
   float* sout = !OUT ? (float*)a.ws + (bh * sa.nseg + seg + 1) * sdv
                 : a.state_out && t0 + SL >= len ? a.state_out + bh * sdv : nullptr;
 
-  Unit us = {F ? 0x1p5f : 1.f, F ? 0x1p-5f : 1.f};  // fp16 only; first such that values of about one do not move it
   // Decays.  Inside a diagonal 32 x 32 tile lambda^(i - j) for j <= i (i this lane's
   // token, j the register's).  At the end of a chunk token 16 x + j counts
   // lambda^(15 - j) lambda^(48 - 16 x).  One tile below the diagonal lambda^(32 + i - j)
@@ -515,7 +501,7 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
       for (int r = 0; r < 16; ++r) {
         asm volatile("" : "+v"(S[x][r]));  // or the load would move behind the condition
         const int d = 32 * x + 16 * (r >> 3) + 8 * h + (r & 7);
-        S[x][r] = whole || (d < D && col < V) ? S[x][r] * us.u : 0.f;  // zeros in the padding
+        S[x][r] = whole || (d < D && col < V) ? S[x][r] : 0.f;  // zeros in the padding
       }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -559,22 +545,19 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
 
     if (OUT) {
+      // The state's operand has one unit for the wave's columns, whose largest magnitude
+      // it follows: 2^-39 of that is what two terms leave out at most.
+      Fresh us = {1.f, 1.f};
       if (F) {
         float m = max_abs(S[0]);
 #pragma unroll
         for (int x = 1; x < DT; ++x) m = fmaxf(m, max_abs(S[x]));
-        if (Unit::leaves(m)) {
-          if (__any(m == __builtin_huge_valf())) {  // the finite ones keep their unit
-            m = 0.f;
+        if (__any(m == __builtin_huge_valf())) {  // the finite ones keep their unit
+          m = 0.f;
 #pragma unroll
-            for (int x = 0; x < DT; ++x) m = max_finite(m, S[x]);
-          }
-          const float f = us.move(m);
-#pragma unroll
-          for (int x = 0; x < DT; ++x)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) S[x][r] *= f;
+          for (int x = 0; x < DT; ++x) m = max_finite(m, S[x]);
         }
+        us = fresh_unit(wave_max(m));
       }
       // Products of the 64 queries with the state, and the scores: keys against queries
       // in the tiles (0, 0), (0, 1) and (1, 1), p holds k_j . q_i.
@@ -588,13 +571,10 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
         p[1] = E::mfma(k0, q1, p[1]);
         p[2] = E::mfma(k1, q1, p[2]);
         V8 sh, sl;
+        float part[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          T hi, lo;
-          two_terms(S[x >> 1][8 * (x & 1) + e], hi, lo);
-          sh[e] = hi;
-          sl[e] = lo;
-        }
+        for (int e = 0; e < 8; ++e) part[e] = S[x >> 1][8 * (x & 1) + e];
+        two_terms<E>(part, us.u, sh, sl);
         inter2[0] = E::mfma(sh, q0, inter2[0]);
         inter2[1] = E::mfma(sh, q1, inter2[1]);
         inter2[0] = E::mfma(sl, q0, inter2[0]);
@@ -618,11 +598,11 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
         const auto add_values = [&](const floatx16& w, int x) {  // values 16 x .. 16 x + 31
           V8 wh[2], wl[2];
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            T hi, lo;
-            two_terms(F ? w[r] * up.u : w[r], hi, lo);
-            wh[r >> 3][r & 7] = hi;
-            wl[r >> 3][r & 7] = lo;
+          for (int y = 0; y < 2; ++y) {
+            float part[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) part[e] = w[8 * y + e];
+            two_terms<E>(part, up.u, wh[y], wl[y]);
           }
           intra = E::mfma(vf[x], wl[0], intra);
           intra = E::mfma(vf[x + 1], wl[1], intra);
@@ -705,24 +685,14 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
       }
       V8 term[4][NT];
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
+      for (int x = 0; x < 4; ++x) {
+        two_terms<E>(w[x], uv.u, term[x][0], term[x][1]);
+        if (!F) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float t = w[x][e];
-          if (F) {  // the unit is a power of two: the product is as exact formed twice
-            T hi, lo;
-            two_terms(t * uv.u, hi, lo);
-            term[x][0][e] = hi;
-            term[x][1][e] = lo;
-          } else {
-#pragma unroll
-            for (int y = 0; y < NT; ++y) {
-              term[x][y][e] = (T)t;
-              t -= (float)term[x][y][e];
-            }
-          }
+          for (int e = 0; e < 8; ++e)
+            term[x][NT - 1][e] = (T)(w[x][e] - (float)term[x][0][e] - (float)term[x][1][e]);
         }
-      const float gain = uv.inv * us.u;
+      }
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const char *p0 = lds + ((ck0 + buf) ^ (64 * d)), *p1 = lds + ((ck1 + buf) ^ (64 * d));
@@ -736,7 +706,7 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
           for (int y = NT - 1; y >= 0; --y) add = E::mfma(kf[x], term[x][y], add);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) S[d][r] = F ? fmaf(add[r], gain, S[d][r] * keep.hi) : fmaf(S[d][r], keep.hi, add[r]);
+        for (int r = 0; r < 16; ++r) S[d][r] = F ? fmaf(add[r], uv.inv, S[d][r] * keep.hi) : fmaf(S[d][r], keep.hi, add[r]);
       }
       // made up for every sixteenth chunk
       owed += pad ? rest_last : rest;
@@ -760,14 +730,14 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
       for (int x = 0; x < DT; ++x)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sout[(32 * x + 16 * (r >> 3) + 8 * h + (r & 7)) * VP] = S[x][r] * us.inv;
+        for (int r = 0; r < 16; ++r) sout[(32 * x + 16 * (r >> 3) + 8 * h + (r & 7)) * VP] = S[x][r];
     } else if (col < V) {
 #pragma unroll
       for (int x = 0; x < DT; ++x)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int d = 32 * x + 16 * (r >> 3) + 8 * h + (r & 7);
-          if (d < D) sout[d * V] = S[x][r] * us.inv;
+          if (d < D) sout[d * V] = S[x][r];
         }
     }
   }

@@ -101,3 +101,16 @@ def test_quiet_values_after_loud_ones_that_have_decayed_keep_the_bits_of_the_sta
     _, wS = ref.decay_attention(f64(q), f64(k), f64(v), f64(ld))
     _, mS = ref.decay_attention(f64(q), np.abs(f64(k)), np.abs(f64(v)), f64(ld))
     state_check(S, wS, mS, 128, loud)
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("T", [3, 70, 400])
+def test_a_state_near_the_end_of_fp32_stays_finite(T, dt):
+    # magnitudes to 3.2e38 (2^127.9) in, a scale that brings the outputs back to ordinary numbers
+    say("decay, large state", T, dt)
+    g = gen(6)
+    q, k, v = (torch.randn((1, T, 2, 64), generator=g) for _ in range(3))
+    S0 = (torch.rand((1, 2, 64, 64), generator=g) * 2 - 1) * 3.2e38
+    q *= 2.0 ** -8
+    o, S, want, wS, mag, mS = attend(*(x.to(DT[dt]) for x in (q, k, v)), (0.0, -0.01), S0, 2.0 ** -120, dt, (T, dt))
+    state_check(S, wS, mS, T, (T, dt))
