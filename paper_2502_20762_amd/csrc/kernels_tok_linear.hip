@@ -23,7 +23,9 @@ __device__ __forceinline__ float act1(float v) {
   if (ACT == NCODEC_ACT_WSILU) return v * __builtin_amdgcn_rcpf(1.f + __expf(-4.f * v));
   if (ACT == NCODEC_ACT_SILU) return v * __builtin_amdgcn_rcpf(1.f + __expf(-v));
   if (ACT == NCODEC_ACT_GELU) {
-    const float a = fminf(fabsf(v), 64.f);  // Phi(-64) is 0: an infinity times it would be no number
+    // Phi(-64) is 0: an infinity times it would be no number.  This minimum keeps a NaN, the
+    // maximum below need not.
+    const float a = __builtin_elementwise_minimum(fabsf(v), 64.f);
     const float t = __builtin_amdgcn_rcpf(fmaf(0.36f, a, 1.f));
     float p = 0.047059200f;
     p = fmaf(p, t, -0.179774719f);

@@ -1,0 +1,42 @@
+"""Token operators at the edges of their arguments: values that are no numbers, infinities, and what is refused."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import tokens as ref
+from paper_2502_20762_amd import ncodec as nc
+from paper_2502_20762_amd import tokens as tk
+from test_gpu_tokens import DEV, DT, f64, gen, rnd, say
+
+pytestmark = pytest.mark.gpu
+
+NAN, INF = float("nan"), float("inf")
+
+
+# few rows, and tiles: more than 2^19 products of rows and weight rows, loaded directly and (k odd) through registers
+@pytest.mark.parametrize("m,k,n", [(5, 70, 90), (300, 256, 256), (700, 512, 1024), (700, 77, 1024)])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("act", ["none", "lrelu", "wsilu", "silu", "gelu"])
+def test_nan_goes_through_every_activation(act, gated, m, k, n):
+    say("nan", act, gated, m, k, n)
+    g = gen(1)
+    rows = 2 * n if gated else n
+    for dt in ("fp16", "bf16"):
+        x, w, b = rnd(g, (m, k), dt), rnd(g, (rows, k), dt, k ** -0.5), rnd(g, (rows,), dt)
+        clean = tk.linear(x.to(DEV), w.to(DEV), b.to(DEV), act=act, gated=gated).cpu()
+        assert torch.isfinite(clean).all()
+        x[1, 3], w[2, k - 1], b[rows - 1] = NAN, NAN, NAN  # a row, a feature, a feature
+        y = tk.linear(x.to(DEV), w.to(DEV), b.to(DEV), act=act, gated=gated).cpu()
+        hit = torch.zeros((m, n), dtype=torch.bool)
+        hit[1] = hit[:, 2] = hit[:, n - 1] = True
+        assert torch.isnan(y[hit]).all() and torch.equal(y[~hit], clean[~hit]), dt
+
+
+@pytest.mark.parametrize("m,n", [(6, 40), (800, 1024)])
+def test_gelu_of_infinities(m, n):
+    # v Phi(v) ends at 0 and at infinity
+    x = torch.zeros((m, 8), dtype=torch.float16, device=DEV)
+    x[0, 0], x[1, 0] = INF, -INF
+    w = torch.ones((n, 8), dtype=torch.float16, device=DEV)
+    y = tk.linear(x, w, act="gelu")
+    assert bool((y[0] == INF).all()) and bool((y[1:] == 0).all())
