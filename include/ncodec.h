@@ -506,7 +506,8 @@ ncodec_status ncodec_qk_norm_rope(const ncodec_qk_shape* shape, const void* d_q,
  * kv_heads x head_dim (value_dim), o: batch x tokens x heads x value_dim, each at
  * its batch, token and head strides, the last dimension contiguous.  Query
  * head h reads key head h / (heads / kv_heads).  d_log_decay: heads float32,
- * values above 0 are taken as 0, -inf keeps nothing.  d_lengths: batch int32, the
+ * values above 0 are taken as 0, -inf keeps nothing, NaN makes its head's
+ * outputs and state NaN.  d_lengths: batch int32, the
  * tokens of each sequence, clamped to [0, tokens]; NULL: all.  Past its length a
  * sequence's inputs are not used, its outputs are zero and its state stands
  * still.  d_state_in: batch x heads x head_dim x value_dim float32, contiguous,

@@ -25,16 +25,17 @@ namespace nc {
 namespace {
 
 // lambda^n = exp2(n * this).  Positive decays count as 0, -inf becomes a
-// number so that lambda^0 is 1 (0 * -inf is not a number).
+// number so that lambda^0 is 1 (0 * -inf is not a number).  A NaN stays one: these
+// minima and maxima keep it.
 __device__ __forceinline__ float log2_decay(float log_decay) {
-  return fmaxf(fminf(log_decay, 0.f), -1e30f) * 1.44269504088896341f;
+  return __builtin_elementwise_maximum(__builtin_elementwise_minimum(log_decay, 0.f), -1e30f) * 1.44269504088896341f;
 }
 
 struct Decay64 {  // lambda^n in two floats, so that long products of it lose nothing
   float hi, lo;
 };
 __device__ __forceinline__ Decay64 decay_pow(float log_decay, int64_t n) {
-  const double l = fmax(fmin((double)log_decay, 0.0), -1e30);
+  const double l = __builtin_elementwise_maximum(__builtin_elementwise_minimum((double)log_decay, 0.0), -1e30);
   const double f = exp((double)n * l);
   const float hi = (float)f;
   return {hi, (float)(f - (double)hi)};

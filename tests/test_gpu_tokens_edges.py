@@ -40,3 +40,23 @@ def test_gelu_of_infinities(m, n):
     w = torch.ones((n, 8), dtype=torch.float16, device=DEV)
     y = tk.linear(x, w, act="gelu")
     assert bool((y[0] == INF).all()) and bool((y[1:] == 0).all())
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("T", [1, 5, 90, 700])
+def test_a_decay_that_is_no_number_is_not_taken_for_one(T, dt):
+    # its head has no outputs and no state, the other heads have theirs; without tokens the state stands still
+    say("nan decay", T, dt)
+    g = gen(2)
+    q, k, v = (rnd(g, (3, T, 3, 64), dt).to(DEV) for _ in range(3))
+    S0 = torch.randn((3, 3, 64, 64), generator=g).to(DEV)
+    lengths = torch.tensor([T, T - T // 3, 0], dtype=torch.int32, device=DEV)
+    ld = torch.tensor([-0.1, -0.02, -0.3], device=DEV)
+    o, S = tk.decay_attention(q, k, v, ld, S0, lengths, return_state=True)
+    ld[1] = NAN
+    o2, S2 = tk.decay_attention(q, k, v, ld, S0, lengths, return_state=True)
+    for b, n in enumerate(lengths.tolist()):
+        assert torch.isnan(o2[b, :n, 1]).all() and bool((o2[b, n:, 1] == 0).all())
+        assert torch.isnan(S2[b, 1]).all() if n else torch.equal(S2[b, 1], S0[b, 1])
+    for h in (0, 2):
+        assert torch.equal(o2[:, :, h], o[:, :, h]) and torch.equal(S2[:, h], S[:, h])
