@@ -513,6 +513,8 @@ ncodec_status ncodec_qk_norm_rope(const ncodec_qk_shape* shape, const void* d_q,
  * still.  d_state_in: batch x heads x head_dim x value_dim float32, contiguous,
  * the state before the first token (NULL: zero); d_state_out: the state after
  * the last one (NULL: not wanted), may be d_state_in itself.
+ * What the formula carries an infinity or a NaN to is not finite, and nothing
+ * else is; where the formula has an infinity, either of the two may stand.
  * tokens = 1 is the recurrent form of a stream that goes on token by token.
  * head_dim and value_dim in [1, 128], heads and kv_heads in [1, 4096],
  * batch * heads < 2^24, tokens in [0, 2^31). */

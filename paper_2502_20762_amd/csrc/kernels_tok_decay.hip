@@ -725,7 +725,7 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
 
   if (sout) {
-    settle();
+    if (nch) settle();  // without tokens the state stands still, an infinity in it too
     sout += col;
     if (D == DP && V == VP) {
 #pragma unroll

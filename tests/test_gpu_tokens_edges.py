@@ -60,3 +60,38 @@ def test_a_decay_that_is_no_number_is_not_taken_for_one(T, dt):
         assert torch.isnan(S2[b, 1]).all() if n else torch.equal(S2[b, 1], S0[b, 1])
     for h in (0, 2):
         assert torch.equal(o2[:, :, h], o[:, :, h]) and torch.equal(S2[:, h], S[:, h])
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("T", [1, 5, 6, 70, 700])
+def test_state_without_tokens_stands_still_whatever_it_holds(T, dt):
+    g = gen(3)
+    q, k, v = (rnd(g, (2, T, 2, 64), dt).to(DEV) for _ in range(3))
+    S0 = torch.randn((2, 2, 64, 64), generator=g).to(DEV)
+    S0[0, 0, 1, 2], S0[0, 1, 60, 63], S0[0, 1, 3, 4] = INF, -INF, 3.0e38
+    lengths = torch.tensor([0, T], dtype=torch.int32, device=DEV)
+    for decay in (0.0, -0.5):
+        ld = torch.full((2,), decay, device=DEV)
+        o, S = tk.decay_attention(q, k, v, ld, S0, lengths, return_state=True)
+        assert torch.equal(S[0], S0[0]) and bool((o[0] == 0).all()) and torch.isfinite(S[1]).all()
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("T", [4, 100, 400])
+@pytest.mark.parametrize("where", ["q", "k", "v", "state"])
+@pytest.mark.parametrize("what", [INF, -INF, NAN])
+def test_what_is_not_finite_reaches_what_the_formula_says(what, where, T, dt):
+    # one value, in the middle of its stretch: the outputs and the state's elements that are not finite are the oracle's
+    say("not finite", what, where, T, dt)
+    g = gen(4)
+    x = {name: rnd(g, (1, T, 2, 64), dt) for name in "qkv"}
+    x["state"] = torch.randn((1, 2, 64, 64), generator=g)
+    at = (0, 1, 5, 40) if where == "state" else (0, T // 2, 1, 40)
+    x[where][at] = what
+    for decay in (-0.05, 0.0):
+        ld = torch.tensor([-0.1, decay])
+        o, S = tk.decay_attention(*(x[name].to(DEV) for name in "qkv"), ld.to(DEV), x["state"].to(DEV), scale=0.125,
+                                  return_state=True)
+        with np.errstate(invalid="ignore"):
+            want, wS = ref.decay_attention(*(f64(x[name]) for name in "qkv"), f64(ld), f64(x["state"]), None, 0.125)
+        assert np.array_equal(np.isfinite(f64(o)), np.isfinite(want)) and np.array_equal(np.isfinite(f64(S)), np.isfinite(wS))
