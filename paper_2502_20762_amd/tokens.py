@@ -4,8 +4,9 @@
 torch and call the library's entry points of the same names on the current stream of the tensors' device; every
 value is computed in the HIP kernels.  They take float16 or bfloat16 tensors and strided views (the last dimension
 contiguous) and raise :class:`ValueError` for tensors that do not fit together, :class:`NcodecError` for what the
-library refuses.  :class:`TokenMixer` runs them together: the layer of a temporal prior that reads the latents of
-all earlier frames through a state of fixed size.
+library refuses.  They have no backward pass: a tensor that requires a gradient is refused where torch records
+gradients, and taken under ``torch.no_grad()``.  :class:`TokenMixer` runs them together: the layer of a temporal
+prior that reads the latents of all earlier frames through a state of fixed size.
 """
 from __future__ import annotations
 
@@ -24,7 +25,13 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+def _no_grad(t):
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError("no backward pass: call under torch.no_grad(), or with tensors that require no gradient")
+
+
 def _dtype(x):
+    _no_grad(x)
     dt = _DTYPES.get(x.dtype)
     if dt is None or not x.is_cuda:
         raise ValueError(f"tensors must be float16 or bfloat16 on the GPU, not {x.dtype} on {x.device}")
@@ -32,7 +39,8 @@ def _dtype(x):
 
 
 def _like(t, dtype, device, shape, what):
-    """t has this type, device (index) and shape, its last dimension contiguous."""
+    """t has this type, device (index) and shape, its last dimension contiguous, and asks for no gradient."""
+    _no_grad(t)
     if t.dtype != dtype or t.get_device() != device:
         raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {dtype} on cuda:{device}")
     if t.shape != shape:

@@ -95,3 +95,26 @@ def test_what_is_not_finite_reaches_what_the_formula_says(what, where, T, dt):
         with np.errstate(invalid="ignore"):
             want, wS = ref.decay_attention(*(f64(x[name]) for name in "qkv"), f64(ld), f64(x["state"]), None, 0.125)
         assert np.array_equal(np.isfinite(f64(o)), np.isfinite(want)) and np.array_equal(np.isfinite(f64(S)), np.isfinite(wS))
+
+
+def test_tensors_that_require_a_gradient_are_refused():
+    # there is no backward pass, and a result without a graph would hide that
+    def made(*shape, dtype=torch.float16):
+        return torch.randn(shape, device=DEV).to(dtype)
+
+    lin = [made(4, 64), made(32, 64), made(32), made(4, 32)]
+    rope = [made(4, 2, 32), made(4, 1, 32), made(32), made(32), torch.zeros((4, 1), dtype=torch.int32, device=DEV),
+            tk.rope_frequencies((16,), device=DEV)]
+    decay = [made(1, 4, 2, 32), made(1, 4, 2, 32), made(1, 4, 2, 16), -torch.ones(2, device=DEV),
+             made(1, 2, 32, 16, dtype=torch.float32)]
+    for call, args in ((lambda *a: tk.linear(*a), lin), (lambda *a: tk.qk_norm_rope(*a, (16,)), rope),
+                       (lambda *a: tk.decay_attention(*a, return_state=True), decay)):
+        call(*args)
+        for i, t in enumerate(args):
+            if t.is_floating_point():
+                t.requires_grad_()
+                with pytest.raises(ValueError, match="no backward pass"):
+                    call(*args)
+                with torch.no_grad():
+                    call(*args)
+                t.requires_grad_(False)
