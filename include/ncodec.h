@@ -436,7 +436,9 @@ ncodec_status ncodec_timing_read(ncodec_ctx* ctx, ncodec_kernel_timing* out, int
  * that does nothing.  EINVAL: a null pointer, enum or value out of range;
  * ESHAPE: a size or stride out of range; ENOMEM: workspace too small or
  * misaligned; EHIP: a HIP call failed.  ncodec_last_error(NULL) gives the
- * message.  Outputs must not overlap inputs unless stated. */
+ * message.  Outputs must not overlap inputs or each other unless stated: EINVAL
+ * where they are not seen to lie apart (one behind the other, or as different
+ * columns, heads or rows of a common period, as parts of one buffer do). */
 typedef enum { NCODEC_DTYPE_FP16 = 0, NCODEC_DTYPE_BF16 = 1 } ncodec_dtype;
 
 /* Activations: v; max(v, 0.1 v); v sigmoid(4 v); v sigmoid(v); v Phi(v). */

@@ -3,9 +3,13 @@
 #include <string>
 
 #include "../../include/ncodec.h"
+#include "areas.hpp"
 #include "tokens.hpp"
 
 namespace {
+
+using nc::all_apart;
+using nc::Area;
 
 // Records the message; nothing is thrown across the C entry.
 ncodec_status set_error(ncodec_status st, const char* where, const char* why, size_t bytes = 0) noexcept {
@@ -108,6 +112,13 @@ extern "C" ncodec_status ncodec_linear(const ncodec_linear_shape* shape, const v
     return set_error(NCODEC_EINVAL, "linear", "a pointer is not aligned to an element");
   if (d_r == d_y && d_r && shape->ldr != shape->ldy)
     return set_error(NCODEC_EINVAL, "linear", "d_y is d_r, but ldy is not ldr");
+  {
+    const ncodec_linear_shape& s = *shape;
+    const int64_t nw = s.n * (s.gated ? 2 : 1);
+    const Area y(d_y, s.n, {s.m, s.ldy}), r(d_r == d_y ? nullptr : d_r, s.n, {s.m, s.ldr});
+    if (!all_apart(y, {Area(d_x, s.k, {s.m, s.ldx}), Area(d_w, s.k, {nw, s.ldw}), Area(d_b, nw, 2), r}))
+      return set_error(NCODEC_EINVAL, "linear", "d_y overlaps an input");
+  }
   return finish(nc::launch_linear({*shape, d_x, d_w, d_b, d_r, d_y}, (hipStream_t)hip_stream), "linear");
 }
 
@@ -125,6 +136,25 @@ extern "C" ncodec_status ncodec_qk_norm_rope(const ncodec_qk_shape* shape, const
   if (!aligned(d_q, 2) || !aligned(d_k, 2) || !aligned(d_qo, 2) || !aligned(d_ko, 2) || !aligned(d_wq, 2) ||
       !aligned(d_wk, 2) || (rot && (!aligned(d_pos, 4) || !aligned(d_freq, 4))))
     return set_error(NCODEC_EINVAL, "qk_norm_rope", "a pointer is not aligned to an element");
+  {
+    const ncodec_qk_shape& s = *shape;
+    const Area q(d_q, s.head_dim, {s.tokens, s.q_token_stride, s.q_heads, s.q_head_stride}),
+        k(d_k, s.head_dim, {s.tokens, s.k_token_stride, s.k_heads, s.k_head_stride}),
+        qo(d_qo, s.head_dim, {s.tokens, s.qo_token_stride, s.q_heads, s.qo_head_stride}),
+        ko(d_ko, s.head_dim, {s.tokens, s.ko_token_stride, s.k_heads, s.ko_head_stride});
+    const Area wq(s.norm ? d_wq : nullptr, s.head_dim, 2), wk(s.norm ? d_wk : nullptr, s.head_dim, 2),
+        pos(rot ? d_pos : nullptr, s.tokens * s.axes, 4),
+        freq(rot ? d_freq : nullptr, s.section[0] + s.section[1] + s.section[2], 4);
+    const auto same = [&](const void* a, const void* b, int64_t heads, int64_t ta, int64_t tb, int64_t ha, int64_t hb) {
+      return a == b && (s.tokens == 1 || ta == tb) && (heads == 1 || ha == hb);
+    };
+    const Area none(nullptr, 0, 2);
+    const bool q_in_place = same(d_q, d_qo, s.q_heads, s.q_token_stride, s.qo_token_stride, s.q_head_stride, s.qo_head_stride),
+               k_in_place = same(d_k, d_ko, s.k_heads, s.k_token_stride, s.ko_token_stride, s.k_head_stride, s.ko_head_stride);
+    if (!all_apart(qo, {q_in_place ? none : q, k, ko, wq, wk, pos, freq}) ||
+        !all_apart(ko, {k_in_place ? none : k, q, wq, wk, pos, freq}))
+      return set_error(NCODEC_EINVAL, "qk_norm_rope", "an output overlaps an input that it is not, or the other output");
+  }
   return finish(nc::launch_qk_norm_rope({*shape, d_q, d_k, d_wq, d_wk, d_pos, d_freq, d_qo, d_ko},
                                         (hipStream_t)hip_stream),
                 "qk_norm_rope");
@@ -153,6 +183,19 @@ extern "C" ncodec_status ncodec_decay_attention(const ncodec_decay_shape* shape,
   const size_t need = nc::decay_workspace_bytes(*shape);
   if (need && (!d_workspace || ws_bytes < need || !aligned(d_workspace, 256)))
     return set_error(NCODEC_ENOMEM, "decay_attention", "the workspace must be 256-byte aligned and hold ", need);
+  {
+    const ncodec_decay_shape& s = *shape;
+    const Area q(d_q, s.head_dim, {s.batch, s.q_batch_stride, s.tokens, s.q_token_stride, s.heads, s.q_head_stride}),
+        k(d_k, s.head_dim, {s.batch, s.k_batch_stride, s.tokens, s.k_token_stride, s.kv_heads, s.k_head_stride}),
+        v(d_v, s.value_dim, {s.batch, s.v_batch_stride, s.tokens, s.v_token_stride, s.kv_heads, s.v_head_stride}),
+        o(d_o, s.value_dim, {s.batch, s.o_batch_stride, s.tokens, s.o_token_stride, s.heads, s.o_head_stride});
+    const int64_t elements = s.batch * s.heads * s.head_dim * s.value_dim;
+    const Area decay(d_log_decay, s.heads, 4), lengths(d_lengths, s.batch, 4), si(d_state_in, elements, 4),
+        so(d_state_out, elements, 4);
+    if (!all_apart(o, {q, k, v, decay, lengths, si, so}) ||
+        !all_apart(so, {q, k, v, decay, lengths, d_state_out == d_state_in ? Area(nullptr, 0, 4) : si}))
+      return set_error(NCODEC_EINVAL, "decay_attention", "an output overlaps an input that it is not, or the other output");
+  }
   return finish(nc::launch_decay_attention({*shape, d_q, d_k, d_v, d_log_decay, d_lengths, d_state_in, d_state_out,
                                             d_o, d_workspace},
                                            (hipStream_t)hip_stream),

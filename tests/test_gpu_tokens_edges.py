@@ -118,3 +118,40 @@ def test_tensors_that_require_a_gradient_are_refused():
                 with torch.no_grad():
                     call(*args)
                 t.requires_grad_(False)
+
+
+def test_outputs_over_inputs_are_refused_and_parts_of_one_buffer_are_not():
+    g = gen(5)
+    x, w = rnd(g, (700, 512), "fp16").to(DEV), rnd(g, (512, 512), "fp16", 0.05).to(DEV)
+    before = x.clone()
+    for bad in (lambda: tk.linear(x, w, out=x), lambda: tk.linear(x[:512], w, out=w), lambda: tk.linear(x[1:], w, out=x[:-1]),
+                lambda: tk.linear(x[:-1], w, residual=x[1:], out=x[:-1])):
+        with pytest.raises(nc.NcodecError) as e:
+            bad()
+        assert e.value.status == nc.NCODEC_EINVAL
+    assert torch.equal(x, before)
+    buf = torch.zeros((700, 1024), dtype=torch.float16, device=DEV)
+    buf[:, :512] = x
+    tk.linear(buf[:, :512], w, out=buf[:, 512:])
+    assert torch.equal(buf[:, :512], x) and torch.equal(buf[:, 512:], tk.linear(x, w))
+    # heads of one buffer: q, k, v, the rotated q and k, and the attention's output
+    T, H, D = 90, 2, 64
+    buf = rnd(g, (2, T, 6 * H, D), "fp16").to(DEV)
+    q, k, v, q2, k2, o = (buf[:, :, H * i:H * i + H] for i in range(6))
+    pos, fr = tk.grid_positions(2, 9, 10, device=DEV), tk.rope_frequencies((16, 8, 8), device=DEV)
+    ld = torch.tensor([-0.1, -0.02], device=DEV)
+    apart = [t.contiguous() for t in (q, k, v)]
+    a, b = tk.qk_norm_rope(apart[0].view(-1, H, D), apart[1].view(-1, H, D), None, None, pos, fr, (16, 8, 8))
+    flat = [t.reshape(2 * T, H, D) if t.is_contiguous() else buf.view(2 * T, 6 * H, D)[:, H * i:H * i + H]
+            for i, t in enumerate((q, k, v, q2, k2, o))]
+    tk.qk_norm_rope(flat[0], flat[1], None, None, pos, fr, (16, 8, 8), q_out=flat[3], k_out=flat[4])
+    assert torch.equal(flat[3], a) and torch.equal(flat[4], b)
+    want = tk.decay_attention(a.view(2, T, H, D), b.view(2, T, H, D), apart[2], ld)
+    tk.decay_attention(q2, k2, v, ld, out=o)
+    assert torch.equal(o, want) and torch.equal(v, apart[2])
+    for bad in (lambda: tk.qk_norm_rope(flat[0], flat[1], q_out=flat[1], k_out=flat[4]),
+                lambda: tk.qk_norm_rope(flat[0], flat[1], q_out=flat[3], k_out=flat[3]),
+                lambda: tk.decay_attention(q, k, v, ld, out=v), lambda: tk.decay_attention(q, k, v, ld, out=q)):
+        with pytest.raises(nc.NcodecError) as e:
+            bad()
+        assert e.value.status == nc.NCODEC_EINVAL
