@@ -433,7 +433,8 @@ ncodec_status ncodec_timing_read(ncodec_ctx* ctx, ncodec_kernel_timing* out, int
  * Elements are IEEE binary16 or bfloat16 (ncodec_dtype), device pointers need
  * the alignment of an element only (16-byte aligned rows are faster), and
  * strides count elements.  A zero count of rows, tokens or sequences is a call
- * that does nothing.  EINVAL: a null pointer, enum or value out of range;
+ * that does nothing, save that attention over sequences without tokens still
+ * gives their states.  EINVAL: a null pointer, enum or value out of range;
  * ESHAPE: a size or stride out of range; ENOMEM: workspace too small or
  * misaligned; EHIP: a HIP call failed.  ncodec_last_error(NULL) gives the
  * message.  Outputs must not overlap inputs or each other unless stated: EINVAL
@@ -514,7 +515,9 @@ ncodec_status ncodec_qk_norm_rope(const ncodec_qk_shape* shape, const void* d_q,
  * sequence's inputs are not used, its outputs are zero and its state stands
  * still.  d_state_in: batch x heads x head_dim x value_dim float32, contiguous,
  * the state before the first token (NULL: zero); d_state_out: the state after
- * the last one (NULL: not wanted), may be d_state_in itself.
+ * the last one (NULL: not wanted), may be d_state_in itself.  A sequence without
+ * tokens, tokens = 0 included, leaves there the state before (zeros where
+ * d_state_in is NULL).
  * What the formula carries an infinity or a NaN to is not finite, and nothing
  * else is; where the formula has an infinity, either of the two may stand.
  * tokens = 1 is the recurrent form of a stream that goes on token by token.

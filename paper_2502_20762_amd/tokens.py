@@ -192,7 +192,8 @@ def decay_attention(q, k, v, log_decay, state=None, lengths=None, scale=None, re
     log_decay: (heads) float32 <= 0, state: (batch, heads, dim, value_dim) float32 before the first token (None:
     zero), lengths: (batch) int32 tokens of each sequence (None: all; past them outputs are zero), scale: default
     dim^-0.5.  Returns o (batch, tokens, heads, value_dim), with return_state (o, state after the last token).
-    ``state_out`` may be ``state`` itself: one token per call is the recurrent form."""
+    ``state_out`` may be ``state`` itself: one token per call is the recurrent form.  Sequences without tokens leave
+    their state as it was (None: zeros)."""
     dt = _dtype(q)
     qs, ks, vs = q.shape, k.shape, v.shape
     _need(len(qs) == 4 and len(ks) == 4 and len(vs) == 4, "q, k and v must be (batch, tokens, heads, dim)")

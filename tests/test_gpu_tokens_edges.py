@@ -155,3 +155,19 @@ def test_outputs_over_inputs_are_refused_and_parts_of_one_buffer_are_not():
         with pytest.raises(nc.NcodecError) as e:
             bad()
         assert e.value.status == nc.NCODEC_EINVAL
+
+
+@pytest.mark.parametrize("T", [0, 1, 80])
+def test_no_tokens_leave_the_state_before_or_zeros_and_no_sequences_leave_nothing(T):
+    # the states are written whether no token is there, or none is counted
+    x = torch.ones((2, T, 1, 32), dtype=torch.float16, device=DEV)
+    ld = torch.zeros(1, device=DEV)
+    none = torch.zeros(2, dtype=torch.int32, device=DEV)
+    S0 = torch.randn((2, 1, 32, 32), device=DEV)
+    out = torch.full_like(S0, 7.0)
+    tk.decay_attention(x, x, x, ld, S0, none, state_out=out)
+    assert torch.equal(out, S0)
+    tk.decay_attention(x, x, x, ld, None, none, state_out=out)
+    assert bool((out == 0).all())
+    o = tk.decay_attention(x[:0], x[:0], x[:0], ld, S0[:0], state_out=out[:0])
+    assert o.shape == (0, T, 1, 32) and bool((out == 0).all())
