@@ -19,6 +19,7 @@
 // and 16.
 #include <algorithm>
 
+#include "token_rules.hpp"
 #include "tokens.hpp"
 
 namespace nc {
@@ -134,8 +135,6 @@ __global__ __launch_bounds__(256) void k_tok_decay_recur(DecayArgs a) {
 }
 
 // ---- chunks -------------------------------------------------------------------
-constexpr int kChunk = 64;
-
 // LDS: two buffers of k (and q), one of v, which goes to registers first thing.
 template <class E, int DP_, int NV_, bool OUT>
 struct Chunk {
@@ -798,35 +797,7 @@ __global__ __launch_bounds__(512) void k_tok_decay_scan(SegArgs sa) {
   }
 }
 
-// Sequences shorter than this run the recurrence, which takes a step of 1 to 2 us for
-// every token where a chunk takes the same time for 1 and 64.  us there / in a chunk: 4
-// tokens 7.4 / 8.4 with 8 heads of 64 x 64, 8.5 / 10.0 with 8 of 128 x 128, 15.6 / 17.0 with
-// 512 of these; 6 tokens 9.5 / 8.4, 11.1 / 10.1, 19.4 / 17.1.
-constexpr int64_t kRecurTokens = 6;
-
-struct Plan {
-  bool chunked;
-  int seg_chunks, nseg;
-};
-
-// One wave a SIMD (1,024 of them) is where splitting a sequence stops to pay for
-// the second pass over k and v: 512 heads of 8 chunks take 44 us whole and 76 us in
-// halves.  Below that the sequences are cut so that two waves share a SIMD, into
-// segments of two chunks at least (16 heads of 510 chunks, 64 x 64: 90 us in 64 segments, 121
-// in 32, 112 in 128; 8 heads of 128 chunks: 44.6 us in twos, 44.1 singly in fp16, 39.4 and
-// 41.0 in bf16).
-Plan plan_of(const ncodec_decay_shape& s) {
-  Plan p{s.tokens >= kRecurTokens, 0, 1};
-  const int64_t chunks = (s.tokens + kChunk - 1) / kChunk, bh = s.batch * s.heads;
-  if (!p.chunked || bh == 0) return p;
-  const int64_t waves = s.value_dim <= 32 ? 1 : s.value_dim <= 64 ? 2 : 4;
-  int64_t nseg = 1;
-  if (bh * waves < 1024) nseg = std::max<int64_t>(1, std::min(chunks / 2, 2048 / (bh * waves)));
-  const int64_t per = (chunks + nseg - 1) / nseg;
-  p.seg_chunks = (int)per;
-  p.nseg = (int)((chunks + per - 1) / per);
-  return p;
-}
+DecayPlan plan_of(const ncodec_decay_shape& s) { return decay_rule(s.batch * s.heads, s.tokens, s.value_dim); }
 
 template <class E, bool VEC>
 hipError_t recur(const DecayArgs& a, hipStream_t st) {
@@ -873,7 +844,7 @@ hipError_t by_dim(const SegArgs& sa, hipStream_t st) {
 template <class E>
 hipError_t run(const DecayArgs& a, hipStream_t st) {
   const ncodec_decay_shape& s = a.s;
-  const Plan p = plan_of(s);
+  const DecayPlan p = plan_of(s);
   if (!p.chunked) {
     const bool vec = s.value_dim % 4 == 0 && (uintptr_t)a.state_in % 16 == 0 && (uintptr_t)a.state_out % 16 == 0;
     return vec ? recur<E, true>(a, st) : recur<E, false>(a, st);
@@ -895,7 +866,7 @@ hipError_t run(const DecayArgs& a, hipStream_t st) {
 }  // namespace
 
 size_t decay_workspace_bytes(const ncodec_decay_shape& s) {
-  const Plan p = plan_of(s);
+  const DecayPlan p = plan_of(s);
   if (p.nseg == 1) return 0;
   return (size_t)(s.batch * s.heads) * (size_t)p.nseg * (size_t)(s.head_dim * s.value_dim) * 4;
 }

@@ -6,6 +6,7 @@
 // Operands are read as they lie in memory: nothing is packed beforehand.
 #include <algorithm>
 
+#include "token_rules.hpp"
 #include "tokens.hpp"
 
 namespace nc {
@@ -405,43 +406,25 @@ hipError_t go_rows(const LinearArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Which kernel, by the size alone (times in us, bf16, both sides; m x k -> n, n the
-// weight rows).
-//  - Few outputs go to the rows kernel, whose waves share K: 130 x 2048 -> 1024
-//    10.4 there and 19.5 on the smallest tile; the two meet at about 2^19 outputs
-//    (512 x 1024 -> 1024: 11.9 and 11.7; 1000 x 256 -> 1024: 7.9 and 5.9).
-//    Its own token blocks grow with the outputs: 64 x 1024 -> 1024 4.1 / 5.0 / 7.1 with
-//    16 / 32 / 64 tokens, 512 x 256 -> 256 4.0 / 3.1 / 3.8, 1000 x 1024 -> 256 9.5 / 7.9 / 7.3.
-//  - Then the largest tile (features x tokens) that still leaves work for most CUs: 256 x 256
-//    from 150 of them on (14793 x 2048 -> 712 64 us, 69 in 256 x 128, 68 in 128 x 128; with 128 of
-//    them, 8160 x 1024 -> 1024, 31.5 against 24.1), 256 x 128 in stages of 64 from 150 of those (8160
-//    x 2048 -> 1024 41.5, 50 in 128 x 128; with 128 of them, 8160 x 2048 -> 512, 33 against 28),
-//    128 x 64 up to three a CU (3000 x 1024 -> 1024 15.0, 18 in 128 x 128), else 128 x 128.
-//  - Short contractions, K < 512, are mostly epilogue and stay with the small tiles (6000 x
-//    256 -> 1024 9.9 in 128 x 64, 11.4 in 256 x 128), and up to K = 512 a large product takes
-//    256 x 128 in stages of 32: two workgroups a CU, one's epilogue behind the other's
-//    products (32640 x 512 -> 2048 with GELU, fp16: 121 to 127, 133 to 139 in 256 x 256).
-// Rows that are not 16-byte aligned go through registers; tiles of three sizes.
 template <class E, bool GATED>
 hipError_t pick(const LinearArgs& a, hipStream_t st) {
   const ncodec_linear_shape& s = a.s;
-  const int64_t nf = s.n * (GATED ? 2 : 1), outs = s.m * nf;
-  if (s.m <= 16 || outs <= ((int64_t)1 << 19)) {
-    if (s.m <= 16 || outs <= 96 * 1024) return go_rows<E, GATED, 1>(a, st);
-    if (s.m <= 32 || outs <= 192 * 1024) return go_rows<E, GATED, 2>(a, st);
-    return go_rows<E, GATED, 4>(a, st);
+  const bool direct =
+      s.k % 8 == 0 && s.ldx % 8 == 0 && s.ldw % 8 == 0 && (uintptr_t)a.x % 16 == 0 && (uintptr_t)a.w % 16 == 0;
+  switch (linear_rule(s.m, s.n * (GATED ? 2 : 1), s.k, direct)) {
+    case LinearKernel::rows16: return go_rows<E, GATED, 1>(a, st);
+    case LinearKernel::rows32: return go_rows<E, GATED, 2>(a, st);
+    case LinearKernel::rows64: return go_rows<E, GATED, 4>(a, st);
+    case LinearKernel::reg128x64: return go_tile<E, GATED, false, 2, 2, 1, 32, 2>(a, st);
+    case LinearKernel::reg128x128: return go_tile<E, GATED, false, 2, 2, 2, 32, 2>(a, st);
+    case LinearKernel::reg256x256: return go_tile<E, GATED, false, 4, 2, 4, 32, 2>(a, st);
+    case LinearKernel::dma128x64: return go_tile<E, GATED, true, 2, 2, 1, 64, 2>(a, st);
+    case LinearKernel::dma128x128: return go_tile<E, GATED, true, 2, 2, 2, 32, 3>(a, st);
+    case LinearKernel::dma256x128k32: return go_tile<E, GATED, true, 4, 2, 2, 32, 3>(a, st);
+    case LinearKernel::dma256x128k64: return go_tile<E, GATED, true, 4, 2, 2, 64, 2>(a, st);
+    case LinearKernel::dma256x256: return go_tile<E, GATED, true, 4, 2, 4, 64, 2>(a, st);
   }
-  const auto tiles = [&](int64_t f, int64_t tok) { return ((s.m + tok - 1) / tok) * ((nf + f - 1) / f); };
-  const bool dma = s.k % 8 == 0 && s.ldx % 8 == 0 && s.ldw % 8 == 0 && (uintptr_t)a.x % 16 == 0 && (uintptr_t)a.w % 16 == 0;
-  const bool small = tiles(128, 64) <= 768;
-  if (!dma) {
-    if (tiles(256, 256) >= 150) return go_tile<E, GATED, false, 4, 2, 4, 32, 2>(a, st);
-    return small ? go_tile<E, GATED, false, 2, 2, 1, 32, 2>(a, st) : go_tile<E, GATED, false, 2, 2, 2, 32, 2>(a, st);
-  }
-  if (s.k <= 512 && tiles(256, 256) >= 512) return go_tile<E, GATED, true, 4, 2, 2, 32, 3>(a, st);
-  if (s.k >= 512 && tiles(256, 256) >= 150) return go_tile<E, GATED, true, 4, 2, 4, 64, 2>(a, st);
-  if (s.k >= 512 && tiles(256, 128) >= 150) return go_tile<E, GATED, true, 4, 2, 2, 64, 2>(a, st);
-  return small ? go_tile<E, GATED, true, 2, 2, 1, 64, 2>(a, st) : go_tile<E, GATED, true, 2, 2, 2, 32, 3>(a, st);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
