@@ -26,13 +26,12 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _no_grad(t):
-    if t.requires_grad and torch.is_grad_enabled():
-        raise ValueError("no backward pass: call under torch.no_grad(), or with tensors that require no gradient")
+_NO_BACKWARD = "no backward pass: call under torch.no_grad(), or with tensors that require no gradient"
 
 
 def _dtype(x):
-    _no_grad(x)
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError(_NO_BACKWARD)
     dt = _DTYPES.get(x.dtype)
     if dt is None or not x.is_cuda:
         raise ValueError(f"tensors must be float16 or bfloat16 on the GPU, not {x.dtype} on {x.device}")
@@ -41,7 +40,8 @@ def _dtype(x):
 
 def _like(t, dtype, device, shape, what):
     """t has this type, device (index) and shape, its last dimension contiguous, and asks for no gradient."""
-    _no_grad(t)
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(_NO_BACKWARD)
     if t.dtype != dtype or t.get_device() != device:
         raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {dtype} on cuda:{device}")
     if t.shape != shape:
