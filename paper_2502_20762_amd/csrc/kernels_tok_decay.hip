@@ -328,7 +328,11 @@ __device__ __forceinline__ void two_terms(const float (&x)[8], float u, typename
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
     const float a = x[i] * u, b = x[i + 1] * u;  // u a power of two: exact, however often it is formed
-    typename E::V2 h = {(typename E::T)a, (typename E::T)b};
+    typename E::V2 h;
+    if (__is_same(E, F16))
+      h = {(typename E::T)a, (typename E::T)b};
+    else  // bf16 has no unit: the upper halves, which no value close to the end of fp32 rounds up to infinity
+      h = __builtin_bit_cast(typename E::V2, __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u));
     asm("" : "+v"(h));  // or each half would be formed anew for its rest
     const typename E::V2 l = {(typename E::T)(a - (float)h.x), (typename E::T)(b - (float)h.y)};
     hi[i] = h.x;

@@ -114,3 +114,16 @@ def test_a_state_near_the_end_of_fp32_stays_finite(T, dt):
     q *= 2.0 ** -8
     o, S, want, wS, mag, mS = attend(*(x.to(DT[dt]) for x in (q, k, v)), (0.0, -0.01), S0, 2.0 ** -120, dt, (T, dt))
     state_check(S, wS, mS, T, (T, dt))
+
+
+@pytest.mark.parametrize("T", [3, 70, 400])
+def test_a_state_past_the_largest_bf16_stays_finite(T):
+    # fp32 ends at 3.4028e38, bf16 at 3.3895e38: between them a first term must not round up
+    say("decay, state past bf16", T)
+    g = gen(7)
+    q, k, v = (torch.randn((1, T, 2, 64), generator=g) for _ in range(3))
+    S0 = torch.where(torch.rand((1, 2, 64, 64), generator=g) < 0.5, -3.402e38, 3.402e38)
+    k *= 2.0 ** -8  # so that what is added is far from what a state at the end still holds
+    q *= 2.0 ** -8
+    o, S, want, wS, mag, mS = attend(*(x.bfloat16() for x in (q, k, v)), (0.0, -0.01), S0, 2.0 ** -120, "bf16", T)
+    state_check(S, wS, mS, T, T)
