@@ -421,8 +421,8 @@ ncodec_status ncodec_timing_enable(ncodec_ctx* ctx, int32_t enable);
 ncodec_status ncodec_timing_read(ncodec_ctx* ctx, ncodec_kernel_timing* out, int32_t max_kinds, int32_t* n_kinds);
 
 /* ---- Token operators ------------------------------------------------------
- * What a mixer over latent tokens is made of: a learned temporal prior that
- * sees more of the past than the previous frame.  A token is one position
+ * What a mixer over latent tokens is made of, a layer that sees more of the
+ * past than the previous frame.  A token is one position
  * (t, h, w) of the 1/16 latent grid.  Matrix products with their epilogue, the
  * norms of queries and keys with the rotation by the token's position, and
  * attention whose memory of all earlier tokens is a state of fixed size.

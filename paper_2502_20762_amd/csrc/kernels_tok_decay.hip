@@ -13,10 +13,10 @@
 // The bytes of q, k, v and o are the floor.  What bounds the chunks is not them but
 // the work between two of them: a wave goes through scores, outputs and state one
 // after the other, MFMAs and the arithmetic on their results taking turns.  130,560
-// tokens of 16 heads of 128 x 128, fp16, 2.1 GB: 766 us (2.8 TB/s; 220 + 14 + 525, VALU
-// issuing 54 % of the time, MFMAs 35 %); 64 sequences of 512 tokens, 8 heads of 64 x 64, 134 MB:
-// 44 us (3.1 TB/s); 8,160 tokens of 8 heads of 64 x 64, 33 MB: 32 us, three launches of 10, 6
-// and 16.
+// tokens of 16 heads of 128 x 128, fp16, 2.1 GB: 832 us (2.6 TB/s; 219 + 14 + 591 at best, in
+// the last VALU issuing 64 % of the CUs' busy time, MFMAs 42 %); 64 sequences of 512 tokens, 8 heads of 64 x
+// 64, 134 MB: 43 us (3.1 TB/s); 8,160 tokens of 8 heads of 64 x 64, 33 MB: 32 us, three launches
+// of 9, 6 and 17.
 #include <algorithm>
 
 #include "token_rules.hpp"
@@ -321,8 +321,9 @@ __device__ __forceinline__ float max_finite(float m, const floatx16& v) {
 // Operands.  Scores, the state and weighted values are fp32; MFMA operands have 16
 // bits.  They go in as sums of 16-bit terms, each the rest of the one before: two
 // hold 22 bits in fp16 and 16 in bf16, where an output keeps 11 and 8, so that the
-// outputs' own rounding is the only one that counts (with one term, as many bits as
-// the output, the error of the outputs was 1.4 times that of their rounding).
+// outputs' own rounding is the only one that counts.  With one term, as many bits as
+// the output, the outputs err 1.4 times as much as their rounding, for 0.88 to 1.1 times
+// the time (130,560 tokens of 16 heads of 128 x 128: 536 us for the last pass, 591 with two).
 template <class E>
 __device__ __forceinline__ void two_terms(const float (&x)[8], float u, typename E::V8& hi, typename E::V8& lo) {
 #pragma unroll
@@ -550,7 +551,7 @@ __global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
     if (OUT) {
       // The state's operand has one unit for the wave's columns, whose largest magnitude
-      // it follows: 2^-39 of that is what two terms leave out at most.
+      // it follows: an element keeps 22 bits, or those above 2^-39 of that magnitude.
       Fresh us = {1.f, 1.f};
       if (F) {
         float m = max_abs(S[0]);
@@ -857,8 +858,8 @@ hipError_t run(const DecayArgs& a, hipStream_t st) {
     return (uintptr_t)x % 16 == 0 && batch % 8 == 0 && token % 8 == 0 && head % 8 == 0 && token < (1 << 26);
   };
   // Straight to LDS where rows are whole 16-byte units, through registers otherwise (8,160
-  // tokens of 8 heads of 64 x 64 31.7 us, 33.9 through registers; 130,560 of 16 heads of 128 x
-  // 128 935, 1,134, one head's tokens next to each other).
+  // tokens of 8 heads of 64 x 64 33.1 us, 35.8 through registers; 130,560 of 16 heads of 128 x
+  // 128, one head's tokens next to each other, 832 and 935).
   const bool dma = s.head_dim % 8 == 0 && s.value_dim % 8 == 0 &&
                    direct(a.q, s.q_batch_stride, s.q_token_stride, s.q_head_stride) &&
                    direct(a.k, s.k_batch_stride, s.k_token_stride, s.k_head_stride) &&

@@ -1,8 +1,8 @@
 // RMS norm of every query and key head and the rotation by the token's
 // position, in one pass over q and k: each element is read once and written
 // once, so the bytes are the bound: 130,560 tokens of 10 + 10 heads of 128, 1.34 GB, take
-// 226 us (5.9 TB/s; a large copy reaches 5.0 and one inside the last-level cache 6.6),
-// 8,160 tokens of 8 + 8 heads of 64, 33 MB, 7.6 us (4.4 TB/s).  A few tokens take the 2.5 to
+// 235 us (5.7 TB/s; a large copy reaches 5.0 and one inside the last-level cache 6.6),
+// 8,160 tokens of 8 + 8 heads of 64, 33 MB, 8.4 us (4.0 TB/s).  A few tokens take the 2.5 to
 // 3 us of a launch.
 #include <algorithm>
 

@@ -55,8 +55,8 @@ constexpr int kChunk = 64;  // tokens
 
 // Sequences shorter than this run the recurrence, which takes a step of 1 to 2 us for
 // every token where a chunk takes the same time for 1 and 64.  us there / in a chunk: 4
-// tokens 7.4 / 8.4 with 8 heads of 64 x 64, 8.5 / 10.0 with 8 of 128 x 128, 15.6 / 17.0 with
-// 512 of these; 6 tokens 9.5 / 8.4, 11.1 / 10.1, 19.4 / 17.1.
+// tokens 7.0 / 8.4 with 8 heads of 64 x 64, 8.2 / 11.4 with 8 of 128 x 128, 18.6 / 19.8 with
+// 512 of these; 6 tokens 9.2 / 8.5, 10.7 / 11.4, 22.2 / 19.8.
 constexpr int64_t kRecurTokens = 6;
 
 struct DecayPlan {
@@ -65,11 +65,14 @@ struct DecayPlan {
 };
 
 // One wave a SIMD (1,024 of them) is where splitting a sequence stops to pay for
-// the second pass over k and v: 512 heads of 8 chunks take 44 us whole and 76 us in
-// halves.  Below that the sequences are cut so that two waves share a SIMD, into
-// segments of two chunks at least (16 heads of 510 chunks, 64 x 64: 90 us in 64 segments, 121
-// in 32, 112 in 128; 8 heads of 128 chunks: 44.6 us in twos, 44.1 singly in fp16, 39.4 and
-// 41.0 in bf16).
+// the second pass over k and v: 512 heads of 8 chunks of 64 x 64 take 43 us whole and 52 in
+// halves.  Below that the sequences are cut into two waves for each SIMD, in
+// segments of two chunks at least (16 heads of 510 chunks, 64 x 64: 93 us in 64 segments, 117
+// in 32, 106 in 128; 8 heads of 128 chunks: 32.0 us in twos, 34.1 singly in fp16, 32.7 and
+// 33.8 in bf16).  Two waves are resident on a SIMD where a workgroup has four, or
+// two and a head_dim up to 64; with fewer waves the LDS of the workgroups, and at
+// 128 x 64 the registers, leave room for one or less, and the others follow (8 heads of
+// 128 chunks: 64 x 32 24 us, 128 x 32 32, 128 x 64 41).
 inline DecayPlan decay_rule(int64_t bh, int64_t tokens, int64_t value_dim) {
   DecayPlan p{tokens >= kRecurTokens, 0, 1};
   const int64_t chunks = (tokens + kChunk - 1) / kChunk;

@@ -1,9 +1,11 @@
-"""A mixer over latent tokens: the layer of a temporal prior that sees every earlier frame.
+"""A mixer over latent tokens: a layer that sees every earlier frame.
 
 The codec's own memory of the past is one frame: the context f_{t-1} and the latent yhat_{t-1} that its prior reads.
 :class:`TokenMixer` reads the decoded latents of a stream as tokens, one per position (t, h, w) of the 1/16 grid, and
 keeps all of them in a state of fixed size (heads x head_dim x head_dim float32), so that a frame costs the same
-however long the stream is.  Encoder and decoder both hold yhat after every frame, so both can run it.
+however long the stream is.  Encoder and decoder both hold yhat after every frame, so both can run it.  It stands
+beside the codec: what it returns is for the caller, and the codec's own prior, entropy model and bitstream do not
+read it.
 
 ``python -m paper_2502_20762_amd.mixer`` codes a short synthetic sequence with random-init weights and runs the mixer
 beside the encoder.

@@ -6,8 +6,8 @@ value is computed in the HIP kernels.  They take float16 or bfloat16 tensors and
 contiguous) and raise :class:`ValueError` for tensors that do not fit together, :class:`NcodecError` for what the
 library refuses, outputs that overlap an input or each other among it (parts of one buffer may be given, and what a
 function says may be the same).  They have no backward pass: a tensor that requires a gradient is refused where torch records
-gradients, and taken under ``torch.no_grad()``.  :class:`TokenMixer` runs them together: the layer of a temporal
-prior that reads the latents of all earlier frames through a state of fixed size.
+gradients, and taken under ``torch.no_grad()``.  :class:`TokenMixer` runs them together: a layer
+that reads the latents of all earlier frames through a state of fixed size.
 """
 from __future__ import annotations
 
