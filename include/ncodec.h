@@ -544,6 +544,122 @@ ncodec_status ncodec_decay_attention(const ncodec_decay_shape* shape, const void
                                      float* d_state_out, void* d_o, void* d_workspace, size_t ws_bytes,
                                      void* hip_stream);
 
+/* Softmax attention over the sequences of a batch, each token seeing tokens up
+ * to itself: all of them (window = 0), or the latest `window` (itself among
+ * them) and the first `sinks`, which stay visible,
+ *   A(i) = { j <= i : window = 0 or i - j < window or j < sinks },
+ *   o_i = sum_{j in A(i)} p_ij v_j,  p_ij = exp(s_ij) / sum_{j in A(i)} exp(s_ij),
+ *   s_ij = scale * q_i . k_j.
+ * q: batch x tokens x heads x head_dim, k and v: batch x tokens x kv_heads x
+ * head_dim (value_dim), o: batch x tokens x heads x value_dim, each at its batch,
+ * token and head strides, the last dimension contiguous.  Query head h reads key
+ * head h / (heads / kv_heads).  d_lengths: batch int32, the tokens of each
+ * sequence, clamped to [0, tokens]; NULL: all.  Past its length a sequence's inputs
+ * are not used and its outputs are zero.  Scores, weights and sums are fp32 up to
+ * the one rounding of o; scores have to be in the range of fp32.  A NaN or an
+ * infinity reaches the tokens that see it and no other; where the formula has an
+ * infinity, either of the two may stand.
+ * head_dim and value_dim in [1, 128], heads and kv_heads in [1, 4096],
+ * batch * heads < 2^24, tokens, window and sinks in [0, 2^31). */
+typedef struct {
+  int32_t dtype;
+  int32_t heads, kv_heads, head_dim, value_dim;
+  float scale;
+  int64_t batch, tokens, window, sinks;
+  int64_t q_batch_stride, q_token_stride, q_head_stride;
+  int64_t k_batch_stride, k_token_stride, k_head_stride;
+  int64_t v_batch_stride, v_token_stride, v_head_stride;
+  int64_t o_batch_stride, o_token_stride, o_head_stride;
+} ncodec_window_shape;
+
+ncodec_status ncodec_window_attention(const ncodec_window_shape* shape, const void* d_q, const void* d_k,
+                                      const void* d_v, const int32_t* d_lengths, void* d_o, void* hip_stream);
+
+/* A cache of keys and values in pages: k pages x page_size x kv_heads x head_dim,
+ * v pages x page_size x kv_heads x value_dim, each at its page, token and head
+ * strides, the last dimension contiguous.  Position j of a sequence is row
+ * j % page_size of page table[j / page_size], where `table` is the sequence's row
+ * of a table of int32 page numbers (batch x columns, rows table_stride apart); it
+ * holds columns * page_size positions.  A number outside [0, pages) is no page:
+ * positions on it are neither read nor written.  Sequences may share pages that are
+ * only read.  Rows that a call writes have to be different ones.
+ * page_size: a power of two up to 4096; kv_heads in [1, 4096], head_dim and
+ * value_dim in [1, 128], pages in [0, 2^31), columns * page_size below 2^31. */
+typedef struct {
+  int32_t dtype;
+  int32_t kv_heads, head_dim, value_dim;
+  int32_t page_size;
+  int32_t reserved; /* 0 */
+  int64_t pages;
+  int64_t k_page_stride, k_token_stride, k_head_stride;
+  int64_t v_page_stride, v_token_stride, v_head_stride;
+} ncodec_cache_shape;
+
+/* Softmax attention of the last token of each sequence over its cached keys and
+ * values: position i = n - 1 of the formula above, n = d_lengths[b] clamped to
+ * [0, columns * page_size], its own key and value in the cache already.  q: batch x
+ * heads x head_dim, o: batch x heads x value_dim at their batch and head strides.
+ * Nothing seen (n = 0, or no page under it): o is zero.
+ * d_mass (or NULL): batch x kv_heads x (columns * page_size) float32, contiguous; the
+ * weights that the heads of a key head give a position are added to its entry, the
+ * entries of positions that are not seen stay as they are.
+ * Limits as above; heads a multiple of kv_heads, at most 4096. */
+typedef struct {
+  int32_t heads;
+  float scale;
+  int64_t batch, columns, table_stride, window, sinks;
+  int64_t q_batch_stride, q_head_stride;
+  int64_t o_batch_stride, o_head_stride;
+} ncodec_paged_shape;
+
+/* Bytes of workspace (256-byte aligned device memory) that the call needs, with
+ * d_mass (mass = 1) or without; 0 for invalid shapes too.  Its content matters to no
+ * later call.  Pure host function. */
+size_t ncodec_paged_attention_workspace_bytes(const ncodec_cache_shape* cache, const ncodec_paged_shape* shape,
+                                              int32_t mass);
+
+ncodec_status ncodec_paged_attention(const ncodec_cache_shape* cache, const ncodec_paged_shape* shape, const void* d_q,
+                                     const void* d_k_cache, const void* d_v_cache, const int32_t* d_table,
+                                     const int32_t* d_lengths, float* d_mass, void* d_o, void* d_workspace,
+                                     size_t ws_bytes, void* hip_stream);
+
+/* Writes keys and values of new tokens into the cache: token i of sequence b, i <
+ * d_counts[b] (clamped to [0, tokens]; NULL: all), goes to position d_starts[b] + i;
+ * what falls outside [0, columns * page_size) goes nowhere.  k: batch x tokens x
+ * kv_heads x head_dim, v likewise, at their batch, token and head strides.  d_mass (or
+ * NULL), as above: the entries of the positions become 0. */
+typedef struct {
+  int64_t batch, tokens, columns, table_stride;
+  int64_t k_batch_stride, k_token_stride, k_head_stride;
+  int64_t v_batch_stride, v_token_stride, v_head_stride;
+} ncodec_append_shape;
+
+ncodec_status ncodec_cache_append(const ncodec_cache_shape* cache, const ncodec_append_shape* shape, const void* d_k,
+                                  const void* d_v, void* d_k_cache, void* d_v_cache, const int32_t* d_table,
+                                  const int32_t* d_starts, const int32_t* d_counts, float* d_mass, void* hip_stream);
+
+/* Cuts each sequence back to its `keep` heaviest tokens, key head by key head, and
+ * copies their rows, in their order, to positions 0 .. of the pages of a new table.
+ * Kept are, of the n = d_lengths[b] (clamped to [0, columns * page_size]) positions,
+ * the first `sinks` and the latest `recent`, and of the others those with the largest
+ * d_mass, a NaN counting as above all numbers and of equals the earlier; all of them
+ * where n <= keep.  d_new_lengths: batch int32, min(n, keep).  d_new_mass: batch x
+ * kv_heads x (new_columns * page_size) float32, the mass of the kept tokens and 0 past
+ * them.  d_kept: batch x kv_heads x keep int32, their old positions, and -1 past them.
+ * The pages of the new table are none of the old one's; rows of theirs past the kept
+ * ones stay as they are, and so do rows whose old position has no page.
+ * keep in [1, new_columns * page_size], sinks + recent <= keep, sinks, recent >= 0,
+ * batch * kv_heads < 2^24. */
+typedef struct {
+  int64_t batch, columns, table_stride, new_columns, new_table_stride;
+  int64_t keep, sinks, recent;
+} ncodec_evict_shape;
+
+ncodec_status ncodec_cache_evict(const ncodec_cache_shape* cache, const ncodec_evict_shape* shape, void* d_k_cache,
+                                 void* d_v_cache, const int32_t* d_table, const int32_t* d_lengths, const float* d_mass,
+                                 const int32_t* d_new_table, int32_t* d_new_lengths, float* d_new_mass,
+                                 int32_t* d_kept, void* hip_stream);
+
 /* Message for the last error on ctx (or the last create failure if ctx is NULL). */
 const char* ncodec_last_error(const ncodec_ctx* ctx);
 

@@ -97,6 +97,113 @@ const char* decay_fault(const ncodec_decay_shape& s, ncodec_status* st) {
   return nullptr;
 }
 
+const char* heads_fault(int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t value_dim) {
+  if (heads < 1 || heads > 4096 || kv_heads < 1 || kv_heads > 4096) return "heads must be in [1, 4096]";
+  if (heads % kv_heads) return "heads must be a multiple of kv_heads";
+  if (head_dim < 1 || head_dim > 128 || value_dim < 1 || value_dim > 128)
+    return "head_dim and value_dim must be in [1, 128]";
+  return nullptr;
+}
+
+bool finite(float f) { return f > -__builtin_huge_valf() && f < __builtin_huge_valf(); }
+
+const char* window_fault(const ncodec_window_shape& s, ncodec_status* st) {
+  *st = NCODEC_EINVAL;
+  if (!dtype_ok(s.dtype)) return "dtype is not an ncodec_dtype";
+  if (!finite(s.scale)) return "scale must be finite";
+  *st = NCODEC_ESHAPE;
+  if (s.tokens < 0 || s.tokens >= kMaxRows) return "tokens must be in [0, 2^31)";
+  if (s.window < 0 || s.window >= kMaxRows || s.sinks < 0 || s.sinks >= kMaxRows)
+    return "window and sinks must be in [0, 2^31)";
+  if (const char* why = heads_fault(s.heads, s.kv_heads, s.head_dim, s.value_dim)) return why;
+  if (s.batch < 0 || s.batch >= (1 << 24) || s.batch * s.heads >= (1 << 24)) return "batch * heads must be below 2^24";
+  const int64_t strides[12] = {s.q_batch_stride, s.q_token_stride, s.q_head_stride, s.k_batch_stride,
+                               s.k_token_stride, s.k_head_stride,  s.v_batch_stride, s.v_token_stride,
+                               s.v_head_stride,  s.o_batch_stride, s.o_token_stride, s.o_head_stride};
+  for (int64_t v : strides)
+    if (!stride_ok(v)) return "a stride is negative or above 2^40";
+  if ((s.batch > 1 && s.o_batch_stride < s.value_dim) || (s.tokens > 1 && s.o_token_stride < s.value_dim) ||
+      (s.heads > 1 && s.o_head_stride < s.value_dim))
+    return "an output stride is below value_dim";
+  return nullptr;
+}
+
+// `written`: rows of the cache have to be different ones.
+const char* cache_fault(const ncodec_cache_shape& c, bool written, ncodec_status* st) {
+  *st = NCODEC_EINVAL;
+  if (!dtype_ok(c.dtype)) return "dtype is not an ncodec_dtype";
+  if (c.reserved) return "reserved must be 0";
+  *st = NCODEC_ESHAPE;
+  if (const char* why = heads_fault(c.kv_heads, c.kv_heads, c.head_dim, c.value_dim)) return why;
+  if (c.page_size < 1 || c.page_size > 4096 || (c.page_size & (c.page_size - 1)))
+    return "page_size must be a power of two up to 4096";
+  if (c.pages < 0 || c.pages >= kMaxRows) return "pages must be in [0, 2^31)";
+  const int64_t strides[6] = {c.k_page_stride, c.k_token_stride, c.k_head_stride,
+                              c.v_page_stride, c.v_token_stride, c.v_head_stride};
+  for (int64_t v : strides)
+    if (!stride_ok(v)) return "a stride is negative or above 2^40";
+  for (int i = 0; written && i < 6; ++i) {
+    const int64_t count = i % 3 == 0 ? c.pages : i % 3 == 1 ? c.page_size : c.kv_heads;
+    if (count > 1 && strides[i] < (i < 3 ? c.head_dim : c.value_dim)) return "a stride of the cache is below its row";
+  }
+  return nullptr;
+}
+
+const char* table_fault(const ncodec_cache_shape& c, int64_t batch, int64_t columns, int64_t stride) {
+  if (batch < 0 || batch >= (1 << 24) || batch * c.kv_heads >= (1 << 24)) return "batch * heads must be below 2^24";
+  if (columns < 0 || columns >= kMaxRows || columns * c.page_size >= kMaxRows) return "columns * page_size must be in [0, 2^31)";
+  if (!stride_ok(stride)) return "a stride is negative or above 2^40";
+  return nullptr;
+}
+
+const char* paged_fault(const ncodec_cache_shape& c, const ncodec_paged_shape& s, ncodec_status* st) {
+  if (const char* why = cache_fault(c, false, st)) return why;
+  *st = NCODEC_EINVAL;
+  if (!finite(s.scale)) return "scale must be finite";
+  *st = NCODEC_ESHAPE;
+  if (const char* why = heads_fault(s.heads, c.kv_heads, c.head_dim, c.value_dim)) return why;
+  if (s.window < 0 || s.window >= kMaxRows || s.sinks < 0 || s.sinks >= kMaxRows)
+    return "window and sinks must be in [0, 2^31)";
+  if (const char* why = table_fault(c, s.batch, s.columns, s.table_stride)) return why;
+  if (s.batch * s.heads >= (1 << 24)) return "batch * heads must be below 2^24";
+  if (!stride_ok(s.q_batch_stride) || !stride_ok(s.q_head_stride) || !stride_ok(s.o_batch_stride) || !stride_ok(s.o_head_stride))
+    return "a stride is negative or above 2^40";
+  if ((s.batch > 1 && s.o_batch_stride < c.value_dim) || (s.heads > 1 && s.o_head_stride < c.value_dim))
+    return "an output stride is below value_dim";
+  return nullptr;
+}
+
+const char* append_fault(const ncodec_cache_shape& c, const ncodec_append_shape& s, ncodec_status* st) {
+  if (const char* why = cache_fault(c, true, st)) return why;
+  if (const char* why = table_fault(c, s.batch, s.columns, s.table_stride)) return why;
+  if (s.tokens < 0 || s.tokens >= kMaxRows) return "tokens must be in [0, 2^31)";
+  const int64_t strides[6] = {s.k_batch_stride, s.k_token_stride, s.k_head_stride,
+                              s.v_batch_stride, s.v_token_stride, s.v_head_stride};
+  for (int64_t v : strides)
+    if (!stride_ok(v)) return "a stride is negative or above 2^40";
+  return nullptr;
+}
+
+const char* evict_fault(const ncodec_cache_shape& c, const ncodec_evict_shape& s, ncodec_status* st) {
+  if (const char* why = cache_fault(c, true, st)) return why;
+  if (const char* why = table_fault(c, s.batch, s.columns, s.table_stride)) return why;
+  if (const char* why = table_fault(c, s.batch, s.new_columns, s.new_table_stride)) return why;
+  if (s.keep < 1 || s.keep > s.new_columns * c.page_size) return "keep must be in [1, new_columns * page_size]";
+  if (s.sinks < 0 || s.recent < 0 || s.sinks > s.keep || s.recent > s.keep - s.sinks)
+    return "sinks + recent must be in [0, keep]";
+  return nullptr;
+}
+
+Area table_area(const int32_t* d, int64_t batch, int64_t columns, int64_t stride) {
+  return Area(d, 2 * columns, {batch, 2 * stride});  // in 16-bit units, as all strided operands
+}
+Area k_area(const ncodec_cache_shape& c, const void* d) {
+  return Area(d, c.head_dim, {c.pages, c.k_page_stride, c.page_size, c.k_token_stride, c.kv_heads, c.k_head_stride});
+}
+Area v_area(const ncodec_cache_shape& c, const void* d) {
+  return Area(d, c.value_dim, {c.pages, c.v_page_stride, c.page_size, c.v_token_stride, c.kv_heads, c.v_head_stride});
+}
+
 }  // namespace
 
 extern "C" ncodec_status ncodec_linear(const ncodec_linear_shape* shape, const void* d_x, const void* d_w,
@@ -200,4 +307,129 @@ extern "C" ncodec_status ncodec_decay_attention(const ncodec_decay_shape* shape,
                                             d_o, d_workspace},
                                            (hipStream_t)hip_stream),
                 "decay_attention");
+}
+
+extern "C" ncodec_status ncodec_window_attention(const ncodec_window_shape* shape, const void* d_q, const void* d_k,
+                                                 const void* d_v, const int32_t* d_lengths, void* d_o,
+                                                 void* hip_stream) {
+  if (!shape) return set_error(NCODEC_EINVAL, "window_attention", "shape is NULL");
+  ncodec_status st;
+  if (const char* why = window_fault(*shape, &st)) return set_error(st, "window_attention", why);
+  if (shape->batch == 0 || shape->tokens == 0) return NCODEC_OK;
+  if (!d_q || !d_k || !d_v || !d_o)
+    return set_error(NCODEC_EINVAL, "window_attention", "d_q, d_k, d_v and d_o must be non-NULL");
+  if (!aligned(d_q, 2) || !aligned(d_k, 2) || !aligned(d_v, 2) || !aligned(d_o, 2) || !aligned(d_lengths, 4))
+    return set_error(NCODEC_EINVAL, "window_attention", "a pointer is not aligned to an element");
+  {
+    const ncodec_window_shape& s = *shape;
+    const Area q(d_q, s.head_dim, {s.batch, s.q_batch_stride, s.tokens, s.q_token_stride, s.heads, s.q_head_stride}),
+        k(d_k, s.head_dim, {s.batch, s.k_batch_stride, s.tokens, s.k_token_stride, s.kv_heads, s.k_head_stride}),
+        v(d_v, s.value_dim, {s.batch, s.v_batch_stride, s.tokens, s.v_token_stride, s.kv_heads, s.v_head_stride}),
+        o(d_o, s.value_dim, {s.batch, s.o_batch_stride, s.tokens, s.o_token_stride, s.heads, s.o_head_stride});
+    if (!all_apart(o, {q, k, v, Area(d_lengths, s.batch, 4)}))
+      return set_error(NCODEC_EINVAL, "window_attention", "d_o overlaps an input");
+  }
+  return finish(nc::launch_window_attention({*shape, d_q, d_k, d_v, d_lengths, d_o}, (hipStream_t)hip_stream),
+                "window_attention");
+}
+
+extern "C" size_t ncodec_paged_attention_workspace_bytes(const ncodec_cache_shape* cache,
+                                                         const ncodec_paged_shape* shape, int32_t mass) {
+  ncodec_status st;
+  if (!cache || !shape || paged_fault(*cache, *shape, &st)) return 0;
+  return nc::paged_workspace_bytes(*cache, *shape, mass != 0);
+}
+
+extern "C" ncodec_status ncodec_paged_attention(const ncodec_cache_shape* cache, const ncodec_paged_shape* shape,
+                                                const void* d_q, const void* d_k_cache, const void* d_v_cache,
+                                                const int32_t* d_table, const int32_t* d_lengths, float* d_mass,
+                                                void* d_o, void* d_workspace, size_t ws_bytes, void* hip_stream) {
+  if (!cache || !shape) return set_error(NCODEC_EINVAL, "paged_attention", "a shape is NULL");
+  ncodec_status st;
+  if (const char* why = paged_fault(*cache, *shape, &st)) return set_error(st, "paged_attention", why);
+  if (shape->batch == 0) return NCODEC_OK;
+  const ncodec_cache_shape& c = *cache;
+  const ncodec_paged_shape& s = *shape;
+  if (!d_q || !d_o || !d_lengths || (s.columns && !d_table) || (c.pages && (!d_k_cache || !d_v_cache)))
+    return set_error(NCODEC_EINVAL, "paged_attention", "d_q, the cache, d_table, d_lengths and d_o must be non-NULL");
+  if (!aligned(d_q, 2) || !aligned(d_k_cache, 2) || !aligned(d_v_cache, 2) || !aligned(d_o, 2) || !aligned(d_table, 4) ||
+      !aligned(d_lengths, 4) || !aligned(d_mass, 4))
+    return set_error(NCODEC_EINVAL, "paged_attention", "a pointer is not aligned to an element");
+  const size_t need = nc::paged_workspace_bytes(c, s, d_mass != nullptr);
+  if (need && (!d_workspace || ws_bytes < need || !aligned(d_workspace, 256)))
+    return set_error(NCODEC_ENOMEM, "paged_attention", "the workspace must be 256-byte aligned and hold ", need);
+  const Area q(d_q, c.head_dim, {s.batch, s.q_batch_stride, s.heads, s.q_head_stride}),
+      o(d_o, c.value_dim, {s.batch, s.o_batch_stride, s.heads, s.o_head_stride}), k = k_area(c, d_k_cache),
+      v = v_area(c, d_v_cache), table = table_area(d_table, s.batch, s.columns, s.table_stride),
+      lengths(d_lengths, s.batch, 4), mass(d_mass, s.batch * c.kv_heads * s.columns * c.page_size, 4);
+  if (!all_apart(o, {q, k, v, table, lengths, mass}) || !all_apart(mass, {q, k, v, table, lengths}))
+    return set_error(NCODEC_EINVAL, "paged_attention", "an output overlaps an input or the other output");
+  return finish(nc::launch_paged_attention({c, s, d_q, d_k_cache, d_v_cache, d_table, d_lengths, d_mass, d_o, d_workspace},
+                                           (hipStream_t)hip_stream),
+                "paged_attention");
+}
+
+extern "C" ncodec_status ncodec_cache_append(const ncodec_cache_shape* cache, const ncodec_append_shape* shape,
+                                             const void* d_k, const void* d_v, void* d_k_cache, void* d_v_cache,
+                                             const int32_t* d_table, const int32_t* d_starts, const int32_t* d_counts,
+                                             float* d_mass, void* hip_stream) {
+  if (!cache || !shape) return set_error(NCODEC_EINVAL, "cache_append", "a shape is NULL");
+  ncodec_status st;
+  if (const char* why = append_fault(*cache, *shape, &st)) return set_error(st, "cache_append", why);
+  const ncodec_cache_shape& c = *cache;
+  const ncodec_append_shape& s = *shape;
+  if (s.batch == 0 || s.tokens == 0 || s.columns == 0 || c.pages == 0) return NCODEC_OK;
+  if (!d_k || !d_v || !d_k_cache || !d_v_cache || !d_table || !d_starts)
+    return set_error(NCODEC_EINVAL, "cache_append", "d_k, d_v, the cache, d_table and d_starts must be non-NULL");
+  if (!aligned(d_k, 2) || !aligned(d_v, 2) || !aligned(d_k_cache, 2) || !aligned(d_v_cache, 2) || !aligned(d_table, 4) ||
+      !aligned(d_starts, 4) || !aligned(d_counts, 4) || !aligned(d_mass, 4))
+    return set_error(NCODEC_EINVAL, "cache_append", "a pointer is not aligned to an element");
+  const Area k(d_k, c.head_dim, {s.batch, s.k_batch_stride, s.tokens, s.k_token_stride, c.kv_heads, s.k_head_stride}),
+      v(d_v, c.value_dim, {s.batch, s.v_batch_stride, s.tokens, s.v_token_stride, c.kv_heads, s.v_head_stride}),
+      kc = k_area(c, d_k_cache), vc = v_area(c, d_v_cache),
+      table = table_area(d_table, s.batch, s.columns, s.table_stride), starts(d_starts, s.batch, 4),
+      counts(d_counts, s.batch, 4), mass(d_mass, s.batch * c.kv_heads * s.columns * c.page_size, 4);
+  if (!all_apart(kc, {k, v, vc, table, starts, counts, mass}) || !all_apart(vc, {k, v, table, starts, counts, mass}) ||
+      !all_apart(mass, {k, v, table, starts, counts}))
+    return set_error(NCODEC_EINVAL, "cache_append", "an output overlaps an input or another output");
+  return finish(nc::launch_cache_append({c, s, d_k, d_v, d_k_cache, d_v_cache, d_table, d_starts, d_counts, d_mass},
+                                        (hipStream_t)hip_stream),
+                "cache_append");
+}
+
+extern "C" ncodec_status ncodec_cache_evict(const ncodec_cache_shape* cache, const ncodec_evict_shape* shape,
+                                            void* d_k_cache, void* d_v_cache, const int32_t* d_table,
+                                            const int32_t* d_lengths, const float* d_mass, const int32_t* d_new_table,
+                                            int32_t* d_new_lengths, float* d_new_mass, int32_t* d_kept,
+                                            void* hip_stream) {
+  if (!cache || !shape) return set_error(NCODEC_EINVAL, "cache_evict", "a shape is NULL");
+  ncodec_status st;
+  if (const char* why = evict_fault(*cache, *shape, &st)) return set_error(st, "cache_evict", why);
+  const ncodec_cache_shape& c = *cache;
+  const ncodec_evict_shape& s = *shape;
+  if (s.batch == 0) return NCODEC_OK;
+  if ((c.pages && (!d_k_cache || !d_v_cache)) || (s.columns && (!d_table || !d_mass)) || !d_lengths || !d_new_table ||
+      !d_new_lengths || !d_new_mass || !d_kept)
+    return set_error(NCODEC_EINVAL, "cache_evict", "the cache, the tables, d_lengths, d_mass and the outputs must be non-NULL");
+  if (!aligned(d_k_cache, 2) || !aligned(d_v_cache, 2) || !aligned(d_table, 4) || !aligned(d_lengths, 4) ||
+      !aligned(d_mass, 4) || !aligned(d_new_table, 4) || !aligned(d_new_lengths, 4) || !aligned(d_new_mass, 4) ||
+      !aligned(d_kept, 4))
+    return set_error(NCODEC_EINVAL, "cache_evict", "a pointer is not aligned to an element");
+  const int64_t bk = s.batch * c.kv_heads;
+  const Area kc = k_area(c, d_k_cache), vc = v_area(c, d_v_cache),
+             table = table_area(d_table, s.batch, s.columns, s.table_stride),
+             new_table = table_area(d_new_table, s.batch, s.new_columns, s.new_table_stride),
+             lengths(d_lengths, s.batch, 4), mass(d_mass, bk * s.columns * c.page_size, 4),
+             new_lengths(d_new_lengths, s.batch, 4), new_mass(d_new_mass, bk * s.new_columns * c.page_size, 4),
+             kept(d_kept, bk * s.keep, 4);
+  if (!all_apart(kc, {vc, table, new_table, lengths, mass, new_lengths, new_mass, kept}) ||
+      !all_apart(vc, {table, new_table, lengths, mass, new_lengths, new_mass, kept}) ||
+      !all_apart(new_lengths, {table, new_table, lengths, mass, new_mass, kept}) ||
+      !all_apart(new_mass, {table, new_table, lengths, mass, kept}) ||
+      !all_apart(kept, {table, new_table, lengths, mass}))
+    return set_error(NCODEC_EINVAL, "cache_evict", "an output overlaps an input or another output");
+  return finish(nc::launch_cache_evict({c, s, d_k_cache, d_v_cache, d_table, d_lengths, d_mass, d_new_table,
+                                        d_new_lengths, d_new_mass, d_kept},
+                                       (hipStream_t)hip_stream),
+                "cache_evict");
 }

@@ -1,5 +1,6 @@
 // Shared by the token operators (matrix product with epilogue, head norms with
-// rotation, attention with a decay): element types and the launch interface.
+// rotation, attention with a decay, with a window and over a cache, and the cache's
+// upkeep): element types and the launch interface.
 #pragma once
 #include "common.hpp"
 #include "internal.hpp"
@@ -69,5 +70,59 @@ struct DecayArgs {
 };
 size_t decay_workspace_bytes(const ncodec_decay_shape& s);
 hipError_t launch_decay_attention(const DecayArgs& a, hipStream_t st);
+
+struct WindowArgs {
+  ncodec_window_shape s;
+  const void* q;
+  const void* k;
+  const void* v;
+  const int32_t* lengths;
+  void* o;
+};
+hipError_t launch_window_attention(const WindowArgs& a, hipStream_t st);
+
+struct PagedArgs {
+  ncodec_cache_shape c;
+  ncodec_paged_shape s;
+  const void* q;
+  const void* k;
+  const void* v;
+  const int32_t* table;
+  const int32_t* lengths;
+  float* mass;
+  void* o;
+  void* ws;
+};
+size_t paged_workspace_bytes(const ncodec_cache_shape& c, const ncodec_paged_shape& s, bool mass);
+hipError_t launch_paged_attention(const PagedArgs& a, hipStream_t st);
+
+struct AppendArgs {
+  ncodec_cache_shape c;
+  ncodec_append_shape s;
+  const void* k;
+  const void* v;
+  void* k_cache;
+  void* v_cache;
+  const int32_t* table;
+  const int32_t* starts;
+  const int32_t* counts;
+  float* mass;
+};
+hipError_t launch_cache_append(const AppendArgs& a, hipStream_t st);
+
+struct EvictArgs {
+  ncodec_cache_shape c;
+  ncodec_evict_shape s;
+  void* k_cache;
+  void* v_cache;
+  const int32_t* table;
+  const int32_t* lengths;
+  const float* mass;
+  const int32_t* new_table;
+  int32_t* new_lengths;
+  float* new_mass;
+  int32_t* kept;
+};
+hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st);
 
 }  // namespace nc

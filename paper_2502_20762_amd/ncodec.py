@@ -79,6 +79,40 @@ class ncodec_decay_shape(ctypes.Structure):
                     "o_batch_stride", "o_token_stride", "o_head_stride")])
 
 
+class ncodec_window_shape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "heads", "kv_heads", "head_dim", "value_dim")]
+                + [("scale", ctypes.c_float)]
+                + [(n, ctypes.c_int64) for n in (
+                    "batch", "tokens", "window", "sinks", "q_batch_stride", "q_token_stride", "q_head_stride",
+                    "k_batch_stride", "k_token_stride", "k_head_stride", "v_batch_stride", "v_token_stride",
+                    "v_head_stride", "o_batch_stride", "o_token_stride", "o_head_stride")])
+
+
+class ncodec_cache_shape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "kv_heads", "head_dim", "value_dim", "page_size", "reserved")]
+                + [(n, ctypes.c_int64) for n in (
+                    "pages", "k_page_stride", "k_token_stride", "k_head_stride", "v_page_stride", "v_token_stride",
+                    "v_head_stride")])
+
+
+class ncodec_paged_shape(ctypes.Structure):
+    _fields_ = ([("heads", ctypes.c_int32), ("scale", ctypes.c_float)]
+                + [(n, ctypes.c_int64) for n in (
+                    "batch", "columns", "table_stride", "window", "sinks", "q_batch_stride", "q_head_stride",
+                    "o_batch_stride", "o_head_stride")])
+
+
+class ncodec_append_shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in (
+        "batch", "tokens", "columns", "table_stride", "k_batch_stride", "k_token_stride", "k_head_stride",
+        "v_batch_stride", "v_token_stride", "v_head_stride")]
+
+
+class ncodec_evict_shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in (
+        "batch", "columns", "table_stride", "new_columns", "new_table_stride", "keep", "sinks", "recent")]
+
+
 class NcodecError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"ncodec status {status}: {message}")
@@ -120,6 +154,15 @@ _SIGNATURES = {
     "ncodec_decay_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(ncodec_decay_shape)]),
     "ncodec_decay_attention": (ctypes.c_int, [ctypes.POINTER(ncodec_decay_shape)] + [_P] * 9
                                + [ctypes.c_size_t, _P]),
+    "ncodec_window_attention": (ctypes.c_int, [ctypes.POINTER(ncodec_window_shape)] + [_P] * 6),
+    "ncodec_paged_attention_workspace_bytes": (ctypes.c_size_t, [
+        ctypes.POINTER(ncodec_cache_shape), ctypes.POINTER(ncodec_paged_shape), ctypes.c_int32]),
+    "ncodec_paged_attention": (ctypes.c_int, [ctypes.POINTER(ncodec_cache_shape), ctypes.POINTER(ncodec_paged_shape)]
+                               + [_P] * 8 + [ctypes.c_size_t, _P]),
+    "ncodec_cache_append": (ctypes.c_int, [ctypes.POINTER(ncodec_cache_shape), ctypes.POINTER(ncodec_append_shape)]
+                            + [_P] * 9),
+    "ncodec_cache_evict": (ctypes.c_int, [ctypes.POINTER(ncodec_cache_shape), ctypes.POINTER(ncodec_evict_shape)]
+                           + [_P] * 10),
     "ncodec_last_error": (ctypes.c_char_p, [_P]),
     "ncodec_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "ncodec_destroy": (None, [_P]),
@@ -309,6 +352,40 @@ def ncodec_decay_attention(shape: ncodec_decay_shape, d_q: int, d_k: int, d_v: i
     _check(load_library().ncodec_decay_attention(ctypes.byref(shape), _p(d_q), _p(d_k), _p(d_v), _p(d_log_decay),
                                                  _p(d_lengths), _p(d_state_in), _p(d_state_out), _p(d_o),
                                                  _p(d_workspace), ws_bytes, stream or None))
+
+
+def ncodec_window_attention(shape: ncodec_window_shape, d_q: int, d_k: int, d_v: int, d_lengths: int, d_o: int,
+                            stream: int = 0) -> None:
+    _check(load_library().ncodec_window_attention(ctypes.byref(shape), _p(d_q), _p(d_k), _p(d_v), _p(d_lengths),
+                                                  _p(d_o), stream or None))
+
+
+def ncodec_paged_attention_workspace_bytes(cache: ncodec_cache_shape, shape: ncodec_paged_shape, mass: int = 0) -> int:
+    return int(load_library().ncodec_paged_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(shape), mass))
+
+
+def ncodec_paged_attention(cache: ncodec_cache_shape, shape: ncodec_paged_shape, d_q: int, d_k_cache: int,
+                           d_v_cache: int, d_table: int, d_lengths: int, d_mass: int, d_o: int, d_workspace: int = 0,
+                           ws_bytes: int = 0, stream: int = 0) -> None:
+    _check(load_library().ncodec_paged_attention(ctypes.byref(cache), ctypes.byref(shape), _p(d_q), _p(d_k_cache),
+                                                 _p(d_v_cache), _p(d_table), _p(d_lengths), _p(d_mass), _p(d_o),
+                                                 _p(d_workspace), ws_bytes, stream or None))
+
+
+def ncodec_cache_append(cache: ncodec_cache_shape, shape: ncodec_append_shape, d_k: int, d_v: int, d_k_cache: int,
+                        d_v_cache: int, d_table: int, d_starts: int, d_counts: int = 0, d_mass: int = 0,
+                        stream: int = 0) -> None:
+    _check(load_library().ncodec_cache_append(ctypes.byref(cache), ctypes.byref(shape), _p(d_k), _p(d_v),
+                                              _p(d_k_cache), _p(d_v_cache), _p(d_table), _p(d_starts), _p(d_counts),
+                                              _p(d_mass), stream or None))
+
+
+def ncodec_cache_evict(cache: ncodec_cache_shape, shape: ncodec_evict_shape, d_k_cache: int, d_v_cache: int,
+                       d_table: int, d_lengths: int, d_mass: int, d_new_table: int, d_new_lengths: int,
+                       d_new_mass: int, d_kept: int, stream: int = 0) -> None:
+    _check(load_library().ncodec_cache_evict(ctypes.byref(cache), ctypes.byref(shape), _p(d_k_cache), _p(d_v_cache),
+                                             _p(d_table), _p(d_lengths), _p(d_mass), _p(d_new_table),
+                                             _p(d_new_lengths), _p(d_new_mass), _p(d_kept), stream or None))
 
 
 def ncodec_last_error(ctx=None) -> str:

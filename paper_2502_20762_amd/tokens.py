@@ -1,6 +1,7 @@
-"""Token operators on torch tensors, and the mixer that they make.
+"""Token operators on torch tensors, and the mixers that they make.
 
-``linear``, ``qk_norm_rope`` and ``decay_attention`` check their arguments, allocate outputs and workspace with
+``linear``, ``qk_norm_rope``, ``decay_attention``, ``window_attention``, ``paged_attention``, ``cache_append`` and
+``cache_evict`` check their arguments, allocate outputs and workspace with
 torch and call the library's entry points of the same names on the current stream of the tensors' device; every
 value is computed in the HIP kernels.  They take float16 or bfloat16 tensors and strided views (the last dimension
 contiguous) and raise :class:`ValueError` for tensors that do not fit together, :class:`NcodecError` for what the
@@ -228,3 +229,159 @@ def decay_attention(q, k, v, log_decay, state=None, lengths=None, scale=None, re
     _call(lib.ncodec_decay_attention, device, ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(),
           _ptr(lengths), _ptr(state), _ptr(state_out), out.data_ptr(), _ptr(ws), need)
     return (out, state_out) if return_state else out
+
+
+def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None, out=None):
+    """Softmax attention over each sequence: token i sees the tokens j <= i with i - j < window (None: all) or j < sinks.
+
+    q: (batch, tokens, heads, dim), k: (batch, tokens, kv_heads, dim), v: (batch, tokens, kv_heads, value_dim),
+    lengths: (batch) int32 tokens of each sequence (None: all; past them outputs are zero), scale: default dim^-0.5.
+    Returns o (batch, tokens, heads, value_dim).  The prompt form of :func:`paged_attention`."""
+    dt = _dtype(q)
+    qs, ks, vs = q.shape, k.shape, v.shape
+    _need(len(qs) == 4 and len(ks) == 4 and len(vs) == 4, "q, k and v must be (batch, tokens, heads, dim)")
+    B, T, H, D = qs
+    hk, V = ks[2], vs[3]
+    _need(D >= 1, "q needs a head dimension")
+    dtype, device = q.dtype, q.get_device()
+    _like(q, dtype, device, qs, "q")
+    _like(k, dtype, device, (B, T, hk, D), "k")
+    _like(v, dtype, device, (B, T, hk, V), "v")
+    if lengths is not None:
+        _like(lengths, torch.int32, device, (B,), "lengths")
+    if out is None:
+        out = q.new_empty((B, T, H, V))
+    else:
+        _like(out, dtype, device, (B, T, H, V), "out")
+    shape = _nc.ncodec_window_shape(dt, H, hk, D, V, D ** -0.5 if scale is None else scale, B, T, _window(window), sinks,
+                                    *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *out.stride()[:3])
+    _call(_nc.load_library().ncodec_window_attention, device, ctypes.byref(shape), q.data_ptr(), k.data_ptr(),
+          v.data_ptr(), _ptr(lengths), out.data_ptr())
+    return out
+
+
+def _window(window):
+    if window is None:
+        return 0
+    _need(window >= 1, "a window holds the token itself at least (None: all tokens)")
+    return window
+
+
+def _cache(dtype, device, k_cache, v_cache):
+    """The descriptor of a cache; k_cache: (pages, page_size, kv_heads, dim), v_cache likewise."""
+    ks, vs = k_cache.shape, v_cache.shape
+    _need(len(ks) == 4 and len(vs) == 4, "k_cache and v_cache must be (pages, page_size, kv_heads, dim)")
+    _like(k_cache, dtype, device, ks, "k_cache")
+    _like(v_cache, dtype, device, (*ks[:3], vs[3]), "v_cache")
+    return _nc.ncodec_cache_shape(_DTYPES[dtype], ks[2], ks[3], vs[3], ks[1], 0, ks[0], *k_cache.stride()[:3],
+                                  *v_cache.stride()[:3])
+
+
+def _table(table, device, batch, what):
+    """Columns and row stride of a table of page numbers, (batch, columns) int32."""
+    shape = table.shape
+    _need(len(shape) == 2, f"{what} must be (batch, columns)")
+    _like(table, torch.int32, device, (batch, shape[1]), what)
+    return shape[1], table.stride(0)
+
+
+def _mass(mass, device, shape, what="mass"):
+    _like(mass, torch.float32, device, shape, what)
+    _need(mass.is_contiguous(), f"{what} must be contiguous")
+
+
+def paged_attention(q, k_cache, v_cache, page_table, lengths, window=None, sinks=0, scale=None, mass=None, out=None):
+    """Softmax attention of the last token of each sequence over its cached keys and values, the token's own among them.
+
+    q: (batch, heads, dim), k_cache: (pages, page_size, kv_heads, dim), v_cache: (pages, page_size, kv_heads,
+    value_dim), page_size a power of two; page_table: (batch, columns) int32, position j of a sequence is row
+    j % page_size of page page_table[b, j // page_size] (a number that is no page holds nothing); lengths: (batch)
+    int32 tokens in the cache.  window, sinks, scale: as in :func:`window_attention`.  mass: (batch, kv_heads, columns *
+    page_size) float32, to which the weights that the heads of each key head give to a position are added.  Returns o
+    (batch, heads, value_dim), zero for a sequence without tokens."""
+    dt = _dtype(q)
+    qs = q.shape
+    _need(len(qs) == 3, "q must be (batch, heads, dim)")
+    B, H, D = qs
+    _need(D >= 1, "q needs a head dimension")
+    dtype, device = q.dtype, q.get_device()
+    _like(q, dtype, device, qs, "q")
+    cache = _cache(dtype, device, k_cache, v_cache)
+    _need(cache.head_dim == D, "q and k_cache must have the same head dimension")
+    columns, table_stride = _table(page_table, device, B, "page_table")
+    _like(lengths, torch.int32, device, (B,), "lengths")
+    if mass is not None:
+        _mass(mass, device, (B, cache.kv_heads, columns * cache.page_size))
+    if out is None:
+        out = q.new_empty((B, H, cache.value_dim))
+    else:
+        _like(out, dtype, device, (B, H, cache.value_dim), "out")
+    shape = _nc.ncodec_paged_shape(H, D ** -0.5 if scale is None else scale, B, columns, table_stride, _window(window),
+                                   sinks, *q.stride()[:2], *out.stride()[:2])
+    lib = _nc.load_library()
+    cref, ref = ctypes.byref(cache), ctypes.byref(shape)
+    need = lib.ncodec_paged_attention_workspace_bytes(cref, ref, 0 if mass is None else 1)
+    ws = q.new_empty(need, dtype=torch.uint8) if need else None
+    _call(lib.ncodec_paged_attention, device, cref, ref, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+          page_table.data_ptr(), lengths.data_ptr(), _ptr(mass), out.data_ptr(), _ptr(ws), need)
+    return out
+
+
+def cache_append(k, v, k_cache, v_cache, page_table, starts, counts=None, mass=None):
+    """Writes keys and values of new tokens into the cache's pages: token i of sequence b to position starts[b] + i.
+
+    k: (batch, tokens, kv_heads, dim), v: (batch, tokens, kv_heads, value_dim); cache and page_table: as in
+    :func:`paged_attention`; starts: (batch) int32; counts: (batch) int32 tokens of each sequence (None: all).  Positions
+    outside the table, or on no page, are not written.  mass: its entries of the written positions become 0."""
+    _dtype(k)
+    ks, vs = k.shape, v.shape
+    _need(len(ks) == 4 and len(vs) == 4, "k and v must be (batch, tokens, kv_heads, dim)")
+    B, T = ks[:2]
+    dtype, device = k.dtype, k.get_device()
+    cache = _cache(dtype, device, k_cache, v_cache)
+    _like(k, dtype, device, (B, T, cache.kv_heads, cache.head_dim), "k")
+    _like(v, dtype, device, (B, T, cache.kv_heads, cache.value_dim), "v")
+    columns, table_stride = _table(page_table, device, B, "page_table")
+    _like(starts, torch.int32, device, (B,), "starts")
+    if counts is not None:
+        _like(counts, torch.int32, device, (B,), "counts")
+    if mass is not None:
+        _mass(mass, device, (B, cache.kv_heads, columns * cache.page_size))
+    shape = _nc.ncodec_append_shape(B, T, columns, table_stride, *k.stride()[:3], *v.stride()[:3])
+    _call(_nc.load_library().ncodec_cache_append, device, ctypes.byref(cache), ctypes.byref(shape), k.data_ptr(),
+          v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(), starts.data_ptr(), _ptr(counts),
+          _ptr(mass))
+
+
+def cache_evict(k_cache, v_cache, page_table, lengths, mass, keep, new_table, sinks=0, recent=0, out=None):
+    """Cuts each sequence back to the ``keep`` heaviest tokens of each key head, copied to the pages of ``new_table``.
+
+    Kept are the first ``sinks`` and the latest ``recent`` tokens and of the others those with the largest mass (a NaN
+    above all numbers, of equals the earlier), in their order.  Cache, page_table, lengths and mass: as in
+    :func:`paged_attention`; new_table: (batch, new_columns) int32, pages of the same cache that are none of the old
+    ones, room for ``keep`` tokens at least.  Returns (lengths, mass, kept): (batch) int32, (batch, kv_heads,
+    new_columns * page_size) float32, zero past the kept tokens, and their old positions, (batch, kv_heads, keep) int32,
+    -1 past them; ``out``: such a tuple to be written."""
+    _dtype(k_cache)
+    dtype, device = k_cache.dtype, k_cache.get_device()
+    cache = _cache(dtype, device, k_cache, v_cache)
+    _need(len(lengths.shape) == 1, "lengths must be (batch)")
+    B, = lengths.shape
+    _like(lengths, torch.int32, device, (B,), "lengths")
+    columns, table_stride = _table(page_table, device, B, "page_table")
+    new_columns, new_stride = _table(new_table, device, B, "new_table")
+    K, page = cache.kv_heads, cache.page_size
+    _mass(mass, device, (B, K, columns * page))
+    _need(1 <= keep <= new_columns * page, "new_table must have room for keep tokens, one at least")
+    if out is None:
+        out = (lengths.new_empty((B,)), mass.new_empty((B, K, new_columns * page)), lengths.new_empty((B, K, keep)))
+    new_lengths, new_mass, kept = out
+    _like(new_lengths, torch.int32, device, (B,), "out[0]")
+    _mass(new_mass, device, (B, K, new_columns * page), "out[1]")
+    _like(kept, torch.int32, device, (B, K, keep), "out[2]")
+    _need(kept.is_contiguous(), "out[2] must be contiguous")
+    shape = _nc.ncodec_evict_shape(B, columns, table_stride, new_columns, new_stride, keep, sinks, recent)
+    _call(_nc.load_library().ncodec_cache_evict, device, ctypes.byref(cache), ctypes.byref(shape), k_cache.data_ptr(),
+          v_cache.data_ptr(), page_table.data_ptr(), lengths.data_ptr(), mass.data_ptr(), new_table.data_ptr(),
+          new_lengths.data_ptr(), new_mass.data_ptr(), kept.data_ptr())
+    return out
