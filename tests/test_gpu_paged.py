@@ -194,6 +194,32 @@ def test_paged_token_whose_scores_are_all_minus_infinity_is_no_number():
     assert torch.isnan(o).all() and torch.isnan(mass[0, 0, :40]).all() and bool((mass[0, 0, 40:] == 0).all())
 
 
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("n", [40, 3000])
+def test_paged_stretches_of_nan_and_of_minus_infinity(n, dt):
+    # a stretch as long as a wave's or a workgroup's share of the cache, the rest with scores that are numbers
+    c = Cache(gen(6), 1, n, 16, 1, 64, 64, dt)
+    q = torch.ones((1, 1, 64), dtype=c.k.dtype, device=DEV)
+    t, page, row = c.table[0].long(), torch.arange(n, device=DEV) // 16, torch.arange(n, device=DEV) % 16
+    for a, b in ((0, 32), (n // 2, n), (0, n - 1), (n - 1, n)):
+        k = c.k.clone()
+        k[t[page[a:b]], row[a:b]] = NAN
+        assert torch.isnan(tk.paged_attention(q, k, c.v, c.table, i32([n]))).all(), (a, b)
+        k[t[page[a:b]], row[a:b]] = -INF
+        mass = torch.zeros((1, 1, c.columns), device=DEV)
+        o = tk.paged_attention(q, k, c.v, c.table, i32([n]), mass=mass)
+        want, mag, wm = paged_reference(q, Seen(c, k), i32([n]), None, 0, 0.125, mass * 0)
+        check(o, want, output_bound(want, mag, np.abs(f64(c.v)).max(), f64(q), f64(c.k), 0.125, 64, n, dt), (a, b))
+        assert bool((mass[0, 0, a:b] == 0).all()) and abs(float(mass.sum()) - 1) < 1e-4
+
+
+class Seen:
+    """A cache with other keys."""
+
+    def __init__(self, c, k):
+        self.k, self.v, self.table = k, c.v, c.table
+
+
 def test_paged_offsets_past_32_bits():
     ld = (1 << 27) + 64  # page 40 begins past 2^32 elements
     buf = torch.empty(41 * ld + 4096, dtype=torch.float16, device=DEV)
