@@ -560,7 +560,7 @@ ncodec_status ncodec_decay_attention(const ncodec_decay_shape* shape, const void
  * infinity reaches the tokens that see it and no other; where the formula has an
  * infinity, either of the two may stand.
  * head_dim and value_dim in [1, 128], heads and kv_heads in [1, 4096],
- * batch * heads < 2^24, tokens, window and sinks in [0, 2^31). */
+ * batch * heads < 2^24, tokens in [0, 2^30], window and sinks in [0, 2^31). */
 typedef struct {
   int32_t dtype;
   int32_t heads, kv_heads, head_dim, value_dim;
@@ -584,7 +584,7 @@ ncodec_status ncodec_window_attention(const ncodec_window_shape* shape, const vo
  * positions on it are neither read nor written.  Sequences may share pages that are
  * only read.  Rows that a call writes have to be different ones.
  * page_size: a power of two up to 4096; kv_heads in [1, 4096], head_dim and
- * value_dim in [1, 128], pages in [0, 2^31), columns * page_size below 2^31. */
+ * value_dim in [1, 128], pages in [0, 2^31), columns * page_size in [0, 2^30]. */
 typedef struct {
   int32_t dtype;
   int32_t kv_heads, head_dim, value_dim;

@@ -22,6 +22,7 @@ ncodec_status set_error(ncodec_status st, const char* where, const char* why, si
 
 constexpr int64_t kMaxRows = (int64_t)1 << 31;
 constexpr int64_t kMaxStride = (int64_t)1 << 40;
+constexpr int64_t kMaxPositions = (int64_t)1 << 30;  // of a sequence that softmax attention sees: 32-bit counts past its end
 
 bool dtype_ok(int32_t d) { return d == NCODEC_DTYPE_FP16 || d == NCODEC_DTYPE_BF16; }
 bool aligned(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
@@ -112,7 +113,7 @@ const char* window_fault(const ncodec_window_shape& s, ncodec_status* st) {
   if (!dtype_ok(s.dtype)) return "dtype is not an ncodec_dtype";
   if (!finite(s.scale)) return "scale must be finite";
   *st = NCODEC_ESHAPE;
-  if (s.tokens < 0 || s.tokens >= kMaxRows) return "tokens must be in [0, 2^31)";
+  if (s.tokens < 0 || s.tokens > kMaxPositions) return "tokens must be in [0, 2^30]";
   if (s.window < 0 || s.window >= kMaxRows || s.sinks < 0 || s.sinks >= kMaxRows)
     return "window and sinks must be in [0, 2^31)";
   if (const char* why = heads_fault(s.heads, s.kv_heads, s.head_dim, s.value_dim)) return why;
@@ -151,7 +152,8 @@ const char* cache_fault(const ncodec_cache_shape& c, bool written, ncodec_status
 
 const char* table_fault(const ncodec_cache_shape& c, int64_t batch, int64_t columns, int64_t stride) {
   if (batch < 0 || batch >= (1 << 24) || batch * c.kv_heads >= (1 << 24)) return "batch * heads must be below 2^24";
-  if (columns < 0 || columns >= kMaxRows || columns * c.page_size >= kMaxRows) return "columns * page_size must be in [0, 2^31)";
+  if (columns < 0 || columns > kMaxPositions || columns * c.page_size > kMaxPositions)
+    return "columns * page_size must be in [0, 2^30]";
   if (!stride_ok(stride)) return "a stride is negative or above 2^40";
   return nullptr;
 }

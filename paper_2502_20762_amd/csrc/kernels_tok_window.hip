@@ -1,72 +1,354 @@
 // Softmax attention with a sliding window and sinks over whole sequences:
 //   o_i = sum_j p_ij v_j over the tokens j that token i sees, p = softmax(scale q_i . k_j).
+//
+// One pass over the keys with a running maximum and sum.  Both products are MFMAs,
+// transposed: scores^T = K q^T with keys as rows and queries as columns, so that a lane
+// holds half of one query's scores and its maximum, sum and rescaling are the lane's own;
+// and outputs^T = V^T p^T, whose operand p the accumulators of the scores already are, in
+// the order of keys that a transposed read of V from LDS gives.
 #include <algorithm>
 
 #include "tok_attend.hpp"
+#include "tok_tiles.hpp"
 
 namespace nc {
 namespace {
 
-// One wave for a token and head: a lane scores a key at a time, a running maximum
-// and sum join the rounds of 64, then each lane sums two columns of v.
-template <class E>
-__global__ __launch_bounds__(256) void k_tok_window(WindowArgs a, int64_t items) {
+constexpr int kTile = 64;     // keys
+constexpr int kQueries = 32;  // of a wave
+constexpr int kWaves = 4;
+
+struct WindowRun {
+  WindowArgs a;
+  int64_t first;        // block of this launch's first workgroup
+  int head_waves;       // waves of a workgroup on different heads of a group; the others on further queries
+  int head_tiles;       // workgroups for a group's heads
+  int query_blocks;     // of a sequence
+  bool q_runs;          // queries are whole 16-byte runs
+};
+
+__device__ __align__(16) uint32_t window_zero16[4];
+
+// Stage kTile rows of d elements from `base` into an LDS tile of W wide rows; rows from
+// `rows` on and elements past d are zero.  DMA: direct loads, which the caller waits for;
+// rows are then 16-byte aligned and their stride is below 2^26.
+template <class E, int W, bool DMA>
+__device__ __forceinline__ void stage_tile(char* lds, const typename E::T* base, int64_t stride, int rows, int d, int wave,
+                                           int lane) {
+  typedef typename E::V8 V8;
+  constexpr int U = W / 8, R = 64 / U, LOADS = kTile / R / kWaves;
+  const int r0 = lane / U, u0 = unit_slot<W>(r0, lane % U);
+  const char* from = (const char*)(base + (int64_t)(R * wave) * stride);
+  const int64_t step = (int64_t)(R * kWaves) * stride * 2;
+  if (DMA && rows >= kTile && d == W) {
+    const uint32_t voff = (uint32_t)r0 * (uint32_t)stride * 2u;
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) {
+      const int i = wave + kWaves * x;
+      dma16s(from, voff + 16 * (u0 ^ unit_slot<W>(R * i, 0)), lds + 1024 * i);
+      from += step;
+    }
+  } else {
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) {
+      const int i = wave + kWaves * x, u = u0 ^ unit_slot<W>(R * i, 0);
+      const char* p = from + r0 * stride * 2 + 16 * u;
+      const bool in = R * i + r0 < rows && 8 * u < d;
+      if (DMA) {
+        dma16(in ? (const void*)p : (const void*)window_zero16, lds + 1024 * i);
+      } else {
+        V8 v = {};
+        if (in) {
+          const int left = d - 8 * u;
+          const typename E::T* e = (const typename E::T*)p;
+          if (left >= 8)
+            __builtin_memcpy(&v, e, 16);
+          else
+#pragma unroll
+            for (int y = 0; y < 8; ++y)
+              if (y < left) v[y] = e[y];
+        }
+        *(V8*)(lds + 1024 * i + 16 * lane) = v;
+      }
+      from += step;
+    }
+  }
+}
+
+template <class V8>
+__device__ __forceinline__ bool any_not_finite(const V8 (&v)[4], uint32_t inf) {
+  typedef unsigned short US8 __attribute__((ext_vector_type(8)));
+  US8 m = __builtin_bit_cast(US8, v[0]) & (unsigned short)0x7fff;
+#pragma unroll
+  for (int x = 1; x < 4; ++x) m = __builtin_elementwise_max(m, __builtin_bit_cast(US8, v[x]) & (unsigned short)0x7fff);
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, (uint32_t)m[e]);
+  return __any(top >= inf);
+}
+
+// DP: padded head width, NV: 32-column tiles of the values.
+template <class E, int DP, int NV, bool DMA>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void k_tok_window(WindowRun run) {
   typedef typename E::T T;
+  typedef typename E::V8 V8;
+  typedef typename E::V4 V4;
+  constexpr bool F = __is_same(E, F16);
+  constexpr int VW = NV == 1 ? 32 : NV == 2 ? 64 : 128;  // LDS row of values
+  constexpr int KB = kTile * DP * 2, STAGE = KB + kTile * VW * 2;
+  constexpr uint32_t INF = F ? 0x7c00 : 0x7f80;
+  // Weights are held at 2^off of exp(score - base), and base is let lag 2^lag behind the
+  // maximum, so that outputs are seldom rescaled: fp16 terms stay below 2^15 and keep the
+  // bits above 2^-32 of the largest weight, bf16 ones leave room for 2^31 tokens.
+  constexpr float off = F ? 7.f : -40.f, lag = 8.f;
+  __shared__ __align__(1024) char lds[2 * STAGE];
+  const WindowArgs& a = run.a;
   const ncodec_window_shape& s = a.s;
-  const int lane = threadIdx.x & 63;
-  const int D = s.head_dim, V = s.value_dim;
-  for (int64_t it = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); it < items; it += (int64_t)gridDim.x * 4) {
-    const int h = (int)(it % s.heads);
-    const int64_t row = it / s.heads, b = row / s.tokens, i = row % s.tokens;
-    const int hk = h / (s.heads / s.kv_heads);
-    const int64_t len = a.lengths ? min(max((int64_t)a.lengths[b], (int64_t)0), s.tokens) : s.tokens;
-    const T* q = (const T*)a.q + b * s.q_batch_stride + i * s.q_token_stride + h * s.q_head_stride;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, l32 = lane & 31;
+  const int group = s.heads / s.kv_heads, D = s.head_dim, V = s.value_dim;
+  // the last queries of all heads first: they see most
+  const int64_t block = run.first + blockIdx.x, per = s.batch * s.kv_heads * run.head_tiles;
+  const int qb = run.query_blocks - 1 - (int)(block / per);
+  uint32_t at = (uint32_t)(block % per);
+  const int ht = at % (uint32_t)run.head_tiles;
+  at /= (uint32_t)run.head_tiles;
+  const int hk = at % (uint32_t)s.kv_heads;
+  const int64_t b = at / (uint32_t)s.kv_heads;
+  const int qw = kWaves / run.head_waves;  // waves along the queries
+  const int hd = hk * group + ht * run.head_waves + wave % run.head_waves;
+  const int64_t len = a.lengths ? min(max((int64_t)a.lengths[b], (int64_t)0), s.tokens) : s.tokens;
+  const int i0 = qb * qw * kQueries;                                     // the workgroup's first query
+  const int wi0 = i0 + wave / run.head_waves * kQueries, i = wi0 + l32;  // the wave's, the lane's
+  const int iend = (int)min((int64_t)i0 + qw * kQueries, len);           // behind its last one
+  const int wend = (int)min((int64_t)wi0 + kQueries, len);
+
+  T* o = (T*)a.o + b * s.o_batch_stride + (int64_t)i * s.o_token_stride + hd * s.o_head_stride;
+  floatx16 out[NV];
+#pragma unroll
+  for (int x = 0; x < NV; ++x)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) out[x][r] = 0.f;
+  float sum = 0.f;
+
+  if (i0 < iend) {
     const T* k = (const T*)a.k + b * s.k_batch_stride + hk * s.k_head_stride;
     const T* v = (const T*)a.v + b * s.v_batch_stride + hk * s.v_head_stride;
-    T* o = (T*)a.o + b * s.o_batch_stride + i * s.o_token_stride + h * s.o_head_stride;
-    float m = -__builtin_huge_valf(), l = 0.f, acc[2] = {};
-    if (i < len) {
-      const Seen seen = seen_by((int)i, s.window, s.sinks);
-      for (int x0 = 0; x0 < seen.count; x0 += 64) {
-        const bool in = x0 + lane < seen.count;
-        const int64_t j = in ? seen.at(x0 + lane) : 0;
-        float z = 0.f;
-        for (int d = 0; d < D; ++d) z = fmaf((float)q[d], (float)k[j * s.k_token_stride + d], z);
-        z = in ? z * s.scale * 1.44269504088896341f : -__builtin_huge_valf();
-        float top = z;
-        for (int w = 32; w; w >>= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, w, 64));
-        const float m1 = __builtin_elementwise_maximum(m, top);
-        const float base = m1 == -__builtin_huge_valf() ? 0.f : m1;
-        const float fade = exp2f(m - base), p = exp2f(z - base - kBelow);
-        float sum = p;
-        for (int w = 32; w; w >>= 1) sum += __shfl_xor(sum, w, 64);
-        l = l * fade + sum;
-        m = m1;
-        acc[0] *= fade;
-        acc[1] *= fade;
-        for (int x = 0; x < min(64, seen.count - x0); ++x) {
-          const float px = __shfl(p, x, 64);
-          const T* vr = v + (int64_t)seen.at(x0 + x) * s.v_token_stride;
-          for (int y = 0; y < 2; ++y)
-            if (lane + 64 * y < V) acc[y] = fmaf(px, (float)vr[lane + 64 * y], acc[y]);
+    const int window = s.window ? (int)s.window : 0x7fffffff, sinks = (int)s.sinks;
+    // tiles: those of the first tokens that the window has left behind, then from the window on
+    const int near = max(0, i0 + 1 - window);
+    const int lead = (min(sinks, near) + kTile - 1) / kTile, from = max(near / kTile, lead);
+    const int tiles = lead + (iend + kTile - 1) / kTile - from;
+    const auto key0 = [&](int t) { return (t < lead ? t : t - lead + from) * kTile; };
+    const auto stage = [&](int t) {
+      char* to = lds + (t & 1) * STAGE;
+      const int j0 = key0(t), rows = (int)min((int64_t)kTile, len - j0);
+      stage_tile<E, DP, DMA>(to, k + (int64_t)j0 * s.k_token_stride, s.k_token_stride, rows, D, wave, lane);
+      stage_tile<E, VW, DMA>(to + KB, v + (int64_t)j0 * s.v_token_stride, s.v_token_stride, rows, V, wave, lane);
+    };
+    stage(0);
+
+    // the scale's sign goes into the queries, so that the largest product is the largest score
+    const float c = s.scale == 0.f ? 1.f : fabsf(s.scale) * 1.44269504088896341f;
+    V8 qf[DP / 16];
+    {
+      const T* q = (const T*)a.q + b * s.q_batch_stride + (int64_t)min(i, (int)len - 1) * s.q_token_stride + hd * s.q_head_stride;
+#pragma unroll
+      for (int x = 0; x < DP / 16; ++x) {
+        const int d = 16 * x + 8 * h;
+        V8 w = {};
+        if (run.q_runs) {
+          if (d < D) w = *(const V8*)(q + d);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (d + e < D) w[e] = q[d + e];
         }
+        if (s.scale <= 0.f) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] = s.scale == 0.f ? (T)((float)w[e] * 0.f) : (T)-w[e];
+        }
+        qf[x] = w;
       }
     }
-    for (int y = 0; y < 2; ++y)
-      if (lane + 64 * y < V) o[lane + 64 * y] = (T)(i < len ? acc[y] / l : 0.f);
+    const int ro = row_offset<DP>(lane);
+    const int pv0 = col_offset<VW, false>(lane, 0), pv1 = col_offset<VW, false>(lane, 1);
+    float mc = -__builtin_huge_valf(), base = 0.f;  // maximum and what is taken from each score, times c
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+
+    for (int t = 0; t < tiles; ++t) {
+      // every wave's loads of tile t have landed (each waited for its own), and every
+      // wave is done with the other buffer
+      lds_barrier();
+      if (t + 1 < tiles) stage(t + 1);
+      const char* kt = lds + (t & 1) * STAGE;
+      const char* vt = kt + KB;
+      const int j0 = key0(t);
+      // does any of the wave's queries see any of the tile's keys, and all all of them?
+      const bool some = j0 < wend && (j0 < sinks || wi0 - (j0 + kTile - 1) < window);
+      const bool all = j0 + kTile - 1 <= wi0 && (wi0 + kQueries - 1 - j0 < window || j0 + kTile <= sinks);
+      if (some) {
+        floatx16 p[2] = {};
+#pragma unroll
+        for (int x = 0; x < DP / 16; ++x) {
+          const char* r = kt + (ro ^ (32 * x));
+          p[0] = E::mfma(*(const V8*)r, qf[x], p[0]);
+          p[1] = E::mfma(*(const V8*)(r + 64 * DP), qf[x], p[1]);
+        }
+        uint32_t seen[2] = {0xffffu, 0xffffu};
+        if (!all) {
+          seen[0] = seen[1] = 0;
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int j = j0 + 32 * y + drow(r, h), d = i - j;
+              const bool in = (uint32_t)d < (uint32_t)window || (d >= 0 && j < sinks);
+              seen[y] |= in ? 1u << r : 0u;
+              p[y][r] = in ? p[y][r] : -__builtin_huge_valf();
+            }
+        }
+        float top = fmaxf(p[0][0], p[1][0]);
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, p[0][r]), p[1][r]);
+        if (__any(fmaf(top, c, -lag) > mc)) {
+          const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+          top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+          // each query by its own scores, whatever the wave's others are
+          const bool rises = fmaf(top, c, -lag) > mc;
+          const float m1 = rises ? top * c : mc, base1 = rises ? m1 - off : base;
+          const float fade = !rises ? 1.f : mc == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(base - base1);
+          mc = m1;
+          base = base1;
+          sum *= fade;
+#pragma unroll
+          for (int x = 0; x < NV; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) out[x][r] *= fade;
+        }
+        V8 hi[4], lo[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          float w[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            w[e] = __builtin_amdgcn_exp2f(fmaf(p[x >> 1][8 * (x & 1) + e], c, -base));
+            sum += w[e];
+          }
+          two_terms<E>(w, 1.f, hi[x], lo[x]);
+        }
+#pragma unroll
+        for (int y = 0; y < NV; ++y) {
+          V8 vf[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            vf[x] = read_cols<E>(vt + ((pv0 ^ (64 * y)) + 32 * VW * x), vt + ((pv1 ^ (64 * y)) + 32 * VW * x));
+          if (!all && any_not_finite(vf, INF)) {
+            // a product would carry it to queries that do not see it too (0 times NaN): it is
+            // taken out, and counted for those that do
+            floatx16 hit = {};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              V8 bad = {}, sees = {};
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const uint32_t u = (uint32_t)__builtin_bit_cast(uint16_t, (T)vf[x][e]) & 0x7fffu;
+                bad[e] = u >= INF ? (T)1.f : (T)0.f;
+                vf[x][e] = u >= INF ? (T)0.f : vf[x][e];
+                sees[e] = seen[x >> 1] >> (8 * (x & 1) + e) & 1 ? (T)1.f : (T)0.f;
+              }
+              hit = E::mfma(bad, sees, hit);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) out[y][r] = hit[r] > 0.f ? __builtin_nanf("") : out[y][r];
+          }
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            out[y] = E::mfma(vf[x], lo[x], out[y]);
+            out[y] = E::mfma(vf[x], hi[x], out[y]);
+          }
+        }
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+    sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    // a token sees itself: without any weight its scores are all -inf, and no weight is a number
+    sum = sum == 0.f ? __builtin_nanf("") : 1.f / sum;
   }
+  if (i >= s.tokens) return;
+  const bool live = i < len;
+  // A lane has four consecutive values four times for each 32, its neighbour l ^ 32 the
+  // four after them: exchanged, each has eight, a 16-byte run of the row.
+#pragma unroll
+  for (int y = 0; y < NV; ++y)
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      V4 x0, x1;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x0[e] = (T)(live ? out[y][8 * g + e] * sum : 0.f);
+        x1[e] = (T)(live ? out[y][8 * g + 4 + e] * sum : 0.f);
+      }
+      typedef uint32_t U2 __attribute__((ext_vector_type(2)));
+      typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+      const U2 u0 = __builtin_bit_cast(U2, x0), u1 = __builtin_bit_cast(U2, x1);
+      const auto w0 = __builtin_amdgcn_permlane32_swap(u0.x, u1.x, false, false);
+      const auto w1 = __builtin_amdgcn_permlane32_swap(u0.y, u1.y, false, false);
+      const U4 w = {w0[0], w1[0], w0[1], w1[1]};
+      const int d = 32 * y + 16 * g + 8 * h, left = V - d;
+      if (left >= 8) {
+        __builtin_memcpy(o + d, &w, 16);
+      } else if (left > 0) {
+        const V8 z = __builtin_bit_cast(V8, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < left) o[d + e] = z[e];
+      }
+    }
+}
+
+template <class E, int DP, int NV, bool DMA>
+hipError_t go(WindowRun run, hipStream_t st) {
+  const ncodec_window_shape& s = run.a.s;
+  const int64_t blocks = s.batch * s.kv_heads * run.head_tiles * run.query_blocks;
+  // a launch counts its threads in 32 bits
+  for (; run.first < blocks; run.first += 1 << 23) {
+    launch(k_tok_window<E, DP, NV, DMA>, dim3((unsigned)std::min<int64_t>(blocks - run.first, 1 << 23)), dim3(64 * kWaves), st, run);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+template <class E, int DP, bool DMA>
+hipError_t by_value(const WindowRun& run, hipStream_t st) {
+  const int V = run.a.s.value_dim;
+  if (V <= 32) return go<E, DP, 1, DMA>(run, st);
+  if (V <= 64) return go<E, DP, 2, DMA>(run, st);
+  if (V <= 96) return go<E, DP, 3, DMA>(run, st);
+  return go<E, DP, 4, DMA>(run, st);
+}
+template <class E>
+hipError_t run_window(const WindowArgs& a, hipStream_t st) {
+  const ncodec_window_shape& s = a.s;
+  const auto runs = [](const void* x, int64_t batch, int64_t token, int64_t head) {
+    return (uintptr_t)x % 16 == 0 && batch % 8 == 0 && token % 8 == 0 && head % 8 == 0;
+  };
+  const int group = s.heads / s.kv_heads, head_waves = group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
+  const int64_t queries = kQueries * (kWaves / head_waves);
+  const WindowRun run{a, 0, head_waves, group / head_waves, (int)((s.tokens + queries - 1) / queries),
+                      s.head_dim % 8 == 0 && runs(a.q, s.q_batch_stride, s.q_token_stride, s.q_head_stride)};
+  const bool dma = s.head_dim % 8 == 0 && s.value_dim % 8 == 0 && runs(a.k, s.k_batch_stride, s.k_token_stride, s.k_head_stride) &&
+                   runs(a.v, s.v_batch_stride, s.v_token_stride, s.v_head_stride) && s.k_token_stride < (1 << 26) &&
+                   s.v_token_stride < (1 << 26);
+  if (s.head_dim <= 64) return dma ? by_value<E, 64, true>(run, st) : by_value<E, 64, false>(run, st);
+  return dma ? by_value<E, 128, true>(run, st) : by_value<E, 128, false>(run, st);
 }
 
 }  // namespace
 
 hipError_t launch_window_attention(const WindowArgs& a, hipStream_t st) {
-  const int64_t items = a.s.batch * a.s.tokens * a.s.heads;
-  const dim3 grid((unsigned)std::min<int64_t>((items + 3) / 4, 1 << 20));
-  if (a.s.dtype == NCODEC_DTYPE_FP16)
-    launch(k_tok_window<F16>, grid, dim3(256), st, a, items);
-  else
-    launch(k_tok_window<BF16>, grid, dim3(256), st, a, items);
-  return hipGetLastError();
+  return a.s.dtype == NCODEC_DTYPE_FP16 ? run_window<F16>(a, st) : run_window<BF16>(a, st);
 }
 
 }  // namespace nc

@@ -2,7 +2,7 @@
 
 Of a score, fp32: (D + 2) products and sums against the sum of magnitudes, and four more operations on its value.  A
 weight then errs by that, by 2^-21 of the exponential, and by its two 16-bit terms (2^-22 in fp16, 2^-16 in bf16, and in
-fp16 2^-39 of the largest weight where the terms are subnormal).  Weights occur above and below the line, their sums are
+fp16 2^-32 of the largest weight where the terms are subnormal).  Weights occur above and below the line, their sums are
 fp32; the output is rounded once."""
 import numpy as np
 import torch
@@ -44,7 +44,7 @@ def output_bound(want, mag, vmax, q, k, scale, D, n, dt):
     """want: the outputs, mag: the same weights over magnitudes of v, n: tokens seen at most."""
     e = (2 * weight_error(q, k, scale, D, dt) + (n + 64) * F32) * mag
     if dt == "fp16":
-        e = e + n * 2.0 ** -39 * vmax
+        e = e + n * 2.0 ** -32 * vmax
     return e * (1 + U[dt]) + U[dt] * np.abs(want) + TINY[dt]
 
 
