@@ -75,6 +75,35 @@ __device__ __forceinline__ void stage_tile(char* lds, const typename E::T* base,
   }
 }
 
+// Eight weights as two 16-bit terms (two_terms() in fewer steps: the rest of an fp16 term
+// is formed and rounded in one instruction).
+__device__ __forceinline__ void weight_terms(const float (&w)[8], half8& hi, half8& lo) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const half2 x = {(f16)w[i], (f16)w[i + 1]};
+    half2 y;
+    // w - x, fp32, rounded once to each half of y
+    asm("v_fma_mixlo_f16 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(y) : "v"(x), "v"(w[i]));
+    asm("v_fma_mixhi_f16 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(y) : "v"(x), "v"(w[i + 1]));
+    hi[i] = x.x;
+    hi[i + 1] = x.y;
+    lo[i] = y.x;
+    lo[i + 1] = y.y;
+  }
+}
+__device__ __forceinline__ void weight_terms(const float (&w)[8], bhalf8& hi, bhalf8& lo) { two_terms<BF16>(w, 1.f, hi, lo); }
+
+// The largest of eight elements' bits without their signs: they order finite values,
+// infinities and NaN.
+template <class V8>
+__device__ __forceinline__ uint32_t largest_bits(const V8& v) {
+  typedef unsigned short US8 __attribute__((ext_vector_type(8)));
+  typedef unsigned short US2 __attribute__((ext_vector_type(2)));
+  const US8 u = __builtin_bit_cast(US8, v) & (unsigned short)0x7fff;
+  const US2 m = __builtin_elementwise_max(__builtin_elementwise_max(u.s01, u.s23), __builtin_elementwise_max(u.s45, u.s67));
+  return max((uint32_t)m.x, (uint32_t)m.y);
+}
+
 template <class V8>
 __device__ __forceinline__ bool any_not_finite(const V8 (&v)[4], uint32_t inf) {
   typedef unsigned short US8 __attribute__((ext_vector_type(8)));
@@ -135,11 +164,22 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     const T* k = (const T*)a.k + b * s.k_batch_stride + hk * s.k_head_stride;
     const T* v = (const T*)a.v + b * s.v_batch_stride + hk * s.v_head_stride;
     const int window = s.window ? (int)s.window : 0x7fffffff, sinks = (int)s.sinks;
-    // tiles: those of the first tokens that the window has left behind, then from the window on
-    const int near = max(0, i0 + 1 - window);
-    const int lead = (min(sinks, near) + kTile - 1) / kTile, from = max(near / kTile, lead);
-    const int tiles = lead + (iend + kTile - 1) / kTile - from;
-    const auto key0 = [&](int t) { return (t < lead ? t : t - lead + from) * kTile; };
+    // Tiles of keys: those of the first tokens that the window has left behind (`lead` of
+    // them), then `from` on.  The ones that all queries of the workgroup see whole come first.
+    const int near = max(0, i0 + 1 - window), last = i0 + qw * kQueries - 1;
+    const int lead = (min(sinks, near) + kTile - 1) / kTile, from = max(near / kTile, lead), end = (iend + kTile - 1) / kTile;
+    const int lead_whole = min(lead, sinks / kTile);
+    const int whole_a = max(from, last < window ? 0 : (last - window + kTile) / kTile), whole_b = max(whole_a, (i0 + 1) / kTile);
+    const int whole = lead_whole + whole_b - whole_a, tiles = lead + end - from;
+    const auto key0 = [&](int t) {
+      int x = t < lead_whole ? t : t - lead_whole + whole_a;
+      if (t >= whole) {
+        x = t - whole + lead_whole;                                   // the rest of the first ones,
+        if (x >= lead) x += from - lead;                              // those before the whole ones
+        if (x >= whole_a && t - whole + lead_whole >= lead) x += whole_b - whole_a;  // and behind them
+      }
+      return x * kTile;
+    };
     const auto stage = [&](int t) {
       char* to = lds + (t & 1) * STAGE;
       const int j0 = key0(t), rows = (int)min((int64_t)kTile, len - j0);
@@ -164,79 +204,143 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
           for (int e = 0; e < 8; ++e)
             if (d + e < D) w[e] = q[d + e];
         }
-        if (s.scale <= 0.f) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = s.scale == 0.f ? (T)((float)w[e] * 0.f) : (T)-w[e];
-        }
         qf[x] = w;
+      }
+      if (s.scale <= 0.f) {
+#pragma unroll
+        for (int x = 0; x < DP / 16; ++x)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) qf[x][e] = s.scale == 0.f ? (T)((float)qf[x][e] * 0.f) : (T)-qf[x][e];
       }
     }
     const int ro = row_offset<DP>(lane);
     const int pv0 = col_offset<VW, false>(lane, 0), pv1 = col_offset<VW, false>(lane, 1);
     float mc = -__builtin_huge_valf(), base = 0.f;  // maximum and what is taken from each score, times c
+
+    // does any of the wave's queries see any of the tile's keys?
+    const auto some = [&](int j0) { return j0 < wend && (j0 < sinks || wi0 - (j0 + kTile - 1) < window); };
+    const auto scores = [&](const char* kt, floatx16(&p)[2]) {
+      p[0] = p[1] = floatx16{};
+      constexpr int N = DP / 16, A = 3;  // reads that many steps ahead
+      V8 kf[N][2];
+      const auto keys = [&](int x) {
+        const char* r = kt + (ro ^ (32 * x));
+        kf[x][0] = *(const V8*)r;
+        kf[x][1] = *(const V8*)(r + 64 * DP);
+      };
+#pragma unroll
+      for (int x = 0; x < A; ++x) keys(x);
+#pragma unroll
+      for (int x = 0; x < N; ++x) {
+        if (x + A < N) keys(x + A);
+        __builtin_amdgcn_sched_barrier(0);
+        p[0] = E::mfma(kf[x][0], qf[x], p[0]);
+        p[1] = E::mfma(kf[x][1], qf[x], p[1]);
+      }
+    };
+    const auto follow = [&](const floatx16(&p)[2]) {  // the base after the maximum
+      float top = fmaxf(p[0][0], p[1][0]);
+#pragma unroll
+      for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, p[0][r]), p[1][r]);
+      if (__any(fmaf(top, c, -lag) > mc)) {
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+        // each query by its own scores, whatever the wave's others are
+        const bool rises = fmaf(top, c, -lag) > mc;
+        const float m1 = rises ? top * c : mc, base1 = rises ? m1 - off : base;
+        const float fade = !rises ? 1.f : mc == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(base - base1);
+        mc = m1;
+        base = base1;
+        sum *= fade;
+#pragma unroll
+        for (int x = 0; x < NV; ++x)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) out[x][r] *= fade;
+      }
+    };
+    // weights of keys 16 x .. of a tile
+    const auto weights = [&](const floatx16(&p)[2], int x, V8& hi, V8& lo) {
+      float w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        w[e] = __builtin_amdgcn_exp2f(fmaf(p[x >> 1][8 * (x & 1) + e], c, -base));
+        sum += w[e];
+      }
+      weight_terms(w, hi, lo);
+    };
+
+#pragma unroll
+    for (int x = 0; x < DP / 16; ++x) asm volatile("" : "+v"(qf[x]));  // here, not in the loop, are the queries waited for
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
-    for (int t = 0; t < tiles; ++t) {
+    int t = 0;
+    for (; t < whole; ++t) {
       // every wave's loads of tile t have landed (each waited for its own), and every
       // wave is done with the other buffer
       lds_barrier();
       if (t + 1 < tiles) stage(t + 1);
       const char* kt = lds + (t & 1) * STAGE;
       const char* vt = kt + KB;
-      const int j0 = key0(t);
-      // does any of the wave's queries see any of the tile's keys, and all all of them?
-      const bool some = j0 < wend && (j0 < sinks || wi0 - (j0 + kTile - 1) < window);
-      const bool all = j0 + kTile - 1 <= wi0 && (wi0 + kQueries - 1 - j0 < window || j0 + kTile <= sinks);
-      if (some) {
-        floatx16 p[2] = {};
+      floatx16 cur[2];
+      __builtin_amdgcn_s_setprio(1);
+      scores(kt, cur);
+      __builtin_amdgcn_s_setprio(0);
+      follow(cur);
+      V8 hi[4], lo[4], vf[2][4];
+      const auto values = [&](int y) {
 #pragma unroll
-        for (int x = 0; x < DP / 16; ++x) {
-          const char* r = kt + (ro ^ (32 * x));
-          p[0] = E::mfma(*(const V8*)r, qf[x], p[0]);
-          p[1] = E::mfma(*(const V8*)(r + 64 * DP), qf[x], p[1]);
+        for (int x = 0; x < 4; ++x)
+          vf[y & 1][x] = read_cols<E>(vt + ((pv0 ^ (64 * y)) + 32 * VW * x), vt + ((pv1 ^ (64 * y)) + 32 * VW * x));
+      };
+      values(0);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) weights(cur, x, hi[x], lo[x]);
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int y = 0; y < NV; ++y) {
+        if (y + 1 < NV) values(y + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          out[y] = E::mfma(vf[y & 1][x], lo[x], out[y]);
+          out[y] = E::mfma(vf[y & 1][x], hi[x], out[y]);
         }
+      }
+      __builtin_amdgcn_s_setprio(0);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    for (; t < tiles; ++t) {
+      lds_barrier();
+      if (t + 1 < tiles) stage(t + 1);
+      const char* kt = lds + (t & 1) * STAGE;
+      const char* vt = kt + KB;
+      const int j0 = key0(t);
+      if (some(j0)) {
+        const bool all = j0 + kTile - 1 <= wi0 && (wi0 + kQueries - 1 - j0 < window || j0 + kTile <= sinks);
+        floatx16 cur[2];
+        __builtin_amdgcn_s_setprio(1);
+        scores(kt, cur);
+        __builtin_amdgcn_s_setprio(0);
         uint32_t seen[2] = {0xffffu, 0xffffu};
         if (!all) {
+          int h0 = h, il = i;
+          asm volatile("" : "+v"(h0), "+v"(il));  // nothing of this is computed, and kept, before the loop
           seen[0] = seen[1] = 0;
 #pragma unroll
           for (int y = 0; y < 2; ++y)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-              const int j = j0 + 32 * y + drow(r, h), d = i - j;
+              const int j = j0 + 32 * y + drow(r, h0), d = il - j;
               const bool in = (uint32_t)d < (uint32_t)window || (d >= 0 && j < sinks);
               seen[y] |= in ? 1u << r : 0u;
-              p[y][r] = in ? p[y][r] : -__builtin_huge_valf();
+              cur[y][r] = in ? cur[y][r] : -__builtin_huge_valf();
             }
         }
-        float top = fmaxf(p[0][0], p[1][0]);
-#pragma unroll
-        for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, p[0][r]), p[1][r]);
-        if (__any(fmaf(top, c, -lag) > mc)) {
-          const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-          top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-          // each query by its own scores, whatever the wave's others are
-          const bool rises = fmaf(top, c, -lag) > mc;
-          const float m1 = rises ? top * c : mc, base1 = rises ? m1 - off : base;
-          const float fade = !rises ? 1.f : mc == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(base - base1);
-          mc = m1;
-          base = base1;
-          sum *= fade;
-#pragma unroll
-          for (int x = 0; x < NV; ++x)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) out[x][r] *= fade;
-        }
+        follow(cur);
         V8 hi[4], lo[4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          float w[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            w[e] = __builtin_amdgcn_exp2f(fmaf(p[x >> 1][8 * (x & 1) + e], c, -base));
-            sum += w[e];
-          }
-          two_terms<E>(w, 1.f, hi[x], lo[x]);
-        }
+        for (int x = 0; x < 4; ++x) weights(cur, x, hi[x], lo[x]);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int y = 0; y < NV; ++y) {
           V8 vf[4];
@@ -269,6 +373,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
           }
         }
       }
+      __builtin_amdgcn_s_setprio(0);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
