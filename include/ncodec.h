@@ -655,10 +655,13 @@ typedef struct {
   int64_t keep, sinks, recent;
 } ncodec_evict_shape;
 
+/* Bytes of workspace, as for the attention. */
+size_t ncodec_cache_evict_workspace_bytes(const ncodec_cache_shape* cache, const ncodec_evict_shape* shape);
+
 ncodec_status ncodec_cache_evict(const ncodec_cache_shape* cache, const ncodec_evict_shape* shape, void* d_k_cache,
                                  void* d_v_cache, const int32_t* d_table, const int32_t* d_lengths, const float* d_mass,
                                  const int32_t* d_new_table, int32_t* d_new_lengths, float* d_new_mass,
-                                 int32_t* d_kept, void* hip_stream);
+                                 int32_t* d_kept, void* d_workspace, size_t ws_bytes, void* hip_stream);
 
 /* Message for the last error on ctx (or the last create failure if ctx is NULL). */
 const char* ncodec_last_error(const ncodec_ctx* ctx);

@@ -399,11 +399,17 @@ extern "C" ncodec_status ncodec_cache_append(const ncodec_cache_shape* cache, co
                 "cache_append");
 }
 
+extern "C" size_t ncodec_cache_evict_workspace_bytes(const ncodec_cache_shape* cache, const ncodec_evict_shape* shape) {
+  ncodec_status st;
+  if (!cache || !shape || evict_fault(*cache, *shape, &st)) return 0;
+  return nc::evict_workspace_bytes(*cache, *shape);
+}
+
 extern "C" ncodec_status ncodec_cache_evict(const ncodec_cache_shape* cache, const ncodec_evict_shape* shape,
                                             void* d_k_cache, void* d_v_cache, const int32_t* d_table,
                                             const int32_t* d_lengths, const float* d_mass, const int32_t* d_new_table,
                                             int32_t* d_new_lengths, float* d_new_mass, int32_t* d_kept,
-                                            void* hip_stream) {
+                                            void* d_workspace, size_t ws_bytes, void* hip_stream) {
   if (!cache || !shape) return set_error(NCODEC_EINVAL, "cache_evict", "a shape is NULL");
   ncodec_status st;
   if (const char* why = evict_fault(*cache, *shape, &st)) return set_error(st, "cache_evict", why);
@@ -417,6 +423,9 @@ extern "C" ncodec_status ncodec_cache_evict(const ncodec_cache_shape* cache, con
       !aligned(d_mass, 4) || !aligned(d_new_table, 4) || !aligned(d_new_lengths, 4) || !aligned(d_new_mass, 4) ||
       !aligned(d_kept, 4))
     return set_error(NCODEC_EINVAL, "cache_evict", "a pointer is not aligned to an element");
+  const size_t need = nc::evict_workspace_bytes(c, s);
+  if (need && (!d_workspace || ws_bytes < need || !aligned(d_workspace, 256)))
+    return set_error(NCODEC_ENOMEM, "cache_evict", "the workspace must be 256-byte aligned and hold ", need);
   const int64_t bk = s.batch * c.kv_heads;
   const Area kc = k_area(c, d_k_cache), vc = v_area(c, d_v_cache),
              table = table_area(d_table, s.batch, s.columns, s.table_stride),
@@ -431,7 +440,7 @@ extern "C" ncodec_status ncodec_cache_evict(const ncodec_cache_shape* cache, con
       !all_apart(kept, {table, new_table, lengths, mass}))
     return set_error(NCODEC_EINVAL, "cache_evict", "an output overlaps an input or another output");
   return finish(nc::launch_cache_evict({c, s, d_k_cache, d_v_cache, d_table, d_lengths, d_mass, d_new_table,
-                                        d_new_lengths, d_new_mass, d_kept},
+                                        d_new_lengths, d_new_mass, d_kept, d_workspace},
                                        (hipStream_t)hip_stream),
                 "cache_evict");
 }

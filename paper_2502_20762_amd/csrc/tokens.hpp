@@ -122,7 +122,9 @@ struct EvictArgs {
   int32_t* new_lengths;
   float* new_mass;
   int32_t* kept;
+  void* ws;
 };
+size_t evict_workspace_bytes(const ncodec_cache_shape& c, const ncodec_evict_shape& s);
 hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st);
 
 }  // namespace nc

@@ -161,8 +161,10 @@ _SIGNATURES = {
                                + [_P] * 8 + [ctypes.c_size_t, _P]),
     "ncodec_cache_append": (ctypes.c_int, [ctypes.POINTER(ncodec_cache_shape), ctypes.POINTER(ncodec_append_shape)]
                             + [_P] * 9),
+    "ncodec_cache_evict_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(ncodec_cache_shape),
+                                                             ctypes.POINTER(ncodec_evict_shape)]),
     "ncodec_cache_evict": (ctypes.c_int, [ctypes.POINTER(ncodec_cache_shape), ctypes.POINTER(ncodec_evict_shape)]
-                           + [_P] * 10),
+                           + [_P] * 10 + [ctypes.c_size_t, _P]),
     "ncodec_last_error": (ctypes.c_char_p, [_P]),
     "ncodec_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "ncodec_destroy": (None, [_P]),
@@ -380,12 +382,17 @@ def ncodec_cache_append(cache: ncodec_cache_shape, shape: ncodec_append_shape, d
                                               _p(d_mass), stream or None))
 
 
+def ncodec_cache_evict_workspace_bytes(cache: ncodec_cache_shape, shape: ncodec_evict_shape) -> int:
+    return int(load_library().ncodec_cache_evict_workspace_bytes(ctypes.byref(cache), ctypes.byref(shape)))
+
+
 def ncodec_cache_evict(cache: ncodec_cache_shape, shape: ncodec_evict_shape, d_k_cache: int, d_v_cache: int,
                        d_table: int, d_lengths: int, d_mass: int, d_new_table: int, d_new_lengths: int,
-                       d_new_mass: int, d_kept: int, stream: int = 0) -> None:
+                       d_new_mass: int, d_kept: int, d_workspace: int = 0, ws_bytes: int = 0, stream: int = 0) -> None:
     _check(load_library().ncodec_cache_evict(ctypes.byref(cache), ctypes.byref(shape), _p(d_k_cache), _p(d_v_cache),
                                              _p(d_table), _p(d_lengths), _p(d_mass), _p(d_new_table),
-                                             _p(d_new_lengths), _p(d_new_mass), _p(d_kept), stream or None))
+                                             _p(d_new_lengths), _p(d_new_mass), _p(d_kept), _p(d_workspace), ws_bytes,
+                                             stream or None))
 
 
 def ncodec_last_error(ctx=None) -> str:

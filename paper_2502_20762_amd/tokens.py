@@ -381,7 +381,11 @@ def cache_evict(k_cache, v_cache, page_table, lengths, mass, keep, new_table, si
     _like(kept, torch.int32, device, (B, K, keep), "out[2]")
     _need(kept.is_contiguous(), "out[2] must be contiguous")
     shape = _nc.ncodec_evict_shape(B, columns, table_stride, new_columns, new_stride, keep, sinks, recent)
-    _call(_nc.load_library().ncodec_cache_evict, device, ctypes.byref(cache), ctypes.byref(shape), k_cache.data_ptr(),
-          v_cache.data_ptr(), page_table.data_ptr(), lengths.data_ptr(), mass.data_ptr(), new_table.data_ptr(),
-          new_lengths.data_ptr(), new_mass.data_ptr(), kept.data_ptr())
+    lib = _nc.load_library()
+    cref, ref = ctypes.byref(cache), ctypes.byref(shape)
+    need = lib.ncodec_cache_evict_workspace_bytes(cref, ref)
+    ws = k_cache.new_empty(need, dtype=torch.uint8) if need else None
+    _call(lib.ncodec_cache_evict, device, cref, ref, k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(),
+          lengths.data_ptr(), mass.data_ptr(), new_table.data_ptr(), new_lengths.data_ptr(), new_mass.data_ptr(),
+          kept.data_ptr(), _ptr(ws), need)
     return out

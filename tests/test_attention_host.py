@@ -101,7 +101,7 @@ def append(cache, shape, **kw):
 
 def evict(cache, shape, **kw):
     p = dict(kc=FAR[0], vc=FAR[1], table=FAR[2], lengths=FAR[3], mass=FAR[4], new_table=FAR[5], new_lengths=FAR[6],
-             new_mass=FAR[7], kept=FAR[8])
+             new_mass=FAR[7], kept=FAR[8], ws=FAR[9], nb=1 << 60)
     p.update(kw)
     return refused(nc.ncodec_cache_evict, "cache_evict", cache, shape, *p.values())
 
@@ -157,8 +157,8 @@ def test_paged_refuses():
     big = paged_shape(columns=100000)
     for mass in (0, 1):
         need = nc.ncodec_paged_attention_workspace_bytes(cache_shape(), big, mass)
-        assert need > 0 or not mass
-        for kw in (dict(ws=0), dict(nb=need - 1), dict(ws=FAR[6] + 16)) if need else ():
+        assert need > 0
+        for kw in (dict(ws=0), dict(nb=need - 1), dict(ws=FAR[6] + 16)):
             assert paged(cache_shape(), big, mass=FAR[9] if mass else 0, **kw) == nc.NCODEC_ENOMEM
 
 
@@ -189,6 +189,12 @@ def test_evict_refuses():
         for name in names:
             if name != out:
                 assert evict(cache_shape(), evict_shape(), **{name: FAR[10], out: FAR[10]}) == nc.NCODEC_EINVAL, (out, name)
+    # a long sequence is shared by workgroups, which meet in the workspace
+    big = evict_shape(columns=100000)
+    need = nc.ncodec_cache_evict_workspace_bytes(cache_shape(), big)
+    assert need > 0 and nc.ncodec_cache_evict_workspace_bytes(cache_shape(), evict_shape(columns=100000, keep=0)) == 0
+    for kw in (dict(ws=0), dict(nb=need - 1), dict(ws=FAR[9] + 16)):
+        assert evict(cache_shape(), big, **kw) == nc.NCODEC_ENOMEM
     nc.ncodec_cache_evict(cache_shape(), evict_shape(batch=0), 0, 0, 0, 0, 0, 0, 0, 0, 0)
 
 

@@ -369,10 +369,15 @@ def test_evict_numbers_that_are_no_page():
     run_evict(2, 200, 2, 64, 64, "fp16", 100, 3, 9, spoil=spoil)
 
 
-def test_evict_long():
-    say("evict long")
-    for kind in ("heavy", "ties"):
-        run_evict(1, 20000, 2, 16, 16, "fp16", 7000, 64, 1000, page=128, kind=kind)
+@pytest.mark.parametrize("kind", ["heavy", "ties", "zeros", "signs", "odd"])
+def test_evict_long(kind):
+    # longer than a workgroup's share of 8192 positions, ends before, at and after it
+    say("evict long", kind)
+    run_evict(1, 20000, 2, 16, 16, "fp16", 7000, 64, 1000, page=128, kind=kind)
+    lengths = [25000, 8191, 8192, 8193, 100, 16384, 0, 24577]
+    run_evict(8, 25000, 1, 8, 8, "bf16", 9000, 0, 0, page=64, lengths=lengths, kind=kind)
+    run_evict(2, 25000, 1, 8, 8, "fp16", 20000, 9000, 10000, page=64, lengths=[25000, 24000], kind=kind)
+    run_evict(2, 17000, 1, 8, 8, "fp16", 9000, 4500, 4500, page=8, lengths=[17000, 9001], kind=kind)
 
 
 def test_evict_of_nothing():
