@@ -1,13 +1,15 @@
-"""A mixer over latent tokens: a layer that sees every earlier frame.
+"""Mixers over latent tokens: layers that see more than the frame before.
 
 The codec's own memory of the past is one frame: the context f_{t-1} and the latent yhat_{t-1} that its prior reads.
 :class:`TokenMixer` reads the decoded latents of a stream as tokens, one per position (t, h, w) of the 1/16 grid, and
 keeps all of them in a state of fixed size (heads x head_dim x head_dim float32), so that a frame costs the same
-however long the stream is.  Encoder and decoder both hold yhat after every frame, so both can run it.  It stands
-beside the codec: what it returns is for the caller, and the codec's own prior, entropy model and bitstream do not
-read it.
+however long the stream is.  :class:`CacheMixer` is the same layer with softmax attention over a window of tokens and
+the first ones, or over the heaviest ones of a budget: an encoder has all tokens of a clip and runs them as a prompt, a
+decoder has them one after the other and keeps their keys and values in the pages of a :class:`TokenCache`.  Encoder
+and decoder both hold yhat after every frame, so both can run them.  They stand beside the codec: what they return is
+for the caller, and the codec's own prior, entropy model and bitstream do not read it.
 
-``python -m paper_2502_20762_amd.mixer`` codes a short synthetic sequence with random-init weights and runs the mixer
+``python -m paper_2502_20762_amd.mixer`` codes a short synthetic sequence with random-init weights and runs both mixers
 beside the encoder.
 """
 from __future__ import annotations
@@ -16,7 +18,8 @@ import math
 
 import torch
 
-from .tokens import decay_attention, grid_positions, linear, qk_norm_rope, rope_frequencies
+from .tokens import (cache_append, cache_evict, decay_attention, grid_positions, linear, paged_attention, qk_norm_rope,
+                     rope_frequencies, window_attention)
 
 
 class TokenMixer:
@@ -65,6 +68,12 @@ class TokenMixer:
     def __call__(self, x, positions, state, lengths=None):
         """x: (batch, tokens, C); positions: (tokens, 3) int32, the same for every stream of the batch; state: moved on
         in place past the tokens; lengths: (batch) int32 tokens of each stream (None: all).  Returns (batch, tokens, C)."""
+        q, k, v = self._project(x, positions)
+        o, _ = decay_attention(q, k, v, self.log_decay, state, lengths, return_state=True, state_out=state)
+        return self._finish(x, o)
+
+    def _project(self, x, positions):
+        """Queries, keys and values of x (batch, tokens, C), normed and rotated, (batch, tokens, heads, dim) each."""
         B, T, C = x.shape
         H, K, D, w = self.H, self.K, self.D, self.w
         qkv = linear(x, w["wqkv"]).view(B * T, H + 2 * K, D)
@@ -73,9 +82,13 @@ class TokenMixer:
             positions = positions.repeat(B, 1)
         qk_norm_rope(q, k, w["q_norm"], w["k_norm"], positions, self.freq, self.sections, q_out=q, k_out=k)
         qkv = qkv.view(B, T, H + 2 * K, D)
-        o, _ = decay_attention(qkv[:, :, :H], qkv[:, :, H:H + K], qkv[:, :, H + K:], self.log_decay, state, lengths,
-                               return_state=True, state_out=state)
-        x = linear(o.view(B, T, H * D), w["wo"], w["bo"], residual=x)
+        return qkv[:, :, :H], qkv[:, :, H:H + K], qkv[:, :, H + K:]
+
+    def _finish(self, x, o):
+        """What follows the attention's output o, (batch, tokens, heads, dim)."""
+        B, T, C = x.shape
+        w = self.w
+        x = linear(o.view(B, T, self.H * self.D), w["wo"], w["bo"], residual=x)
         h = linear(x, w["w1"], w["b1"], act="wsilu", gated=True)
         return linear(h, w["w2"], w["b2"], residual=x)
 
@@ -85,6 +98,95 @@ class TokenMixer:
         x = yhat.reshape(C, h * w).t().contiguous().to(self.dtype)
         y = self(x[None], grid_positions(1, h, w, t0=t, device=self.device), state)
         return y[0].t().reshape(C, h, w)
+
+
+class TokenCache:
+    """Keys and values of the latest tokens of a batch of streams, in pages.
+
+    capacity: tokens of a stream at most.  With ``keep`` every position's attention weights are summed, and a cache
+    that would overflow is cut back to its ``keep`` heaviest tokens first, the first ``sinks`` and the latest
+    ``recent`` among them; ``keep`` has to leave room for the tokens that come at once.  Without it an append that
+    does not fit is refused."""
+
+    def __init__(self, batch, capacity, kv_heads, head_dim, value_dim=None, page_size=16, keep=None, sinks=0, recent=0,
+                 dtype=torch.float16, device="cuda:0"):
+        columns = -(-capacity // page_size)
+        if keep is not None and not 0 < keep < capacity:
+            raise ValueError("keep must be in [1, capacity)")
+        self.capacity, self.keep, self.sinks, self.recent = capacity, keep, sinks, recent
+        self.most = 0  # tokens of the fullest stream at most: known without asking the GPU
+        pages = batch * columns
+        count = 2 * pages if keep is not None else pages  # an eviction copies to pages that are free
+        self.k = torch.zeros((count, page_size, kv_heads, head_dim), dtype=dtype, device=device)
+        self.v = torch.zeros((count, page_size, kv_heads, value_dim or head_dim), dtype=dtype, device=device)
+        tables = torch.arange(count, dtype=torch.int32, device=device).view(-1, batch, columns)
+        self.table, self.free = tables[0], tables[1] if keep is not None else None
+        self.lengths = torch.zeros(batch, dtype=torch.int32, device=device)
+        self.mass = torch.zeros((batch, kv_heads, columns * page_size), device=device) if keep is not None else None
+
+    def append(self, k, v, counts=None):
+        """Adds tokens, k and v (batch, tokens, kv_heads, dim); counts: (batch) int32 of each stream (None: all)."""
+        T = k.shape[1]
+        if self.most + T > self.capacity and self.keep is not None:
+            self.evict()
+        if self.most + T > self.capacity:
+            raise ValueError(f"{T} tokens do not fit a cache of {self.capacity} that may hold {self.most}")
+        cache_append(k, v, self.k, self.v, self.table, self.lengths, counts, self.mass)
+        self.lengths += T if counts is None else counts.clamp(0, T)
+        self.most += T
+
+    def attend(self, q, window=None, sinks=0):
+        """Attention of each stream's last token, q (batch, heads, dim)."""
+        return paged_attention(q, self.k, self.v, self.table, self.lengths, window, sinks, mass=self.mass)
+
+    def evict(self):
+        """Cuts every stream back to its ``keep`` heaviest tokens; returns their old positions."""
+        self.lengths, self.mass, kept = cache_evict(self.k, self.v, self.table, self.lengths, self.mass, self.keep,
+                                                    self.free, self.sinks, self.recent)
+        self.table, self.free = self.free, self.table
+        self.most = min(self.most, self.keep)
+        return kept
+
+
+class CacheMixer(TokenMixer):
+    """The layer of :class:`TokenMixer` with softmax attention: a token sees the latest ``window`` tokens, itself among
+    them (None: all), and the first ``sinks``."""
+
+    def __init__(self, channels, heads=4, kv_heads=None, head_dim=64, expand=2, window=None, sinks=0, **more):
+        super().__init__(channels, heads, kv_heads, head_dim, expand, **more)
+        self.window, self.sinks = window, sinks
+
+    def new_cache(self, capacity, batch=1, page_size=16, keep=None, recent=0):
+        """A cache of streams that have seen nothing; with ``keep`` it holds no window of tokens, but the heaviest."""
+        if keep is not None and self.window is not None:
+            raise ValueError("a cache that keeps the heaviest tokens goes with window=None")
+        return TokenCache(batch, capacity, self.K, self.D, None, page_size, keep, self.sinks, recent, self.dtype, self.device)
+
+    def __call__(self, x, positions, cache=None, lengths=None):
+        """The prompt form: x (batch, tokens, C) are the first tokens of their streams, positions (tokens, 3) int32;
+        lengths: (batch) int32 tokens of each stream (None: all).  ``cache``, empty before, holds them afterwards.
+        Returns (batch, tokens, C)."""
+        q, k, v = self._project(x, positions)
+        if cache is not None:
+            if cache.most:
+                raise ValueError("a prompt begins its streams: the cache must be empty")
+            cache.append(k, v, lengths)
+        return self._finish(x, window_attention(q, k, v, self.window, self.sinks, lengths))
+
+    def step(self, x, position, cache):
+        """The next token of every stream, x (batch, C) at position (1, 3); returns (batch, C)."""
+        x = x[:, None]
+        q, k, v = self._project(x, position)
+        cache.append(k, v)
+        return self._finish(x, cache.attend(q[:, 0], self.window, self.sinks)[:, None])[:, 0]
+
+    def frame(self, yhat, t, cache):
+        """The mixer over the latent of frame t, (C, h, w), token by token; returns the same shape."""
+        C, h, w = yhat.shape
+        x = yhat.reshape(C, h * w).t().contiguous().to(self.dtype)
+        positions = grid_positions(1, h, w, t0=t, device=self.device)
+        y = [self.step(x[i:i + 1], positions[i:i + 1], cache) for i in range(h * w)]
+        return torch.cat(y).t().reshape(C, h, w)
 
 
 def main():
@@ -97,13 +199,17 @@ def main():
     codec = Codec(H, W, C, 2, 2, "fp16", synth.make_weights(C, 2, 2), device=device)
     mixer = TokenMixer(C, device=device)
     state = mixer.new_state()
+    exact = CacheMixer(C, sinks=4, device=device)
+    cache = exact.new_cache(24, keep=16, recent=4)
     for t, frame in enumerate(synth.frame_sequence("tiny")):
         codec.encode(torch.from_numpy(frame).to(device))
         _, yhat = codec.get_state()
         y = mixer.frame(yhat, t, state)
+        z = exact.frame(yhat, t, cache)
         torch.cuda.synchronize()
         print(f"frame {t}: latent {tuple(yhat.shape)}, mixed rms {float(y.float().square().mean().sqrt()):.4f}, "
-              f"state {state.numel() * 4} bytes, rms {float(state.square().mean().sqrt()):.4f}")
+              f"state {state.numel() * 4} bytes, rms {float(state.square().mean().sqrt()):.4f}; over the cache "
+              f"{float(z.float().square().mean().sqrt()):.4f}, {int(cache.lengths[0])} tokens held")
 
 
 if __name__ == "__main__":

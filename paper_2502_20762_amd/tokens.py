@@ -7,8 +7,8 @@ value is computed in the HIP kernels.  They take float16 or bfloat16 tensors and
 contiguous) and raise :class:`ValueError` for tensors that do not fit together, :class:`NcodecError` for what the
 library refuses, outputs that overlap an input or each other among it (parts of one buffer may be given, and what a
 function says may be the same).  They have no backward pass: a tensor that requires a gradient is refused where torch records
-gradients, and taken under ``torch.no_grad()``.  :class:`TokenMixer` runs them together: a layer
-that reads the latents of all earlier frames through a state of fixed size.
+gradients, and taken under ``torch.no_grad()``.  ``TokenMixer`` and ``CacheMixer`` run them together: layers that
+read the latents of earlier frames through a state of fixed size, and through a cache of their keys and values.
 """
 from __future__ import annotations
 
@@ -270,24 +270,27 @@ def _window(window):
 def _cache(dtype, device, k_cache, v_cache):
     """The descriptor of a cache; k_cache: (pages, page_size, kv_heads, dim), v_cache likewise."""
     ks, vs = k_cache.shape, v_cache.shape
-    _need(len(ks) == 4 and len(vs) == 4, "k_cache and v_cache must be (pages, page_size, kv_heads, dim)")
+    if len(ks) != 4 or len(vs) != 4:
+        raise ValueError("k_cache and v_cache must be (pages, page_size, kv_heads, dim)")
     _like(k_cache, dtype, device, ks, "k_cache")
     _like(v_cache, dtype, device, (*ks[:3], vs[3]), "v_cache")
-    return _nc.ncodec_cache_shape(_DTYPES[dtype], ks[2], ks[3], vs[3], ks[1], 0, ks[0], *k_cache.stride()[:3],
-                                  *v_cache.stride()[:3])
+    a, b = k_cache.stride(), v_cache.stride()
+    return _nc.ncodec_cache_shape(_DTYPES[dtype], ks[2], ks[3], vs[3], ks[1], 0, ks[0], a[0], a[1], a[2], b[0], b[1], b[2])
 
 
 def _table(table, device, batch, what):
     """Columns and row stride of a table of page numbers, (batch, columns) int32."""
     shape = table.shape
-    _need(len(shape) == 2, f"{what} must be (batch, columns)")
+    if len(shape) != 2:
+        raise ValueError(f"{what} must be (batch, columns)")
     _like(table, torch.int32, device, (batch, shape[1]), what)
     return shape[1], table.stride(0)
 
 
 def _mass(mass, device, shape, what="mass"):
     _like(mass, torch.float32, device, shape, what)
-    _need(mass.is_contiguous(), f"{what} must be contiguous")
+    if not mass.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
 
 
 def paged_attention(q, k_cache, v_cache, page_table, lengths, window=None, sinks=0, scale=None, mass=None, out=None):
