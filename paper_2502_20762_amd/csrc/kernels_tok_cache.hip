@@ -15,25 +15,19 @@ namespace {
 constexpr int kUnits = 8, kMaxRows = 128;
 
 struct Split {
-  int rows;              // of a workgroup
-  int uk, uv;            // units of a head's key and value
-  uint64_t row, k, v;    // ceil(2^32 / units of a row, uk, uv): quotients of indices below 2^26
+  int rows;            // of a workgroup
+  int dk, dv, uk, uv;  // elements and units of a head's key and value
+  uint64_t row, k, v;  // ceil(2^32 / units of a row, uk, uv): quotients of indices below 2^26
 };
 __device__ __forceinline__ int quotient(uint32_t i, uint64_t magic) { return (int)((i * magic) >> 32); }
 
-template <int U>
-struct Unit {
-  typedef uint16_t T __attribute__((ext_vector_type(U)));
-};
-template <>
-struct Unit<1> {
-  typedef uint16_t T;
-};
-
-// from(r, h, v), to(r, h, v): first element of row r's head h, key or value, or NULL.
-template <int U, class From, class To>
+// from(r, h, v), to(r, h, v): first element of row r's head h, key or value, or NULL.  A
+// head's last unit ends with it: where its elements are no multiple of U it moves
+// some of the unit before once more.
+template <int U, bool ALIGNED, class From, class To>
 __device__ __forceinline__ void move_rows(const Split& s, int rows, int heads, From from, To to) {
-  typedef typename Unit<U>::T T;
+  typedef uint16_t T __attribute__((ext_vector_type(U == 1 ? 2 : U)));
+  typedef T Loose __attribute__((aligned(2)));
   const int per = heads * (s.uk + s.uv), all = rows * per;
   for (int i0 = threadIdx.x; i0 < all; i0 += kUnits * 256) {
     T v[kUnits];
@@ -49,27 +43,44 @@ __device__ __forceinline__ void move_rows(const Split& s, int rows, int heads, F
       uint16_t* dst = to(r, h, value);
       const uint16_t* src = from(r, h, value);
       if (!dst || !src) continue;
-      p[x] = dst + U * u;
-      v[x] = *(const T*)(src + U * u);
+      const int d = ALIGNED ? U * u : min(U * u, (value ? s.dv : s.dk) - U);
+      p[x] = dst + d;
+      if (U == 1)
+        v[x][0] = src[d];
+      else if (ALIGNED)
+        v[x] = *(const T*)(src + d);
+      else
+        __builtin_memcpy(&v[x], src + d, sizeof(T));
     }
 #pragma unroll
-    for (int x = 0; x < kUnits; ++x)
-      if (p[x]) *(T*)p[x] = v[x];
+    for (int x = 0; x < kUnits; ++x) {
+      if (!p[x]) continue;
+      // device memory, which the compiler does not see behind the NULL
+      if (U == 1)
+        *(__attribute__((address_space(1))) uint16_t*)p[x] = v[x][0];
+      else if (ALIGNED)
+        *(__attribute__((address_space(1))) T*)p[x] = v[x];
+      else
+        *(__attribute__((address_space(1))) Loose*)p[x] = v[x];
+    }
   }
 }
 
-// Units of so many elements as all rows and strides are made of, and rows for two
-// thousand units a workgroup.
-int unit_of(std::initializer_list<int64_t> sizes, std::initializer_list<const void*> bases) {
+// Units of 16 bytes wherever heads are that wide, at the alignment of an element where
+// bases or strides are no better (33,011 tokens of 3 sequences, 4 heads of 75 and 128: 275 us
+// in single elements).
+bool runs(std::initializer_list<int64_t> sizes, std::initializer_list<const void*> bases) {
   int64_t all = 0;
   for (int64_t v : sizes) all |= v;
   for (const void* p : bases) all |= (int64_t)((uintptr_t)p / 2);
-  return all % 8 == 0 ? 8 : all % 2 == 0 ? 2 : 1;
+  return all % 8 == 0;
 }
 Split split_of(const ncodec_cache_shape& c, int heads, int unit, int64_t rows) {
   Split s;
-  s.uk = c.head_dim / unit;
-  s.uv = c.value_dim / unit;
+  s.dk = c.head_dim;
+  s.dv = c.value_dim;
+  s.uk = (c.head_dim + unit - 1) / unit;
+  s.uv = (c.value_dim + unit - 1) / unit;
   const int64_t per = (int64_t)heads * (s.uk + s.uv);
   s.rows = (int)std::max<int64_t>(1, std::min<int64_t>({2048 / per, kMaxRows, rows}));
   const auto magic = [](uint64_t d) { return (((uint64_t)1 << 32) + d - 1) / d; };
@@ -79,7 +90,7 @@ Split split_of(const ncodec_cache_shape& c, int heads, int unit, int64_t rows) {
   return s;
 }
 
-template <int U>
+template <int U, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_tok_append(AppendArgs a, Split sp, int64_t first, int64_t blocks) {
   __shared__ int64_t page[kMaxRows];  // -1: the token goes nowhere
   __shared__ int line[kMaxRows];
@@ -104,7 +115,7 @@ __global__ __launch_bounds__(256) void k_tok_append(AppendArgs a, Split sp, int6
   __syncthreads();
   const uint16_t* k = (const uint16_t*)a.k + b * s.k_batch_stride + i0 * s.k_token_stride;
   const uint16_t* v = (const uint16_t*)a.v + b * s.v_batch_stride + i0 * s.v_token_stride;
-  move_rows<U>(
+  move_rows<U, ALIGNED>(
       sp, rows, c.kv_heads,
       [&](int r, int h, bool value) {
         return value ? v + r * s.v_token_stride + h * s.v_head_stride : k + r * s.k_token_stride + h * s.k_head_stride;
@@ -117,7 +128,7 @@ __global__ __launch_bounds__(256) void k_tok_append(AppendArgs a, Split sp, int6
       });
 }
 
-template <int U>
+template <int U, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_tok_evict_move(EvictArgs a, Split sp, int64_t first, int64_t blocks) {
   __shared__ int64_t from[kMaxRows], to[kMaxRows];  // pages; to -1: not copied
   __shared__ int from_line[kMaxRows], to_line[kMaxRows];
@@ -144,7 +155,7 @@ __global__ __launch_bounds__(256) void k_tok_evict_move(EvictArgs a, Split sp, i
   }
   __syncthreads();
   uint16_t *k = (uint16_t*)a.k_cache + h * c.k_head_stride, *v = (uint16_t*)a.v_cache + h * c.v_head_stride;
-  move_rows<U>(
+  move_rows<U, ALIGNED>(
       sp, rows, 1,
       [&](int r, int, bool value) -> const uint16_t* {
         if (to[r] < 0) return nullptr;
@@ -417,24 +428,24 @@ __global__ __launch_bounds__(1024) void k_tok_evict_round(PickRun run, int64_t f
   write_kept(a, bh, p, ch, j0, segment, S, w, u, lds);
 }
 
-template <int U>
+template <int U, bool ALIGNED>
 hipError_t append(const AppendArgs& a, hipStream_t st) {
   const Split sp = split_of(a.c, a.c.kv_heads, U, a.s.tokens);
   const int64_t blocks = (a.s.tokens + sp.rows - 1) / sp.rows, all = a.s.batch * blocks;
   // a launch counts its threads in 32 bits
   for (int64_t first = 0; first < all; first += 1 << 23) {
-    launch(k_tok_append<U>, dim3((unsigned)std::min<int64_t>(all - first, 1 << 23)), dim3(256), st, a, sp, first, blocks);
+    launch(k_tok_append<U, ALIGNED>, dim3((unsigned)std::min<int64_t>(all - first, 1 << 23)), dim3(256), st, a, sp, first, blocks);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
-template <int U>
+template <int U, bool ALIGNED>
 hipError_t move(const EvictArgs& a, hipStream_t st) {
   const Split sp = split_of(a.c, 1, U, a.s.keep);
   const int64_t blocks = (a.s.keep + sp.rows - 1) / sp.rows, all = a.s.batch * a.c.kv_heads * blocks;
   for (int64_t first = 0; first < all; first += 1 << 23) {
-    launch(k_tok_evict_move<U>, dim3((unsigned)std::min<int64_t>(all - first, 1 << 23)), dim3(256), st, a, sp, first, blocks);
+    launch(k_tok_evict_move<U, ALIGNED>, dim3((unsigned)std::min<int64_t>(all - first, 1 << 23)), dim3(256), st, a, sp, first, blocks);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -478,11 +489,12 @@ size_t hist_bytes(const ncodec_cache_shape& c, const ncodec_evict_shape& s, int6
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t st) {
   const ncodec_cache_shape& c = a.c;
   const ncodec_append_shape& s = a.s;
-  const int unit = unit_of({c.head_dim, c.value_dim, c.k_page_stride, c.k_token_stride, c.k_head_stride, c.v_page_stride,
-                            c.v_token_stride, c.v_head_stride, s.k_batch_stride, s.k_token_stride, s.k_head_stride,
-                            s.v_batch_stride, s.v_token_stride, s.v_head_stride},
-                           {a.k, a.v, a.k_cache, a.v_cache});
-  return unit == 8 ? append<8>(a, st) : unit == 2 ? append<2>(a, st) : append<1>(a, st);
+  if (c.head_dim < 8 || c.value_dim < 8) return append<1, false>(a, st);
+  const bool aligned = runs({c.head_dim, c.value_dim, c.k_page_stride, c.k_token_stride, c.k_head_stride, c.v_page_stride,
+                             c.v_token_stride, c.v_head_stride, s.k_batch_stride, s.k_token_stride, s.k_head_stride,
+                             s.v_batch_stride, s.v_token_stride, s.v_head_stride},
+                            {a.k, a.v, a.k_cache, a.v_cache});
+  return aligned ? append<8, true>(a, st) : append<8, false>(a, st);
 }
 
 size_t evict_workspace_bytes(const ncodec_cache_shape& c, const ncodec_evict_shape& s) {
@@ -507,10 +519,11 @@ hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st) {
     if (e == hipSuccess) e = round<3>(run, bk * segments, st);
   }
   if (e != hipSuccess) return e;
-  const int unit = unit_of({c.head_dim, c.value_dim, c.k_page_stride, c.k_token_stride, c.k_head_stride, c.v_page_stride,
-                            c.v_token_stride, c.v_head_stride},
-                           {a.k_cache, a.v_cache});
-  return unit == 8 ? move<8>(a, st) : unit == 2 ? move<2>(a, st) : move<1>(a, st);
+  if (c.head_dim < 8 || c.value_dim < 8) return move<1, false>(a, st);
+  const bool aligned = runs({c.head_dim, c.value_dim, c.k_page_stride, c.k_token_stride, c.k_head_stride, c.v_page_stride,
+                             c.v_token_stride, c.v_head_stride},
+                            {a.k_cache, a.v_cache});
+  return aligned ? move<8, true>(a, st) : move<8, false>(a, st);
 }
 
 }  // namespace nc

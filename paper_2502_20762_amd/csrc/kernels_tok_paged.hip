@@ -55,24 +55,19 @@ __device__ __forceinline__ Steps steps_of(const Seen& s, int n) {
 }
 
 // N elements from p; those from `left` on, or all where !in, are zero.  VEC: whole
-// runs only, aligned to them.
+// runs only, aligned to them; otherwise whole runs lie where they may, and a row's last,
+// shorter one goes element by element.
 template <int N, bool VEC>
 __device__ __forceinline__ void load_run(uint32_t (&r)[N / 2], const uint16_t* p, bool in, int left) {
+  typedef uint32_t V __attribute__((ext_vector_type(N / 2)));
+  typedef V Loose __attribute__((aligned(2)));
 #pragma unroll
   for (int i = 0; i < N / 2; ++i) r[i] = 0;
-  if (VEC) {
-    if (in && left >= N) {
-      if (N == 8) {
-        const intx4 v = *(const intx4*)p;
+  if (in && left >= N) {
+    const V v = VEC ? *(const V*)p : *(const Loose*)p;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i % (N / 2)] = (uint32_t)v[i];
-      } else {
-        const intx2 v = *(const intx2*)p;
-        r[0] = (uint32_t)v[0];
-        r[1] = (uint32_t)v[1];
-      }
-    }
-  } else if (in) {
+    for (int i = 0; i < N / 2; ++i) r[i] = v[i];
+  } else if (!VEC && in && left > 0) {
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (i < left) r[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
