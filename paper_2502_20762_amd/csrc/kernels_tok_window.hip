@@ -10,6 +10,7 @@
 
 #include "tok_attend.hpp"
 #include "tok_tiles.hpp"
+#include "token_rules.hpp"
 
 namespace nc {
 namespace {
@@ -116,8 +117,9 @@ __device__ __forceinline__ bool any_not_finite(const V8 (&v)[4], uint32_t inf) {
   return __any(top >= inf);
 }
 
-// DP: padded head width, NV: 32-column tiles of the values.
-template <class E, int DP, int NV, bool DMA>
+// DP: padded head width, NV: 32-column tiles of the values.  KS: tiles of a round, each for
+// waves of its own, which join at the end.
+template <class E, int DP, int NV, bool DMA, int KS>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void k_tok_window(WindowRun run) {
   typedef typename E::T T;
   typedef typename E::V8 V8;
@@ -130,7 +132,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   // maximum, so that outputs are seldom rescaled: fp16 terms stay below 2^15 and keep the
   // bits above 2^-32 of the largest weight, bf16 ones leave room for 2^31 tokens.
   constexpr float off = F ? 7.f : -40.f, lag = 8.f;
-  __shared__ __align__(1024) char lds[2 * STAGE];
+  __shared__ __align__(1024) char lds[2 * KS * STAGE];
   const WindowArgs& a = run.a;
   const ncodec_window_shape& s = a.s;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -144,11 +146,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   at /= (uint32_t)run.head_tiles;
   const int hk = at % (uint32_t)s.kv_heads;
   const int64_t b = at / (uint32_t)s.kv_heads;
-  const int qw = kWaves / run.head_waves;  // waves along the queries
-  const int hd = hk * group + ht * run.head_waves + wave % run.head_waves;
+  const int ks = wave / (kWaves / KS), qwave = wave % (kWaves / KS);
+  const int qw = kWaves / KS / run.head_waves;  // waves along the queries
+  const int hd = hk * group + ht * run.head_waves + qwave % run.head_waves;
   const int64_t len = a.lengths ? min(max((int64_t)a.lengths[b], (int64_t)0), s.tokens) : s.tokens;
   const int i0 = qb * qw * kQueries;                                     // the workgroup's first query
-  const int wi0 = i0 + wave / run.head_waves * kQueries, i = wi0 + l32;  // the wave's, the lane's
+  const int wi0 = i0 + qwave / run.head_waves * kQueries, i = wi0 + l32;  // the wave's, the lane's
   const int iend = (int)min((int64_t)i0 + qw * kQueries, len);           // behind its last one
   const int wend = (int)min((int64_t)wi0 + kQueries, len);
 
@@ -181,10 +184,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       return x * kTile;
     };
     const auto stage = [&](int t) {
-      char* to = lds + (t & 1) * STAGE;
-      const int j0 = key0(t), rows = (int)min((int64_t)kTile, len - j0);
-      stage_tile<E, DP, DMA>(to, k + (int64_t)j0 * s.k_token_stride, s.k_token_stride, rows, D, wave, lane);
-      stage_tile<E, VW, DMA>(to + KB, v + (int64_t)j0 * s.v_token_stride, s.v_token_stride, rows, V, wave, lane);
+#pragma unroll
+      for (int x = 0; x < KS; ++x) {
+        if (t + x >= tiles) break;
+        char* to = lds + ((t / KS & 1) * KS + x) * STAGE;
+        const int j0 = key0(t + x), rows = (int)min((int64_t)kTile, len - j0);
+        stage_tile<E, DP, DMA>(to, k + (int64_t)j0 * s.k_token_stride, s.k_token_stride, rows, D, wave, lane);
+        stage_tile<E, VW, DMA>(to + KB, v + (int64_t)j0 * s.v_token_stride, s.v_token_stride, rows, V, wave, lane);
+      }
     };
     stage(0);
 
@@ -274,12 +281,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
     int t = 0;
-    for (; t < whole; ++t) {
-      // every wave's loads of tile t have landed (each waited for its own), and every
+    for (; t + KS <= whole; t += KS) {
+      // every wave's loads of this round have landed (each waited for its own), and every
       // wave is done with the other buffer
       lds_barrier();
-      if (t + 1 < tiles) stage(t + 1);
-      const char* kt = lds + (t & 1) * STAGE;
+      if (t + KS < tiles) stage(t + KS);
+      const char* kt = lds + ((t / KS & 1) * KS + ks) * STAGE;
       const char* vt = kt + KB;
       floatx16 cur[2];
       __builtin_amdgcn_s_setprio(1);
@@ -309,13 +316,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       __builtin_amdgcn_s_setprio(0);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
-    for (; t < tiles; ++t) {
+    for (; t < tiles; t += KS) {
       lds_barrier();
-      if (t + 1 < tiles) stage(t + 1);
-      const char* kt = lds + (t & 1) * STAGE;
+      if (t + KS < tiles) stage(t + KS);
+      const char* kt = lds + ((t / KS & 1) * KS + ks) * STAGE;
       const char* vt = kt + KB;
-      const int j0 = key0(t);
-      if (some(j0)) {
+      const int j0 = key0(min(t + ks, tiles - 1));
+      if (t + ks < tiles && some(j0)) {
         const bool all = j0 + kTile - 1 <= wi0 && (wi0 + kQueries - 1 - j0 < window || j0 + kTile <= sinks);
         floatx16 cur[2];
         __builtin_amdgcn_s_setprio(1);
@@ -376,11 +383,40 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       __builtin_amdgcn_s_setprio(0);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
+    if (KS > 1) {
+      // the second half's maximum, sum and outputs, lane by lane
+      float* mine = (float*)lds + (qwave * 64 + lane) * 4;  // and 16 outputs at a time, 16 bytes a lane
+      constexpr int STEP = kWaves / KS * 64 * 4;
+      lds_barrier();
+      if (ks) {
+        *(floatx4*)mine = floatx4{mc, base, sum, 0.f};
+#pragma unroll
+        for (int x = 0; x < 4 * NV; ++x)
+          *(floatx4*)(mine + (x + 1) * STEP) =
+              floatx4{out[x / 4][x % 4 * 4], out[x / 4][x % 4 * 4 + 1], out[x / 4][x % 4 * 4 + 2], out[x / 4][x % 4 * 4 + 3]};
+      }
+      lds_barrier();
+      if (ks) return;
+      const floatx4 other = *(const floatx4*)mine;
+      const float none = -__builtin_huge_valf();
+      const float b1 = mc == none ? other[1] : other[0] == none ? base : fmaxf(base, other[1]);
+      // what saw no score above -inf counts nothing, but for a NaN
+      const float f0 = mc == none ? (sum != sum ? 1.f : 0.f) : __builtin_amdgcn_exp2f(base - b1);
+      const float f1 = other[0] == none ? (other[2] != other[2] ? 1.f : 0.f) : __builtin_amdgcn_exp2f(other[1] - b1);
+      sum = sum * f0 + other[2] * f1;
+#pragma unroll
+      for (int x = 0; x < 4 * NV; ++x) {
+        const floatx4 w = *(const floatx4*)(mine + (x + 1) * STEP);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[x / 4][x % 4 * 4 + e] = out[x / 4][x % 4 * 4 + e] * f0 + w[e] * f1;
+      }
+    }
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
     sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
     // a token sees itself: without any weight its scores are all -inf, and no weight is a number
     sum = sum == 0.f ? __builtin_nanf("") : 1.f / sum;
   }
+  if (KS > 1 && ks) return;
   if (i >= s.tokens) return;
   const bool live = i < len;
   // A lane has four consecutive values four times for each 32, its neighbour l ^ 32 the
@@ -413,25 +449,36 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     }
 }
 
-template <class E, int DP, int NV, bool DMA>
+template <class E, int DP, int NV, bool DMA, int KS>
 hipError_t go(WindowRun run, hipStream_t st) {
   const ncodec_window_shape& s = run.a.s;
+  const int group = s.heads / s.kv_heads, waves = kWaves / KS;
+  run.head_waves = group % waves == 0 ? waves : group % 2 == 0 ? 2 : 1;
+  run.head_tiles = group / run.head_waves;
+  const int64_t queries = kQueries * (waves / run.head_waves);
+  run.query_blocks = (int)((s.tokens + queries - 1) / queries);
   const int64_t blocks = s.batch * s.kv_heads * run.head_tiles * run.query_blocks;
   // a launch counts its threads in 32 bits
   for (; run.first < blocks; run.first += 1 << 23) {
-    launch(k_tok_window<E, DP, NV, DMA>, dim3((unsigned)std::min<int64_t>(blocks - run.first, 1 << 23)), dim3(64 * kWaves), st, run);
+    launch(k_tok_window<E, DP, NV, DMA, KS>, dim3((unsigned)std::min<int64_t>(blocks - run.first, 1 << 23)), dim3(64 * kWaves), st, run);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
+template <class E, int DP, int NV, bool DMA>
+hipError_t by_blocks(const WindowRun& run, hipStream_t st) {
+  const ncodec_window_shape& s = run.a.s;
+  return window_halves(s.batch * s.heads, s.tokens, s.head_dim, s.value_dim) ? go<E, DP, NV, DMA, 2>(run, st)
+                                                                             : go<E, DP, NV, DMA, 1>(run, st);
+}
 template <class E, int DP, bool DMA>
 hipError_t by_value(const WindowRun& run, hipStream_t st) {
   const int V = run.a.s.value_dim;
-  if (V <= 32) return go<E, DP, 1, DMA>(run, st);
-  if (V <= 64) return go<E, DP, 2, DMA>(run, st);
-  if (V <= 96) return go<E, DP, 3, DMA>(run, st);
-  return go<E, DP, 4, DMA>(run, st);
+  if (V <= 32) return by_blocks<E, DP, 1, DMA>(run, st);
+  if (V <= 64) return by_blocks<E, DP, 2, DMA>(run, st);
+  if (V <= 96) return by_blocks<E, DP, 3, DMA>(run, st);
+  return by_blocks<E, DP, 4, DMA>(run, st);
 }
 template <class E>
 hipError_t run_window(const WindowArgs& a, hipStream_t st) {
@@ -439,9 +486,7 @@ hipError_t run_window(const WindowArgs& a, hipStream_t st) {
   const auto runs = [](const void* x, int64_t batch, int64_t token, int64_t head) {
     return (uintptr_t)x % 16 == 0 && batch % 8 == 0 && token % 8 == 0 && head % 8 == 0;
   };
-  const int group = s.heads / s.kv_heads, head_waves = group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
-  const int64_t queries = kQueries * (kWaves / head_waves);
-  const WindowRun run{a, 0, head_waves, group / head_waves, (int)((s.tokens + queries - 1) / queries),
+  const WindowRun run{a, 0, 0, 0, 0,
                       s.head_dim % 8 == 0 && runs(a.q, s.q_batch_stride, s.q_token_stride, s.q_head_stride)};
   const bool dma = s.head_dim % 8 == 0 && s.value_dim % 8 == 0 && runs(a.k, s.k_batch_stride, s.k_token_stride, s.k_head_stride) &&
                    runs(a.v, s.v_batch_stride, s.v_token_stride, s.v_head_stride) && s.k_token_stride < (1 << 26) &&

@@ -86,4 +86,18 @@ inline DecayPlan decay_rule(int64_t bh, int64_t tokens, int64_t value_dim) {
   return p;
 }
 
+// ---- attention with a window
+// Whether a workgroup's four waves share 64 queries, two waves a query on alternate tiles
+// of keys, instead of 128: twice the workgroups, of half the length, for up to twice the
+// loads of keys and values.  bh: batch * heads.  us whole / in halves, 64 x 64 heads, all
+// earlier tokens seen: 8 heads of 200 tokens 10.8 / 8.9, 1560 32 / 21, 8160 159 / 135, 16,000 with
+// a window of 4080 (1000 workgroups of 128 queries) 226 / 224.  With wider heads the tiles in
+// halves leave room for one workgroup a CU: 128 x 128, 8 heads over 2 of 1560 tokens (104
+// workgroups) 43 / 29, 16 over 4 of 3000 (384) 86 / 91, 8 of 8160 with a window of 2000 (512)
+// 108 / 146.  Up to 64 tokens there is but one tile.
+inline bool window_halves(int64_t bh, int64_t tokens, int64_t head_dim, int64_t value_dim) {
+  const int64_t blocks = bh * ((tokens + 127) / 128);
+  return tokens > 64 && blocks <= (head_dim <= 64 && value_dim <= 64 ? 1000 : 256);
+}
+
 }  // namespace nc

@@ -91,6 +91,68 @@ def test_long(T, H, K, D, V, window, sinks, dt):
     run(1, T, H, K, D, V, dt, window, sinks)
 
 
+# padded widths, direct loads or not, and each with waves that share queries in halves or not: (batch, heads, kv_heads, head
+# width, value width)
+FORMS = {(D, V, halves): (B, H, K, D, V)
+         for D in (64, 33, 128, 75) for V in (32, 64, 33, 96, 128, 100)
+         for halves, B, H, K in ((True, 2, 4, 1), (False, 17 if D <= 64 and V <= 64 else 5, 32, 8))}
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_every_form(form):
+    say("window form", form)
+    B, H, K, D, V = FORMS[form]
+    run(B, 130 if form[2] else 129, H, K, D, V, "fp16" if V % 64 else "bf16", 70, 3)
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("what", [INF, NAN])
+def test_what_is_not_finite_where_waves_do_not_share_queries(what, dt):
+    g = gen(12)
+    B, T, H, K = 5, 150, 32, 8
+    x = [rnd(g, (B, T, h, 128), dt) for h in (H, K, K)]
+    clean = tk.window_attention(*(t.to(DEV) for t in x), 60, 4).cpu()
+    for i, at in ((1, 70), (2, 70), (2, 1), (2, 149)):
+        y = [t.clone() for t in x]
+        y[i][1, at, 5, 40] = what
+        o = tk.window_attention(*(t.to(DEV) for t in y), 60, 4).cpu()
+        hit = torch.zeros((B, T, H, 128), dtype=torch.bool)
+        seen = torch.arange(T) >= at
+        if at >= 4:
+            seen &= torch.arange(T) < at + 60
+        hit[1, seen, 20:24] = True
+        if i == 2:
+            hit &= torch.arange(128) == 40
+        fine = torch.isfinite(o)
+        if i == 2:
+            assert torch.equal(fine, ~hit), (i, at)
+        else:  # a score of -inf takes its token away, all others end the mean
+            assert bool(fine[~hit].all()) and not bool(fine[hit].all())
+        assert torch.equal(o[~hit], clean[~hit])
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+def test_stretches_of_minus_infinity_and_nan_between_the_halves(dt):
+    # tiles of 64 keys go to the two waves of a query in turn: whole tiles of one of them, or all of its own
+    T = 500
+    q = torch.ones((1, T, 1, 64), device=DEV).to(torch.float16 if dt == "fp16" else torch.bfloat16)
+    v = rnd(gen(13), (1, T, 1, 64), dt).to(DEV)
+    tile = torch.arange(T, device=DEV) // 64
+    for gone in (tile % 2 == 0, tile % 2 == 1, tile < 3, tile == 7, tile < 8):
+        k = torch.ones_like(q)
+        k[0, gone] = -INF
+        o = tk.window_attention(q, k, v, scale=0.01)
+        with np.errstate(invalid="ignore"):
+            want = ref.window_attention(f64(q), f64(k), f64(v), scale=0.01)
+        assert np.array_equal(np.isfinite(f64(o)), np.isfinite(want))
+        fine = np.isfinite(want)
+        assert np.abs(f64(o) - want)[fine].max(initial=0) <= 2 * U[dt] * np.abs(f64(v)).max()
+        k[0, gone] = NAN
+        o = tk.window_attention(q, k, v, scale=0.01)
+        first = int(gone.nonzero()[0])
+        assert torch.isnan(o[0, first:]).all() and torch.isfinite(o[0, :first]).all()
+
+
 @pytest.mark.parametrize("dt", ["fp16", "bf16"])
 def test_peaked_and_flat_weights(dt):
     # scores of some hundreds: one token takes all; scale 0: all weigh the same
@@ -171,6 +233,15 @@ def test_padding_is_not_used(T):
         x[0, T - 23:], x[1, 5:] = NAN, INF
     b = tk.window_attention(q, k, v, 50, 3, ln)
     assert torch.equal(a, b) and torch.isfinite(a).all()
+
+
+def test_a_sequence_does_not_depend_on_the_others_of_its_batch():
+    # bit for bit, where the same number of workgroups takes both
+    g = gen(14)
+    q, k, v = (rnd(g, (4, 200, 2, 64), "bf16").to(DEV) for _ in range(3))
+    whole = tk.window_attention(q, k, v, 90, 10)
+    q[[0, 2, 3]], k[[0, 2, 3]], v[[0, 2, 3]] = 3 * q[[2, 3, 0]], -k[[3, 0, 2]], v[[3, 0, 2]]
+    assert torch.equal(tk.window_attention(q, k, v, 90, 10)[1], whole[1])
 
 
 def test_each_sequence_by_itself_and_prefixes_agree():
