@@ -3,6 +3,7 @@
 // tokens to keep is a radix selection in three rounds of 11, 11 and 10 bits.
 #include <algorithm>
 
+#include "token_rules.hpp"
 #include "tokens.hpp"
 
 namespace nc {
@@ -29,12 +30,13 @@ __device__ __forceinline__ void move_rows(const Split& s, int rows, int heads, F
   typedef uint16_t T __attribute__((ext_vector_type(U == 1 ? 2 : U)));
   typedef T Loose __attribute__((aligned(2)));
   const int per = heads * (s.uk + s.uv), all = rows * per;
-  for (int i0 = threadIdx.x; i0 < all; i0 += kUnits * 256) {
+  const int threads = blockDim.x;
+  for (int i0 = threadIdx.x; i0 < all; i0 += kUnits * threads) {
     T v[kUnits];
     uint16_t* p[kUnits];
 #pragma unroll
     for (int x = 0; x < kUnits; ++x) {
-      const int i = i0 + 256 * x;
+      const int i = i0 + threads * x;
       p[x] = nullptr;
       if (i >= all) continue;
       const int r = s.rows == 1 ? 0 : quotient(i, s.row), q = i - r * per;
@@ -128,48 +130,57 @@ __global__ __launch_bounds__(256) void k_tok_append(AppendArgs a, Split sp, int6
       });
 }
 
+// Rows of positions x0 .. x0 + rows - 1 of a sequence's head, to the new pages.
+struct Places {
+  int64_t from[kMaxRows], to[kMaxRows];  // pages; to -1: not copied
+  int from_line[kMaxRows], to_line[kMaxRows];
+};
 template <int U, bool ALIGNED>
-__global__ __launch_bounds__(256) void k_tok_evict_move(EvictArgs a, Split sp, int64_t first, int64_t blocks) {
-  __shared__ int64_t from[kMaxRows], to[kMaxRows];  // pages; to -1: not copied
-  __shared__ int from_line[kMaxRows], to_line[kMaxRows];
+__device__ __forceinline__ void move_kept(const EvictArgs& a, const Split& sp, Places& at, int64_t bh, int64_t x0, int rows) {
   const ncodec_cache_shape& c = a.c;
   const ncodec_evict_shape& s = a.s;
-  const int64_t block = first + blockIdx.x, bh = block / blocks, x0 = block % blocks * sp.rows, b = bh / c.kv_heads;
-  const int h = (int)(bh % c.kv_heads), rows = (int)min((int64_t)sp.rows, s.keep - x0);
+  const int64_t b = bh / c.kv_heads;
+  const int h = (int)(bh % c.kv_heads), shift = __ffs(c.page_size) - 1;
   const int32_t* kept = a.kept + bh * s.keep + x0;
-  if (kept[0] < 0) return;  // the kept ones come first
-  if ((int)threadIdx.x < rows) {
-    const int32_t j = kept[threadIdx.x];
-    const int64_t x = x0 + threadIdx.x;
-    const int shift = __ffs(c.page_size) - 1;
+  for (int r = threadIdx.x; r < rows; r += blockDim.x) {
+    const int32_t j = kept[r];
+    const int64_t x = x0 + r;
     int64_t p = -1, q = -1;
     if (j >= 0) {
       p = a.table[b * s.table_stride + (j >> shift)];
       q = a.new_table[b * s.new_table_stride + (x >> shift)];
       if (p < 0 || p >= c.pages || q < 0 || q >= c.pages) q = -1;
     }
-    from[threadIdx.x] = p;
-    to[threadIdx.x] = q;
-    from_line[threadIdx.x] = j & (c.page_size - 1);
-    to_line[threadIdx.x] = (int)(x & (c.page_size - 1));
+    at.from[r] = p;
+    at.to[r] = q;
+    at.from_line[r] = j & (c.page_size - 1);
+    at.to_line[r] = (int)(x & (c.page_size - 1));
   }
   __syncthreads();
   uint16_t *k = (uint16_t*)a.k_cache + h * c.k_head_stride, *v = (uint16_t*)a.v_cache + h * c.v_head_stride;
   move_rows<U, ALIGNED>(
       sp, rows, 1,
       [&](int r, int, bool value) -> const uint16_t* {
-        if (to[r] < 0) return nullptr;
-        return value ? v + from[r] * c.v_page_stride + from_line[r] * c.v_token_stride
-                     : k + from[r] * c.k_page_stride + from_line[r] * c.k_token_stride;
+        if (at.to[r] < 0) return nullptr;
+        return value ? v + at.from[r] * c.v_page_stride + at.from_line[r] * c.v_token_stride
+                     : k + at.from[r] * c.k_page_stride + at.from_line[r] * c.k_token_stride;
       },
       [&](int r, int, bool value) {
-        return value ? v + to[r] * c.v_page_stride + to_line[r] * c.v_token_stride
-                     : k + to[r] * c.k_page_stride + to_line[r] * c.k_token_stride;
+        return value ? v + at.to[r] * c.v_page_stride + at.to_line[r] * c.v_token_stride
+                     : k + at.to[r] * c.k_page_stride + at.to_line[r] * c.k_token_stride;
       });
 }
 
+template <int U, bool ALIGNED>
+__global__ __launch_bounds__(256) void k_tok_evict_move(EvictArgs a, Split sp, int64_t first, int64_t blocks) {
+  __shared__ Places at;
+  const int64_t block = first + blockIdx.x, bh = block / blocks, x0 = block % blocks * sp.rows;
+  if (a.kept[bh * a.s.keep + x0] < 0) return;  // the kept ones come first
+  move_kept<U, ALIGNED>(a, sp, at, bh, x0, (int)min((int64_t)sp.rows, a.s.keep - x0));
+}
+
 // ---- which tokens are kept --------------------------------------------------
-constexpr int kBins = 2048, kMost = 8, kSegment = 1024 * kMost;  // positions of a thread, of a workgroup, at most
+constexpr int kBins = 2048, kMost = 8;  // kMost: positions of a thread at most
 constexpr int kShift[3] = {21, 10, 0};                           // of a round's 11, 11 and 10 bits
 
 struct PickRun {
@@ -299,10 +310,12 @@ __device__ __forceinline__ void load_weights(const float* mass, int j0, int end,
   for (int e = 0; e < kMine; ++e) u[e] = weight_key(w[e]);
 }
 
-// A workgroup for a whole sequence and head, of up to 1024 kMine positions.
-template <int kMine>
-__global__ __launch_bounds__(1024) void k_tok_evict_pick(EvictArgs a, int64_t first) {
+// A workgroup for a whole sequence and head, of up to 1024 kMine positions.  U > 0: it also
+// moves the rows.
+template <int kMine, int U, bool ALIGNED>
+__global__ __launch_bounds__(1024) void k_tok_evict_pick(EvictArgs a, Split sp, int64_t first) {
   __shared__ int hist[kBins], lds[16];
+  __shared__ Places at;
   __shared__ int2 found;
   const int64_t bh = first + blockIdx.x;
   const Pick p = pick_of(a, bh);
@@ -335,6 +348,12 @@ __global__ __launch_bounds__(1024) void k_tok_evict_pick(EvictArgs a, int64_t fi
     ch = {bits, want, 0, 0};
   }
   write_kept(a, bh, p, ch, j0, 0, 1, w, u, lds);
+  if constexpr (U > 0) {
+    for (int64_t x0 = 0; x0 < p.m; x0 += kMaxRows) {
+      __syncthreads();  // the list is written, and the places before are read
+      move_kept<U, ALIGNED>(a, sp, at, bh, x0, (int)min((int64_t)kMaxRows, p.m - x0));
+    }
+  }
 }
 
 // The same for longer ones, a workgroup a segment and a launch a round: round 0 to 2
@@ -456,12 +475,14 @@ constexpr int64_t kMostBlocks = 1 << 21;  // of up to 1024 threads, which a laun
 
 // Four positions a thread where 1024 threads hold them all (64 sequences of 2040, 8 heads:
 // 10.6 us, 12.8 with eight).
-template <int kMine>
-hipError_t pick(const EvictArgs& a, int64_t positions, int64_t blocks, hipStream_t st) {
+template <int kMine, int U, bool ALIGNED>
+hipError_t pick(const EvictArgs& a, const Split& sp, hipStream_t st) {
+  const int64_t blocks = a.s.batch * a.c.kv_heads, positions = a.s.columns * a.c.page_size;
   unsigned threads = 64;  // a power of two, so that they share the bins evenly
   while (threads * kMine < positions) threads *= 2;
+  if (U > 0) threads = std::max(threads, 256u);
   for (int64_t first = 0; first < blocks; first += kMostBlocks) {
-    launch(k_tok_evict_pick<kMine>, dim3((unsigned)std::min(blocks - first, kMostBlocks)), dim3(threads), st, a, first);
+    launch(k_tok_evict_pick<kMine, U, ALIGNED>, dim3((unsigned)std::min(blocks - first, kMostBlocks)), dim3(threads), st, a, sp, first);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -506,11 +527,18 @@ size_t evict_workspace_bytes(const ncodec_cache_shape& c, const ncodec_evict_sha
 hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st) {
   const ncodec_cache_shape& c = a.c;
   const ncodec_evict_shape& s = a.s;
-  const int64_t bk = s.batch * c.kv_heads, segments = segments_of(c, s);
+  const int64_t bk = s.batch * c.kv_heads, segments = segments_of(c, s), positions = s.columns * c.page_size;
+  const bool wide = c.head_dim >= 8 && c.value_dim >= 8;
+  const bool aligned = runs({c.head_dim, c.value_dim, c.k_page_stride, c.k_token_stride, c.k_head_stride, c.v_page_stride,
+                             c.v_token_stride, c.v_head_stride},
+                            {a.k_cache, a.v_cache});
+  if (evict_in_one(positions, s.keep, c.head_dim + c.value_dim)) {
+    const Split sp = split_of(c, 1, wide ? 8 : 1, kMaxRows);
+    return !wide ? pick<4, 1, false>(a, sp, st) : aligned ? pick<4, 8, true>(a, sp, st) : pick<4, 8, false>(a, sp, st);
+  }
   hipError_t e = hipSuccess;
   if (segments == 1) {
-    const int64_t cap = s.columns * c.page_size;
-    e = cap <= 4096 ? pick<4>(a, cap, bk, st) : pick<8>(a, cap, bk, st);
+    e = positions <= 4096 ? pick<4, 0, false>(a, Split{}, st) : pick<8, 0, false>(a, Split{}, st);
   } else {
     const PickRun run{a, (int)segments, (int32_t*)a.ws, (int32_t*)((char*)a.ws + hist_bytes(c, s, segments))};
     e = round<0>(run, bk * segments, st);
@@ -519,11 +547,7 @@ hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st) {
     if (e == hipSuccess) e = round<3>(run, bk * segments, st);
   }
   if (e != hipSuccess) return e;
-  if (c.head_dim < 8 || c.value_dim < 8) return move<1, false>(a, st);
-  const bool aligned = runs({c.head_dim, c.value_dim, c.k_page_stride, c.k_token_stride, c.k_head_stride, c.v_page_stride,
-                             c.v_token_stride, c.v_head_stride},
-                            {a.k_cache, a.v_cache});
-  return aligned ? move<8, true>(a, st) : move<8, false>(a, st);
+  return !wide ? move<1, false>(a, st) : aligned ? move<8, true>(a, st) : move<8, false>(a, st);
 }
 
 }  // namespace nc

@@ -94,17 +94,6 @@ __device__ __forceinline__ void weight_terms(const float (&w)[8], half8& hi, hal
 }
 __device__ __forceinline__ void weight_terms(const float (&w)[8], bhalf8& hi, bhalf8& lo) { two_terms<BF16>(w, 1.f, hi, lo); }
 
-// The largest of eight elements' bits without their signs: they order finite values,
-// infinities and NaN.
-template <class V8>
-__device__ __forceinline__ uint32_t largest_bits(const V8& v) {
-  typedef unsigned short US8 __attribute__((ext_vector_type(8)));
-  typedef unsigned short US2 __attribute__((ext_vector_type(2)));
-  const US8 u = __builtin_bit_cast(US8, v) & (unsigned short)0x7fff;
-  const US2 m = __builtin_elementwise_max(__builtin_elementwise_max(u.s01, u.s23), __builtin_elementwise_max(u.s45, u.s67));
-  return max((uint32_t)m.x, (uint32_t)m.y);
-}
-
 template <class V8>
 __device__ __forceinline__ bool any_not_finite(const V8 (&v)[4], uint32_t inf) {
   typedef unsigned short US8 __attribute__((ext_vector_type(8)));

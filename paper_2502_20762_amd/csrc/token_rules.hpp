@@ -100,4 +100,15 @@ inline bool window_halves(int64_t bh, int64_t tokens, int64_t head_dim, int64_t 
   return tokens > 64 && blocks <= (head_dim <= 64 && value_dim <= 64 ? 1000 : 256);
 }
 
+// ---- eviction from a cache
+constexpr int64_t kSegment = 8192;  // positions of a workgroup that chooses; longer sequences are shared by several
+
+// Whether the workgroup that chooses a head's tokens also moves their rows, and saves a
+// launch: as long as those are few.  width: elements of a key and a value.  us a call apart / in
+// one: 15 sequences of 8 heads, 54 tokens of 64 + 64 21.2 / 15.7, 22 of 8, 183 of these 19.5 / 16.9,
+// one of 250 18.2 / 16.6; 5 of 4, 393 of 64 + 32 17.9 / 20.0, 46 of 8, 317 of 128 + 128 28.2 / 36.1.
+inline bool evict_in_one(int64_t positions, int64_t keep, int64_t width) {
+  return positions <= 4096 && keep * width <= 32768;
+}
+
 }  // namespace nc

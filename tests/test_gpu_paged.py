@@ -348,7 +348,9 @@ def test_evict_sizes(cap, keep, sinks, recent, kind):
 @pytest.mark.parametrize("D,V", [(1, 1), (75, 33), (8, 16), (40, 128), (128, 128), (127, 127)])
 @pytest.mark.parametrize("layout", ["tokens", "heads", "beside"])
 def test_evict_widths(D, V, layout, dt):
+    # in one launch, and the rows in a launch of their own
     run_evict(2, 90, 3, D, V, dt, 33, 2, 5, layout=layout)
+    run_evict(1, 5000, 2, D, V, dt, 1700, 20, 50, page=64, layout=layout, lengths=[4900])
 
 
 def test_evict_ragged():
