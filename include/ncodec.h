@@ -560,7 +560,8 @@ ncodec_status ncodec_decay_attention(const ncodec_decay_shape* shape, const void
  * infinity reaches the tokens that see it and no other; where the formula has an
  * infinity, either of the two may stand.
  * head_dim and value_dim in [1, 128], heads and kv_heads in [1, 4096],
- * batch * heads < 2^24, tokens in [0, 2^30], window and sinks in [0, 2^31). */
+ * batch * heads < 2^24, tokens in [0, 2^30], window and sinks in [0, 2^31),
+ * |scale| <= 2^100. */
 typedef struct {
   int32_t dtype;
   int32_t heads, kv_heads, head_dim, value_dim;

@@ -106,12 +106,13 @@ const char* heads_fault(int64_t heads, int64_t kv_heads, int64_t head_dim, int64
   return nullptr;
 }
 
-bool finite(float f) { return f > -__builtin_huge_valf() && f < __builtin_huge_valf(); }
+// Softmax attention takes the scale times log2(e): room for that.
+bool scale_ok(float f) { return f >= -0x1p100f && f <= 0x1p100f; }
 
 const char* window_fault(const ncodec_window_shape& s, ncodec_status* st) {
   *st = NCODEC_EINVAL;
   if (!dtype_ok(s.dtype)) return "dtype is not an ncodec_dtype";
-  if (!finite(s.scale)) return "scale must be finite";
+  if (!scale_ok(s.scale)) return "scale must be in [-2^100, 2^100]";
   *st = NCODEC_ESHAPE;
   if (s.tokens < 0 || s.tokens > kMaxPositions) return "tokens must be in [0, 2^30]";
   if (s.window < 0 || s.window >= kMaxRows || s.sinks < 0 || s.sinks >= kMaxRows)
@@ -161,7 +162,7 @@ const char* table_fault(const ncodec_cache_shape& c, int64_t batch, int64_t colu
 const char* paged_fault(const ncodec_cache_shape& c, const ncodec_paged_shape& s, ncodec_status* st) {
   if (const char* why = cache_fault(c, false, st)) return why;
   *st = NCODEC_EINVAL;
-  if (!finite(s.scale)) return "scale must be finite";
+  if (!scale_ok(s.scale)) return "scale must be in [-2^100, 2^100]";
   *st = NCODEC_ESHAPE;
   if (const char* why = heads_fault(s.heads, c.kv_heads, c.head_dim, c.value_dim)) return why;
   if (s.window < 0 || s.window >= kMaxRows || s.sinks < 0 || s.sinks >= kMaxRows)

@@ -36,7 +36,7 @@ def window(shape, **kw):
     return refused(nc.ncodec_window_attention, "window_attention", shape, *p.values())
 
 
-@pytest.mark.parametrize("bad", [dict(dtype=7), dict(scale=float("inf")), dict(scale=float("nan"))])
+@pytest.mark.parametrize("bad", [dict(dtype=7), dict(scale=float("inf")), dict(scale=float("nan")), dict(scale=-2e30)])
 def test_window_refuses_values(bad):
     assert window(window_shape(**bad)) == nc.NCODEC_EINVAL
 
@@ -143,7 +143,7 @@ def test_paged_refuses():
                 dict(sinks=1 << 31), dict(q_head_stride=-1), dict(o_head_stride=7), dict(o_batch_stride=7), dict(batch=1 << 22)):
         assert paged(cache_shape(), paged_shape(**bad)) == nc.NCODEC_ESHAPE, bad
         assert nc.ncodec_paged_attention_workspace_bytes(cache_shape(), paged_shape(**bad), 1) == 0
-    for bad in (float("nan"), float("-inf")):
+    for bad in (float("nan"), float("-inf"), 2e30):
         assert paged(cache_shape(), paged_shape(scale=bad)) == nc.NCODEC_EINVAL
     for kw in (dict(q=0), dict(k=0), dict(v=0), dict(table=0), dict(lengths=0), dict(o=0), dict(q=FAKE + 1), dict(k=FAKE + 1),
                dict(table=FAKE + 2), dict(lengths=FAKE + 2), dict(mass=FAKE + 2)):

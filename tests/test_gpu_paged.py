@@ -237,6 +237,32 @@ def test_paged_offsets_past_32_bits():
     assert torch.equal(tk.paged_attention(q, k, v, c.table, ln), want)
 
 
+def test_paged_without_pages_columns_or_sequences():
+    x = torch.ones((2, 4, 64), dtype=torch.float16, device=DEV)
+    c = Cache(gen(8), 2, 32, 16, 2, 64, 32, "fp16")
+    none = torch.zeros((2, 0), dtype=torch.int32, device=DEV)
+    for k, v, t in ((c.k[:0], c.v[:0], c.table), (c.k, c.v, none), (c.k[:0], c.v[:0], none)):
+        m = torch.ones((2, 2, 16 * t.shape[1]), device=DEV)
+        o = tk.paged_attention(x, k, v, t, i32([7, 0]), mass=m)
+        assert bool((o == 0).all()) and o.shape == (2, 4, 32) and bool((m == 1).all())
+        tk.cache_append(torch.ones((2, 3, 2, 64), dtype=torch.float16, device=DEV), torch.ones((2, 3, 2, 32), dtype=torch.float16, device=DEV),
+                        k, v, t, i32([0, 1]), mass=m)
+    assert tk.paged_attention(x[:0], c.k, c.v, c.table[:0], i32([])).shape == (0, 4, 32)
+
+
+def test_paged_columns_behind_the_last_token_may_hold_anything():
+    g = gen(9)
+    for page in (1, 8, 16, 32):
+        c = Cache(g, 2, 96, page, 2, 64, 64, "fp16")
+        q, ln = rnd(g, (2, 4, 64), "fp16").to(DEV), i32([33, 1])
+        a = tk.paged_attention(q, c.k, c.v, c.table, ln)
+        for junk in (-1, 2 ** 31 - 1, 0, c.pages):
+            t = c.table.clone()
+            for b, n in enumerate((33, 1)):
+                t[b, -(-n // page):] = junk
+            assert torch.equal(a, tk.paged_attention(q, c.k, c.v, t, ln)), (page, junk)
+
+
 # ---------------------------------------------------------------- writes
 def run_append(B, T, K, D, V, dt, page=16, before=None, counts=None, mass=True, layout="tokens", rows="packed", offset=0,
                seed=0, spoil=None, columns=None):
