@@ -258,7 +258,7 @@ struct Chosen {
 };
 template <int kMine>
 __device__ __forceinline__ void write_kept(const EvictArgs& a, int64_t bh, const Pick& p, const Chosen& ch, int j0, int segment,
-                                           int segments, const float (&w)[kMine], const uint32_t (&u)[kMine], int* lds) {
+                                           int segments, const uint32_t (&u)[kMine], int* lds, uint16_t* list) {
   const ncodec_evict_shape& s = a.s;
   const int64_t new_cap = s.new_columns * a.c.page_size;
   int32_t* kept = a.kept + bh * s.keep;
@@ -273,19 +273,26 @@ __device__ __forceinline__ void write_kept(const EvictArgs& a, int64_t bh, const
   }
   int all;
   const int before = block_scan(sure | ties << 16, lds, all);  // both below 2^14
-  sure = ch.sure + (before & 0xffff);
+  // in order into LDS, and from there next to each other (8,192 positions: 7 us of scattered stores)
+  const int first = ch.sure + min(ch.ties, ch.equal);
+  const int count = (all & 0xffff) + min(ch.ties + (all >> 16), ch.equal) - min(ch.ties, ch.equal);
+  sure = before & 0xffff;
   ties = ch.ties + (before >> 16);
 #pragma unroll
   for (int e = 0; e < kMine; ++e) {
     const int j = j0 + e;
     const bool mid = j >= p.lo && j < p.hi, is = j < p.n && (!mid || u[e] > ch.key), tie = mid && u[e] == ch.key;
-    if (is || (tie && ties < ch.equal)) {
-      const int to = sure + min(ties, ch.equal);
-      kept[to] = j;
-      new_mass[to] = w[e];
-    }
+    if (is || (tie && ties < ch.equal)) list[sure + min(ties, ch.equal) - min(ch.ties, ch.equal)] = (uint16_t)(kMine * threadIdx.x + e);
     sure += is ? 1 : 0;
     ties += tie ? 1 : 0;
+  }
+  __syncthreads();
+  const float* mass = a.mass + bh * s.columns * a.c.page_size;
+  const int start = j0 - kMine * (int)threadIdx.x;
+  for (int x = threadIdx.x; x < count; x += blockDim.x) {
+    const int j = start + list[x];
+    kept[first + x] = j;
+    new_mass[first + x] = mass[j];
   }
   const int64_t step = (int64_t)segments * blockDim.x;
   for (int64_t x = p.m + (int64_t)segment * blockDim.x + threadIdx.x; x < new_cap; x += step) {
@@ -296,7 +303,8 @@ __device__ __forceinline__ void write_kept(const EvictArgs& a, int64_t bh, const
 }
 
 template <int kMine>
-__device__ __forceinline__ void load_weights(const float* mass, int j0, int end, float (&w)[kMine], uint32_t (&u)[kMine]) {
+__device__ __forceinline__ void load_keys(const float* mass, int j0, int end, uint32_t (&u)[kMine]) {
+  float w[kMine];
   if (j0 + kMine <= end) {
     floatx4 v[kMine / 4];
     __builtin_memcpy(v, mass + j0, sizeof(v));
@@ -315,14 +323,14 @@ __device__ __forceinline__ void load_weights(const float* mass, int j0, int end,
 template <int kMine, int U, bool ALIGNED>
 __global__ __launch_bounds__(1024) void k_tok_evict_pick(EvictArgs a, Split sp, int64_t first) {
   __shared__ int hist[kBins], lds[16];
+  __shared__ uint16_t list[1024 * kMine];
   __shared__ Places at;
   __shared__ int2 found;
   const int64_t bh = first + blockIdx.x;
   const Pick p = pick_of(a, bh);
   const int j0 = threadIdx.x * kMine;
-  float w[kMine];
   uint32_t u[kMine];
-  load_weights(a.mass + bh * a.s.columns * a.c.page_size, j0, p.n, w, u);
+  load_keys(a.mass + bh * a.s.columns * a.c.page_size, j0, p.n, u);
   Chosen ch = {0xffffffffu, 0, 0, 0};
   if (p.want == p.hi - p.lo) {  // all of them: no choice
     ch = {0u, p.want, 0, 0};
@@ -347,7 +355,7 @@ __global__ __launch_bounds__(1024) void k_tok_evict_pick(EvictArgs a, Split sp, 
     }
     ch = {bits, want, 0, 0};
   }
-  write_kept(a, bh, p, ch, j0, 0, 1, w, u, lds);
+  write_kept(a, bh, p, ch, j0, 0, 1, u, lds, list);
   if constexpr (U > 0) {
     for (int64_t x0 = 0; x0 < p.m; x0 += kMaxRows) {
       __syncthreads();  // the list is written, and the places before are read
@@ -363,15 +371,15 @@ template <int ROUND>
 __global__ __launch_bounds__(1024) void k_tok_evict_round(PickRun run, int64_t first) {
   constexpr int kMine = kMost;
   __shared__ int hist[kBins], lds[16];
+  __shared__ uint16_t list[1024 * kMine];
   __shared__ int2 found;
   const EvictArgs& a = run.a;
   const int S = run.segments, segment = (int)((first + blockIdx.x) % S);
   const int64_t bh = (first + blockIdx.x) / S;
   const Pick p = pick_of(a, bh);
   const int j0 = segment * kSegment + threadIdx.x * kMine;
-  float w[kMine];
   uint32_t u[kMine];
-  load_weights(a.mass + bh * a.s.columns * a.c.page_size, j0, p.n, w, u);
+  load_keys(a.mass + bh * a.s.columns * a.c.page_size, j0, p.n, u);
   int32_t* hists = run.hist + bh * 3 * S * kBins;
   int32_t* meta = run.meta + bh * (4 + S);
   const bool choice = p.want > 0 && p.want < p.hi - p.lo;
@@ -444,7 +452,7 @@ __global__ __launch_bounds__(1024) void k_tok_evict_round(PickRun run, int64_t f
   const int start = min(segment * kSegment, p.n);
   ch.sure += min(start, p.lo) + max(0, start - p.hi);
   if (p.want == p.hi - p.lo) ch.sure += max(0, min(start, p.hi) - p.lo);
-  write_kept(a, bh, p, ch, j0, segment, S, w, u, lds);
+  write_kept(a, bh, p, ch, j0, segment, S, u, lds, list);
 }
 
 template <int U, bool ALIGNED>
