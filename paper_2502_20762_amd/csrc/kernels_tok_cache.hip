@@ -1,6 +1,12 @@
 // The upkeep of a paged cache: new tokens into its pages, and eviction by
 // accumulated attention weight.  Both move rows, bound by the bytes; the choice of the
 // tokens to keep is a radix selection in three rounds of 11, 11 and 10 bits.
+//
+// 130,560 tokens of 4 heads of 128 + 128 into the cache, 535 MB: 108 us (4.9 TB/s, a large
+// copy's rate).  64 sequences of up to 2,040 tokens cut to 1,020, 8 heads of 64 + 64: 11 us for the
+// choice and 53 for the rows (196 MB, 3.7 TB/s; heads of a token side by side in the grid were no
+// faster), one of 130,560 to 32,640, 4 heads of 128 + 128: four launches of 5, 8, 8 and 11.5 us,
+// each waiting for the counts of the one before, and 35 for the rows (134 MB, 3.9 TB/s).
 #include <algorithm>
 
 #include "token_rules.hpp"

@@ -5,7 +5,19 @@
 // transposed: scores^T = K q^T with keys as rows and queries as columns, so that a lane
 // holds half of one query's scores and its maximum, sum and rescaling are the lane's own;
 // and outputs^T = V^T p^T, whose operand p the accumulators of the scores already are, in
-// the order of keys that a transposed read of V from LDS gives.
+// the order of keys that a transposed read of V from LDS gives.  Weights enter that product
+// as two 16-bit terms each (22 bits in fp16, 16 in bf16): with one, as many bits as the output,
+// the outputs err 1.4 times as much as their rounding, for 0.74 to 0.85 of the time.
+//
+// A workgroup's four waves share tiles of 64 keys and values in LDS, 32 queries a wave: of
+// four heads of a group, or of one.  What bounds it is a wave's own sequence of scores,
+// weights and outputs, of which the other wave of the SIMD hides a part: 32,640 tokens of 16
+// heads over 4 of 128 x 128, 8,160 in sight, bf16, 2.0 TFLOP: 2.4 to 2.6 ms (0.8 PFLOP/s, 1.2 with the
+// second terms, which is what the library's large product reaches; MFMAs run 60 % of the CUs'
+// busy time, VALU issues 52 %, 30 % of a wave's time goes by at waits and barriers); 8,160 tokens of 8 heads of 64 x 64, 4,080 in sight, fp16: 109 to 119 us (MFMAs 42 %,
+// VALU 63 % in a larger case of that kind).  Tried and no faster there: the next tile's scores beside
+// the weights of this one, weights and products of 16 keys in turn, 64 queries a wave, three
+// waves a SIMD, two or eight waves a workgroup.
 #include <algorithm>
 
 #include "tok_attend.hpp"
@@ -21,11 +33,11 @@ constexpr int kWaves = 4;
 
 struct WindowRun {
   WindowArgs a;
-  int64_t first;        // block of this launch's first workgroup
-  int head_waves;       // waves of a workgroup on different heads of a group; the others on further queries
-  int head_tiles;       // workgroups for a group's heads
-  int query_blocks;     // of a sequence
-  bool q_runs;          // queries are whole 16-byte runs
+  int64_t first;     // block of this launch's first workgroup
+  int head_waves;    // waves of a workgroup on different heads of a group; the others on further queries
+  int head_tiles;    // workgroups for a group's heads
+  int query_blocks;  // of a sequence
+  bool q_runs;       // queries are whole 16-byte runs
 };
 
 __device__ __align__(16) uint32_t window_zero16[4];
@@ -76,20 +88,19 @@ __device__ __forceinline__ void stage_tile(char* lds, const typename E::T* base,
   }
 }
 
-// Eight weights as two 16-bit terms (two_terms() in fewer steps: the rest of an fp16 term
-// is formed and rounded in one instruction).
+// Eight weights as two 16-bit terms (as two_terms(), in fewer steps: the rest of an fp16 term
+// is formed and rounded in one instruction, a multiply-add of mixed types).
 __device__ __forceinline__ void weight_terms(const float (&w)[8], half8& hi, half8& lo) {
+  float minus = -1.f;
+  asm("" : "+s"(minus));  // or the multiply-add would become a conversion and a subtraction
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
-    const half2 x = {(f16)w[i], (f16)w[i + 1]};
-    half2 y;
-    // w - x, fp32, rounded once to each half of y
-    asm("v_fma_mixlo_f16 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(y) : "v"(x), "v"(w[i]));
-    asm("v_fma_mixhi_f16 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(y) : "v"(x), "v"(w[i + 1]));
+    half2 x = {(f16)w[i], (f16)w[i + 1]};
+    asm("" : "+v"(x));  // or each half would be formed anew for its rest
     hi[i] = x.x;
     hi[i + 1] = x.y;
-    lo[i] = y.x;
-    lo[i + 1] = y.y;
+    lo[i] = (f16)__builtin_fmaf((float)x.x, minus, w[i]);
+    lo[i + 1] = (f16)__builtin_fmaf((float)x.y, minus, w[i + 1]);
   }
 }
 __device__ __forceinline__ void weight_terms(const float (&w)[8], bhalf8& hi, bhalf8& lo) { two_terms<BF16>(w, 1.f, hi, lo); }
