@@ -103,17 +103,18 @@ class TokenMixer:
 class TokenCache:
     """Keys and values of the latest tokens of a batch of streams, in pages.
 
-    capacity: tokens of a stream at most.  With ``keep`` every position's attention weights are summed, and a cache
-    that would overflow is cut back to its ``keep`` heaviest tokens first, the first ``sinks`` and the latest
-    ``recent`` among them; ``keep`` has to leave room for the tokens that come at once.  Without it an append that
+    capacity: tokens of a stream at most.  With ``keep`` a cache that would overflow is cut back first, to the first
+    ``sinks`` and the latest ``recent`` tokens and, up to ``keep`` tokens in all, the heaviest of the others by the
+    attention weights that :meth:`attend` has given them (``weigh=False``: none are summed, for a ``keep`` that the first
+    and the latest fill); ``keep`` has to leave room for the tokens that come at once.  Without ``keep`` an append that
     does not fit is refused."""
 
     def __init__(self, batch, capacity, kv_heads, head_dim, value_dim=None, page_size=16, keep=None, sinks=0, recent=0,
-                 dtype=torch.float16, device="cuda:0"):
+                 weigh=True, dtype=torch.float16, device="cuda:0"):
         columns = -(-capacity // page_size)
         if keep is not None and not 0 < keep < capacity:
             raise ValueError("keep must be in [1, capacity)")
-        self.capacity, self.keep, self.sinks, self.recent = capacity, keep, sinks, recent
+        self.capacity, self.keep, self.sinks, self.recent, self.weigh = capacity, keep, sinks, recent, weigh
         self.most = 0  # tokens of the fullest stream at most: known without asking the GPU
         pages = batch * columns
         count = 2 * pages if keep is not None else pages  # an eviction copies to pages that are free
@@ -137,10 +138,11 @@ class TokenCache:
 
     def attend(self, q, window=None, sinks=0):
         """Attention of each stream's last token, q (batch, heads, dim)."""
-        return paged_attention(q, self.k, self.v, self.table, self.lengths, window, sinks, mass=self.mass)
+        return paged_attention(q, self.k, self.v, self.table, self.lengths, window, sinks,
+                               mass=self.mass if self.weigh else None)
 
     def evict(self):
-        """Cuts every stream back to its ``keep`` heaviest tokens; returns their old positions."""
+        """Cuts every stream back to ``keep`` tokens; returns their old positions."""
         self.lengths, self.mass, kept = cache_evict(self.k, self.v, self.table, self.lengths, self.mass, self.keep,
                                                     self.free, self.sinks, self.recent)
         self.table, self.free = self.free, self.table
@@ -157,10 +159,18 @@ class CacheMixer(TokenMixer):
         self.window, self.sinks = window, sinks
 
     def new_cache(self, capacity, batch=1, page_size=16, keep=None, recent=0):
-        """A cache of streams that have seen nothing; with ``keep`` it holds no window of tokens, but the heaviest."""
-        if keep is not None and self.window is not None:
-            raise ValueError("a cache that keeps the heaviest tokens goes with window=None")
-        return TokenCache(batch, capacity, self.K, self.D, None, page_size, keep, self.sinks, recent, self.dtype, self.device)
+        """A cache of streams that have seen nothing.  Without a window, ``keep`` and ``recent`` bound it as they do a
+        :class:`TokenCache`.  With one, a cache with room for more than the window and the first tokens lets go of what no
+        later token sees, and takes streams of any length."""
+        weigh = self.window is None
+        if not weigh:
+            if keep is not None:
+                raise ValueError("a cache that keeps the heaviest tokens goes with window=None")
+            recent = self.window - 1
+            if max(1, self.sinks + recent) < capacity:
+                keep = max(1, self.sinks + recent)
+        return TokenCache(batch, capacity, self.K, self.D, None, page_size, keep, self.sinks, recent, weigh, self.dtype,
+                          self.device)
 
     def __call__(self, x, positions, cache=None, lengths=None):
         """The prompt form: x (batch, tokens, C) are the first tokens of their streams, positions (tokens, 3) int32;

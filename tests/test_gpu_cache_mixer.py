@@ -70,6 +70,27 @@ def test_streams_of_different_length():
         assert rms(y[b:b + 1], f64(m.step(last[b:b + 1], pos[40:], alone))) <= 16 * U[torch.float16]
 
 
+@pytest.mark.parametrize("window,sinks,capacity", [(30, 3, 40), (30, 0, 30), (2, 1, 5), (17, 20, 64), (1, 0, 4)])
+def test_a_window_takes_streams_of_any_length(window, sinks, capacity):
+    # what has left the window leaves the cache, and the tokens after it see what the prompt's do
+    m = CacheMixer(64, heads=4, kv_heads=2, window=window, sinks=sinks, device=DEV)
+    x = torch.randn((2, 150, 64), device=DEV).half()
+    pos = grid_positions(1, 10, 15, device=DEV)
+    want = f64(m(x, pos))
+    cache = m.new_cache(capacity, batch=2, page_size=8)
+    lengths = torch.tensor([4, 1], dtype=torch.int32, device=DEV)
+    m(x[:, :4].contiguous(), pos[:4], cache, lengths)
+    y = torch.stack([m.step(torch.stack([x[0, 4 + t], x[1, 1 + t]]), pos[4 + t:5 + t], cache) for t in range(146)])
+    torch.cuda.synchronize()
+    assert rms(y[:, 0], want[0, 4:]) <= 16 * U[torch.float16]
+    assert cache.most <= capacity and cache.lengths.tolist()[0] <= capacity and bool((cache.mass == 0).all())
+    # the other stream is three tokens behind, with the positions of the first
+    alone = m.new_cache(capacity, page_size=8)
+    m(x[1:, :1].contiguous(), pos[:1], alone)
+    z = torch.cat([m.step(x[1:, 1 + t], pos[4 + t:5 + t], alone) for t in range(146)])
+    assert rms(y[:, 1], f64(z)) <= 16 * U[torch.float16]
+
+
 def test_a_budget_holds_the_first_the_latest_and_the_heaviest():
     m = CacheMixer(64, heads=4, kv_heads=2, sinks=3, device=DEV)
     full = m.new_cache(200)
