@@ -167,22 +167,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     const T* k = (const T*)a.k + b * s.k_batch_stride + hk * s.k_head_stride;
     const T* v = (const T*)a.v + b * s.v_batch_stride + hk * s.v_head_stride;
     const int window = s.window ? (int)s.window : 0x7fffffff, sinks = (int)s.sinks;
-    // Tiles of keys: those of the first tokens that the window has left behind (`lead` of
-    // them), then `from` on.  The ones that all queries of the workgroup see whole come first.
-    const int near = max(0, i0 + 1 - window), last = i0 + qw * kQueries - 1;
-    const int lead = (min(sinks, near) + kTile - 1) / kTile, from = max(near / kTile, lead), end = (iend + kTile - 1) / kTile;
-    const int lead_whole = min(lead, sinks / kTile);
-    const int whole_a = max(from, last < window ? 0 : (last - window + kTile) / kTile), whole_b = max(whole_a, (i0 + 1) / kTile);
-    const int whole = lead_whole + whole_b - whole_a, tiles = lead + end - from;
-    const auto key0 = [&](int t) {
-      int x = t < lead_whole ? t : t - lead_whole + whole_a;
-      if (t >= whole) {
-        x = t - whole + lead_whole;                                   // the rest of the first ones,
-        if (x >= lead) x += from - lead;                              // those before the whole ones
-        if (x >= whole_a && t - whole + lead_whole >= lead) x += whole_b - whole_a;  // and behind them
-      }
-      return x * kTile;
-    };
+    const WindowTiles all_tiles = window_tiles(i0, qw * kQueries, len, (int)s.window, sinks);
+    const int whole = all_tiles.whole, tiles = all_tiles.count;
+    const auto key0 = [&](int t) { return all_tiles.key0(t); };
     const auto stage = [&](int t) {
 #pragma unroll
       for (int x = 0; x < KS; ++x) {

@@ -100,6 +100,40 @@ inline bool window_halves(int64_t bh, int64_t tokens, int64_t head_dim, int64_t 
   return tokens > 64 && blocks <= (head_dim <= 64 && value_dim <= 64 ? 1000 : 256);
 }
 
+// The tiles of 64 keys that the queries i0 .. i0 + queries - 1 of a sequence of `len` tokens see:
+// those of the first tokens that the window has left behind (`lead` of them), then `from`
+// on.  The ones that all of the queries see whole come first, `whole` of them.  len > i0;
+// window = 0: all earlier tokens.  In constant expressions, so that the kernel uses it too.
+struct WindowTiles {
+  int lead, from, lead_whole, whole_a, whole_b, whole, count;
+  // first key of the t-th one
+  constexpr int key0(int t) const {
+    int x = t < lead_whole ? t : t - lead_whole + whole_a;
+    if (t >= whole) {
+      const int y = t - whole + lead_whole;  // the rest of the first ones,
+      x = y < lead ? y : y + from - lead;    // those before the whole ones
+      if (y >= lead && x >= whole_a) x += whole_b - whole_a;  // and behind them
+    }
+    return 64 * x;
+  }
+};
+constexpr int lesser(int a, int b) { return a < b ? a : b; }
+constexpr int greater(int a, int b) { return a < b ? b : a; }
+constexpr WindowTiles window_tiles(int i0, int queries, int64_t len, int window, int sinks) {
+  const int last = i0 + queries - 1, end = (int)(len < last + 1 ? len : last + 1);
+  const int near = window && i0 + 1 > window ? i0 + 1 - window : 0;  // the first that the window of i0 holds
+  WindowTiles w{};
+  w.lead = (lesser(sinks, near) + 63) / 64;
+  w.from = greater(near / 64, w.lead);
+  const int behind = (i0 + 1) / 64;  // tiles up to here hold no token after the first query
+  w.lead_whole = lesser(lesser(w.lead, sinks / 64), behind);
+  w.whole_a = greater(w.from, window && last >= window ? (last - window + 64) / 64 : 0);
+  w.whole_b = greater(w.whole_a, behind);
+  w.whole = w.lead_whole + w.whole_b - w.whole_a;
+  w.count = w.lead + (end + 63) / 64 - w.from;
+  return w;
+}
+
 // ---- eviction from a cache
 constexpr int64_t kSegment = 8192;  // positions of a workgroup that chooses; longer sequences are shared by several
 

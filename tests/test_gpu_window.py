@@ -61,6 +61,16 @@ def test_windows_and_sinks(window, sinks):
     run(1, 300, 2, 2, 32, 32, "fp16", window, sinks)
 
 
+@pytest.mark.parametrize("window", [None, 1, 17, 40, 64, 130])
+@pytest.mark.parametrize("sinks", [0, 5, 64, 100, 1000])
+def test_windows_and_sinks_of_shared_heads(window, sinks):
+    # waves on heads of a group: 32 queries a workgroup, which begin inside a tile of keys
+    say("window shared", window, sinks)
+    run(1, 300, 4, 1, 32, 32, "fp16", window, sinks)
+    run(1, 300, 2, 1, 128, 32, "bf16", window, sinks)
+    run(3, 140, 128, 2, 16, 128, "fp16", window, sinks)  # waves that do not share queries
+
+
 @pytest.mark.parametrize("dt", ["fp16", "bf16"])
 @pytest.mark.parametrize("window,sinks", [(None, 0), (50, 4), (200, 100)])
 def test_ragged(window, sinks, dt):
