@@ -282,10 +282,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_tok_paged(PagedRun run) {
       const float my = ml[y][0][h], ly = ml[y][1][h];
       none = none || ly == kAllMinusInf;
       const float f = my == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(my - M);
-      if (f != 0.f || ly != ly) {
-        L = fmaf(ly, f, L);
-        O = fmaf(part[y][h][d], f, O);
-      }
+      L = fmaf(ly, f, L);  // also where f is 0: what is no number stays so
+      O = fmaf(part[y][h][d], f, O);
     }
     if (none && L == 0.f) L = kAllMinusInf;
     if (run.splits == 1 && d < V)
@@ -325,7 +323,7 @@ __global__ __launch_bounds__(1024) void k_tok_paged_join(PagedRun run, int heads
     for (int y = 0; y < kMaxSplits / 64; ++y) {
       none = none || l[y] == kAllMinusInf;
       f[y] = m[y] == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(m[y] - M);
-      if (f[y] != 0.f || l[y] != l[y]) L = fmaf(l[y], f[y], L);
+      L = fmaf(l[y], f[y], L);
     }
     for (int w = 32; w; w >>= 1) L += __shfl_xor(L, w, 64);
     if (__any(none) && L == 0.f) L = __builtin_nanf("");
@@ -353,8 +351,7 @@ __global__ __launch_bounds__(1024) void k_tok_paged_join(PagedRun run, int heads
       }
 #pragma unroll
       for (int y = 0; y < 8; ++y) {
-        const float fx = x + y * waves < run.splits ? fade[x + y * waves] : 0.f;
-        if (fx == 0.f) continue;  // a split that saw nothing has written no outputs
+        const float fx = x + y * waves < run.splits ? fade[x + y * waves] : 0.f;  // 0: the last split once more
         sum[0] = fmaf(v[y][0], fx, sum[0]);
         sum[1] = fmaf(v[y][1], fx, sum[1]);
       }

@@ -213,6 +213,24 @@ def test_paged_stretches_of_nan_and_of_minus_infinity(n, dt):
         assert bool((mass[0, 0, a:b] == 0).all()) and abs(float(mass.sum()) - 1) < 1e-4
 
 
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("n,low", [(40, 32), (3000, 1500), (3000, 2999), (20000, 9000)])
+def test_paged_values_that_are_no_numbers_count_however_small_their_weight(n, low, dt):
+    # `low` tokens, as many as a wave's or a workgroup's share, weigh exp(-512) of the others, or of the last one
+    c = Cache(gen(6), 1, n, 16, 1, 64, 64, dt)
+    q = torch.full((1, 1, 64), 8.0, dtype=c.k.dtype, device=DEV)
+    t, j = c.table[0].long(), torch.arange(n, device=DEV)
+    for key in (-8.0, -INF):
+        c.k.zero_()
+        c.k[t[j[:low] // 16], j[:low] % 16] = key
+        v = c.v.clone()
+        v[t[5 // 16], 5, 0, 3] = NAN
+        o, clean = (tk.paged_attention(q, c.k, x, c.table, i32([n])) for x in (v, c.v))
+        assert torch.isnan(o[0, 0, 3]) and torch.isfinite(clean).all()
+        rest = torch.arange(64, device=DEV) != 3
+        assert torch.equal(o[..., rest], clean[..., rest])
+
+
 class Seen:
     """A cache with other keys."""
 
