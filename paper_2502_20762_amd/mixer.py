@@ -128,10 +128,11 @@ class TokenCache:
     def append(self, k, v, counts=None):
         """Adds tokens, k and v (batch, tokens, kv_heads, dim); counts: (batch) int32 of each stream (None: all)."""
         T = k.shape[1]
-        if self.most + T > self.capacity and self.keep is not None:
-            self.evict()
+        held = self.most if self.keep is None else min(self.most, self.keep)
+        if held + T > self.capacity:  # before anything is let go
+            raise ValueError(f"{T} tokens do not fit a cache of {self.capacity} that holds {held} at least")
         if self.most + T > self.capacity:
-            raise ValueError(f"{T} tokens do not fit a cache of {self.capacity} that may hold {self.most}")
+            self.evict()
         cache_append(k, v, self.k, self.v, self.table, self.lengths, counts, self.mass)
         self.lengths += T if counts is None else counts.clamp(0, T)
         self.most += T
@@ -161,7 +162,7 @@ class CacheMixer(TokenMixer):
     def new_cache(self, capacity, batch=1, page_size=16, keep=None, recent=0):
         """A cache of streams that have seen nothing.  Without a window, ``keep`` and ``recent`` bound it as they do a
         :class:`TokenCache`.  With one, a cache with room for more than the window and the first tokens lets go of what no
-        later token sees, and takes streams of any length."""
+        later token sees, and takes streams of any length, whose prompt has to fit it."""
         weigh = self.window is None
         if not weigh:
             if keep is not None:

@@ -145,3 +145,15 @@ def test_refusals():
         CacheMixer(64, window=4, device=DEV).new_cache(8, keep=4)
     with pytest.raises(ValueError, match="fit"):
         m(torch.randn((1, 20, 64), device=DEV).half(), grid_positions(1, 4, 5, device=DEV), m.new_cache(16, keep=8))
+
+
+def test_an_append_that_is_refused_leaves_the_cache_as_it_was():
+    cache = TokenCache(2, 16, 1, 64, keep=8, sinks=1, recent=2, device=DEV)
+    x = torch.randn((2, 14, 1, 64), device=DEV).half()
+    cache.append(x[:, :12], x[:, :12])
+    for tokens in (9, 14):
+        with pytest.raises(ValueError, match="fit"):
+            cache.append(x[:, :tokens], x[:, :tokens])
+        assert cache.most == 12 and cache.lengths.tolist() == [12, 12]
+    cache.append(x[:, :8], x[:, :8])
+    assert cache.most == 16 and cache.lengths.tolist() == [16, 16]

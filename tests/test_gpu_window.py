@@ -344,3 +344,21 @@ def test_refusals():
             tk.window_attention(*args)
         with torch.no_grad():
             tk.window_attention(*args)
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+def test_window_values_that_are_no_numbers_count_however_small_their_weight(dt):
+    # tiles of 64 keys go to two waves in turn; the low ones weigh exp(-512) of the others
+    T, tile = 500, torch.arange(500, device=DEV) // 64
+    q = torch.full((1, T, 1, 64), 8.0, device=DEV).to(torch.float16 if dt == "fp16" else torch.bfloat16)
+    clean_v = torch.randn((1, T, 1, 64), device=DEV).to(q.dtype)
+    for low in (tile % 2 == 0, tile % 2 == 1, tile < 3):
+        k = torch.zeros_like(q)
+        k[0, low] = -8.0
+        at = int(low.nonzero()[5])
+        v = clean_v.clone()
+        v[0, at, 0, 3] = NAN
+        o, clean = (tk.window_attention(q, k, x) for x in (v, clean_v))
+        assert torch.isnan(o[0, at:, 0, 3]).all() and torch.isfinite(clean).all()
+        o[0, at:, 0, 3] = clean[0, at:, 0, 3]
+        assert torch.equal(o, clean)
