@@ -173,7 +173,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_tok_paged(PagedRun run) {
 
   const float scale = s.scale * 1.44269504088896341f, off = F ? 14.f : -kBelow;
   floatx4 o[VW] = {};
-  float m = -__builtin_huge_valf(), base = 0.f, l = 0.f;
+  float m = -__builtin_huge_valf(), l = 0.f;
   bool any = false;
   int x = x0 + wave;
   int cur[2] = {-1, -1};
@@ -196,7 +196,10 @@ __global__ __launch_bounds__(64 * kWaves) void k_tok_paged(PagedRun run) {
     }
     float w[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = z[e >> 2][e & 3] * scale;
+    for (int e = 0; e < 8; ++e) {
+      w[e] = z[e >> 2][e & 3] * scale;
+      asm("" : "+v"(w[e]));  // rounded: the maximum is one of them
+    }
     // positions that are not seen, here or for want of a page
     bool all = pos + kStep <= n && (pos + kStep <= seen.first || pos >= seen.near);
     if (PAGE)
@@ -228,18 +231,18 @@ __global__ __launch_bounds__(64 * kWaves) void k_tok_paged(PagedRun run) {
       top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
       const float m1 = fmaxf(m, top);
-      const float base1 = m1 == -__builtin_huge_valf() ? 0.f : m1 - off;
-      const float fade = m == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(base - base1);
+      const float fade = m == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(m - m1);
       m = m1;
-      base = base1;
       l *= fade;
 #pragma unroll
       for (int i = 0; i < VW; ++i) o[i] *= fade;
     }
+    const float from = m == -__builtin_huge_valf() ? 0.f : m;
     float p[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(w[e] - base);
+      // in two steps: where scores are so large that off vanishes beside them, the largest weight is still 2^off
+      p[e] = __builtin_amdgcn_exp2f((w[e] - from) + off);
       l += p[e];
     }
     V8 hi, lo;
@@ -378,19 +381,20 @@ __global__ __launch_bounds__(1024) void k_tok_paged_join(PagedRun run, int heads
     float f[kMaxSplits / 64];
     const float2 ml = join(bh0 + g, f);
     if (lane == 0) {
-      lds[2 * g] = ml.x - (__is_same(E, F16) ? 14.f : -kBelow);  // the sums hold weights 2^14 or 2^-32 of the largest
+      lds[2 * g] = ml.x;
       lds[2 * g + 1] = ml.y;
     }
   }
   __syncthreads();
   float* mass = a.mass + (int64_t)bk * cap;
+  const float off = __is_same(E, F16) ? 14.f : -kBelow;  // the sums hold weights 2^off of the largest
   for (int64_t x = block * (int64_t)blockDim.x + threadIdx.x; x < seen.count; x += (int64_t)mass_blocks * blockDim.x) {
     const int j = seen.at((int)x);
     const int32_t page = a.table[b * s.table_stride + (j >> shift)];
     const float before = mass[j];
     float w = 0.f;
     for (int g = 0; g < group; ++g)
-      w = fmaf(__builtin_amdgcn_exp2f(run.z[(bh0 + g) * run.zstride + j] - lds[2 * g]), lds[2 * g + 1], w);
+      w = fmaf(__builtin_amdgcn_exp2f((run.z[(bh0 + g) * run.zstride + j] - lds[2 * g]) + off), lds[2 * g + 1], w);
     if ((uint32_t)page < (uint32_t)c.pages) mass[j] = before + w;
   }
 }

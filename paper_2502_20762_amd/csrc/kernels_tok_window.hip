@@ -132,6 +132,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   // maximum, so that outputs are seldom rescaled: fp16 terms stay below 2^15 and keep the
   // bits above 2^-32 of the largest weight, bf16 ones leave room for 2^31 tokens.
   constexpr float off = F ? 7.f : -40.f, lag = 8.f;
+  // Scores whose product with c this large a number is would, rounded once for the base and not
+  // at all in the weights, leave that room: they are multiplied first.
+  constexpr float kLarge = 0x1p22f, kNothing = -0x1.fffffep127f;
   __shared__ __align__(1024) char lds[2 * KS * STAGE];
   const WindowArgs& a = run.a;
   const ncodec_window_shape& s = a.s;
@@ -209,7 +212,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     }
     const int ro = row_offset<DP>(lane);
     const int pv0 = col_offset<VW, false>(lane, 0), pv1 = col_offset<VW, false>(lane, 1);
-    float mc = -__builtin_huge_valf(), base = 0.f;  // maximum and what is taken from each score, times c
+    float base = kNothing;  // what is taken from each score, times c
+    float cl = c;           // 1: the lane's query has large scores, multiplied already
+    bool large = false;     // has any of the wave's?
 
     // does any of the wave's queries see any of the tile's keys?
     const auto some = [&](int j0) { return j0 < wend && (j0 < sinks || wi0 - (j0 + kTile - 1) < window); };
@@ -232,18 +237,33 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
         p[1] = E::mfma(kf[x][1], qf[x], p[1]);
       }
     };
-    const auto follow = [&](const floatx16(&p)[2]) {  // the base after the maximum
+    const auto multiply = [&](floatx16(&p)[2], float by) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        p[0][r] *= by;
+        p[1][r] *= by;
+      }
+    };
+    const auto follow = [&](floatx16(&p)[2]) {  // the base after the maximum
+      if (large) multiply(p, cl == c ? 1.f : c);
       float top = fmaxf(p[0][0], p[1][0]);
 #pragma unroll
       for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, p[0][r]), p[1][r]);
-      if (__any(fmaf(top, c, -lag) > mc)) {
+      if (__any(fmaf(top, cl, -base) > off + lag)) {
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
         top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
         // each query by its own scores, whatever the wave's others are
-        const bool rises = fmaf(top, c, -lag) > mc;
-        const float m1 = rises ? top * c : mc, base1 = rises ? m1 - off : base;
-        const float fade = !rises ? 1.f : mc == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(base - base1);
-        mc = m1;
+        const bool rises = fmaf(top, cl, -base) > off + lag;
+        const bool now = rises && cl == c && fabsf(top * cl) >= kLarge;
+        if (__any(now)) {
+          top *= now ? c : 1.f;
+          asm("" : "+v"(top));  // rounded, as the scores are
+          multiply(p, now ? c : 1.f);
+          cl = now ? 1.f : cl;
+          large = true;
+        }
+        const float base1 = rises ? fmaf(top, cl, -off) : base;
+        const float fade = rises ? __builtin_amdgcn_exp2f(base - base1) : 1.f;
         base = base1;
         sum *= fade;
 #pragma unroll
@@ -257,7 +277,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       float w[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        w[e] = __builtin_amdgcn_exp2f(fmaf(p[x >> 1][8 * (x & 1) + e], c, -base));
+        w[e] = __builtin_amdgcn_exp2f(fmaf(p[x >> 1][8 * (x & 1) + e], cl, -base));
         sum += w[e];
       }
       weight_terms(w, hi, lo);
@@ -376,7 +396,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       constexpr int STEP = kWaves / KS * 64 * 4;
       lds_barrier();
       if (ks) {
-        *(floatx4*)mine = floatx4{mc, base, sum, 0.f};
+        *(floatx4*)mine = floatx4{base, sum, 0.f, 0.f};
 #pragma unroll
         for (int x = 0; x < 4 * NV; ++x)
           *(floatx4*)(mine + (x + 1) * STEP) =
@@ -385,12 +405,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       lds_barrier();
       if (ks) return;
       const floatx4 other = *(const floatx4*)mine;
-      const float none = -__builtin_huge_valf();
-      const float b1 = mc == none ? other[1] : other[0] == none ? base : fmaxf(base, other[1]);
-      // what saw no score above -inf counts nothing, but for a NaN
-      const float f0 = mc == none ? (sum != sum ? 1.f : 0.f) : __builtin_amdgcn_exp2f(base - b1);
-      const float f1 = other[0] == none ? (other[2] != other[2] ? 1.f : 0.f) : __builtin_amdgcn_exp2f(other[1] - b1);
-      sum = sum * f0 + other[2] * f1;
+      const float b1 = fmaxf(base, other[0]);
+      const float f0 = __builtin_amdgcn_exp2f(base - b1), f1 = __builtin_amdgcn_exp2f(other[0] - b1);
+      sum = sum * f0 + other[1] * f1;
 #pragma unroll
       for (int x = 0; x < 4 * NV; ++x) {
         const floatx4 w = *(const floatx4*)(mine + (x + 1) * STEP);

@@ -231,6 +231,32 @@ def test_paged_values_that_are_no_numbers_count_however_small_their_weight(n, lo
         assert torch.equal(o[..., rest], clean[..., rest])
 
 
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("scale", [1.1e3, 1e5, 3e5, 1.7e6, 1.3e7, -1.9e8, 3.3e12, 1e25])
+def test_paged_large_scores(scale, dt):
+    # in fp32 they are further apart than powers of two: weights err, but no more than by their scores' rounding,
+    # which is nothing where one token is ahead by more than that
+    say("paged large scores", scale, dt)
+    g = gen(14)
+    for B, n, H, K, D in ((8, 40, 4, 2, 64), (3, 3000, 32, 1, 128), (2, 20000, 2, 2, 64)):
+        c = Cache(g, B, n, 16, K, D, 64, dt)
+        q, ln, mass = rnd(g, (B, H, D), dt).to(DEV), i32([n] * B), torch.zeros((B, K, c.columns), device=DEV)
+        o = f64(tk.paged_attention(q, c.k, c.v, c.table, ln, scale=scale))
+        assert np.array_equal(o, f64(tk.paged_attention(q, c.k, c.v, c.table, ln, scale=scale, mass=mass)))
+        want, _, wm = paged_reference(q, c, ln, None, 0, scale, mass * 0)
+        top = np.abs(f64(c.v)).max()
+        assert np.isfinite(o).all() and np.abs(o).max() <= top * (1 + 2 * U[dt])
+        assert bool(torch.isfinite(mass).all()) and np.abs(f64(mass.sum(-1)) - H // K).max() < 1e-3 * (H // K)
+        t = f64(c.table).astype(np.int64)[:, np.arange(n) // 16]
+        k = f64(c.k)[t, np.arange(n) % 16]  # (B, n, K, D)
+        kk = np.repeat(k, H // K, 2)
+        s = scale * np.einsum("bhd,bjhd->bhj", f64(q), kk)
+        mag = abs(scale) * np.einsum("bhd,bjhd->bhj", np.abs(f64(q)), np.abs(kk)).max()
+        last = np.sort(s)[..., -2:]
+        sure = last[..., 1] - last[..., 0] > 2 * (D + 6) * F32 * mag + 32
+        assert np.abs(o - want)[sure].max(initial=0) <= U[dt] * top * (1 + 2 * U[dt]) + 2.0 ** -15 * top
+
+
 class Seen:
     """A cache with other keys."""
 

@@ -362,3 +362,36 @@ def test_window_values_that_are_no_numbers_count_however_small_their_weight(dt):
         assert torch.isnan(o[0, at:, 0, 3]).all() and torch.isfinite(clean).all()
         o[0, at:, 0, 3] = clean[0, at:, 0, 3]
         assert torch.equal(o, clean)
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("scale", [1.1e3, 1e5, 3e5, 1.7e6, 1.3e7, -1.9e8, 3.3e12, 1e25])
+def test_large_scores(scale, dt):
+    # in fp32 they are further apart than powers of two: weights err, but no more than by their scores' rounding,
+    # which is nothing where one token is ahead by more than that
+    say("window large scores", scale, dt)
+    g = gen(14)
+    for B, T, H, K, D in ((1, 300, 2, 1, 64), (1, 150, 4, 4, 128), (3, 140, 128, 2, 16)):
+        q, k, v = (rnd(g, (B, T, h, D), dt).to(DEV) for h in (H, K, K))
+        for window, sinks in ((None, 0), (70, 3)):
+            o = f64(tk.window_attention(q, k, v, window, sinks, scale=scale))
+            want = ref.window_attention(f64(q), f64(k), f64(v), window, sinks, scale=scale)
+            assert np.isfinite(o).all(), (T, window)
+            top = np.abs(f64(v)).max()
+            assert np.abs(o).max() <= top * (1 + 2 * U[dt])
+            sure = ahead(f64(q), f64(k), scale, window, sinks)
+            assert sure.mean() > 0.5
+            assert np.abs(o - want)[sure].max() <= U[dt] * top * (1 + 2 * U[dt]) + 2.0 ** -15 * top, (T, window)
+
+
+def ahead(q, k, scale, window, sinks):
+    """(B, T, H): is one token ahead of all others by twice what fp32 scores err by, and 32 more?"""
+    B, T, H, D = q.shape
+    kk = np.repeat(k, H // k.shape[2], 2)
+    s = scale * np.einsum("bihd,bjhd->bhij", q, kk)
+    mag = abs(scale) * np.einsum("bihd,bjhd->bhij", np.abs(q), np.abs(kk)).max()
+    i, j = np.arange(T)[:, None], np.arange(T)[None]
+    s[..., ~((j <= i) & ((i - j < (window or T)) | (j < sinks)))] = -np.inf
+    s.sort()
+    second = np.where(np.isfinite(s[..., -2]), s[..., -2], s[..., -1] - 1e300)
+    return (s[..., -1] - second > 2 * (D + 6) * 2.0 ** -24 * mag + 32).transpose(0, 2, 1)
