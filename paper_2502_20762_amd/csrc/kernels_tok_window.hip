@@ -125,8 +125,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   typedef typename E::V8 V8;
   typedef typename E::V4 V4;
   constexpr bool F = __is_same(E, F16);
-  constexpr int VW = NV == 1 ? 32 : NV == 2 ? 64 : 128;  // LDS row of values
-  constexpr int KB = kTile * DP * 2, STAGE = KB + kTile * VW * 2;
+  constexpr int VW = NV == 1 ? 32 : NV == 4 ? 128 : 64;  // LDS row of values; of 96 the last 32 in a tile of their own
+  constexpr int KB = kTile * DP * 2, VB = kTile * VW * 2, STAGE = KB + kTile * NV * 64;
   constexpr uint32_t INF = F ? 0x7c00 : 0x7f80;
   // Weights are held at 2^off of exp(score - base), and base is let lag 2^lag behind the
   // maximum, so that outputs are seldom rescaled: fp16 terms stay below 2^15 and keep the
@@ -184,7 +184,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
         char* to = lds + ((t / KS & 1) * KS + x) * STAGE;
         const int j0 = key0(t + x), rows = (int)min((int64_t)kTile, len - j0);
         stage_tile<E, DP, DMA>(to, k + (int64_t)j0 * s.k_token_stride, s.k_token_stride, rows, D, wave, lane);
-        stage_tile<E, VW, DMA>(to + KB, v + (int64_t)j0 * s.v_token_stride, s.v_token_stride, rows, V, wave, lane);
+        stage_tile<E, VW, DMA>(to + KB, v + (int64_t)j0 * s.v_token_stride, s.v_token_stride, rows, min(V, VW), wave, lane);
+        if (NV == 3)
+          stage_tile<E, 32, DMA>(to + KB + VB, v + (int64_t)j0 * s.v_token_stride + 64, s.v_token_stride, rows, V - 64, wave, lane);
       }
     };
     stage(0);
@@ -216,6 +218,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     }
     const int ro = row_offset<DP>(lane);
     const int pv0 = col_offset<VW, false>(lane, 0), pv1 = col_offset<VW, false>(lane, 1);
+    const int pw0 = VB + col_offset<32, false>(lane, 0), pw1 = VB + col_offset<32, false>(lane, 1);
+    // columns 32 y .. of values 16 x .. of a tile
+    const auto columns = [&](const char* vt, int y, int x) {
+      return NV == 3 && y == 2 ? read_cols<E>(vt + pw0 + 32 * 32 * x, vt + pw1 + 32 * 32 * x)
+                               : read_cols<E>(vt + (pv0 ^ (64 * y)) + 32 * VW * x, vt + (pv1 ^ (64 * y)) + 32 * VW * x);
+    };
     float base = kNothing;  // what is taken from each score, times c
     float cl = c;           // 1: the lane's query has large scores, multiplied already
     bool large = false;     // has any of the wave's?
@@ -308,7 +316,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       const auto values = [&](int y) {
 #pragma unroll
         for (int x = 0; x < 4; ++x)
-          vf[y & 1][x] = read_cols<E>(vt + ((pv0 ^ (64 * y)) + 32 * VW * x), vt + ((pv1 ^ (64 * y)) + 32 * VW * x));
+          vf[y & 1][x] = columns(vt, y, x);
       };
       values(0);
 #pragma unroll
@@ -364,7 +372,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
           V8 vf[4];
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            vf[x] = read_cols<E>(vt + ((pv0 ^ (64 * y)) + 32 * VW * x), vt + ((pv1 ^ (64 * y)) + 32 * VW * x));
+            vf[x] = columns(vt, y, x);
           if (!all && any_not_finite(vf, INF)) {
             // a product would carry it to queries that do not see it too (0 times NaN): it is
             // taken out, and counted for those that do
