@@ -485,8 +485,9 @@ hipError_t go(WindowRun run, hipStream_t st) {
 template <class E, int DP, int NV, bool DMA>
 hipError_t by_blocks(const WindowRun& run, hipStream_t st) {
   const ncodec_window_shape& s = run.a.s;
-  return window_halves(s.batch * s.heads, s.tokens, s.head_dim, s.value_dim) ? go<E, DP, NV, DMA, 2>(run, st)
-                                                                             : go<E, DP, NV, DMA, 1>(run, st);
+  return window_halves(s.batch * s.heads, s.tokens, s.head_dim, s.value_dim, s.window, s.sinks, run.a.lengths)
+             ? go<E, DP, NV, DMA, 2>(run, st)
+             : go<E, DP, NV, DMA, 1>(run, st);
 }
 template <class E, int DP, bool DMA>
 hipError_t by_value(const WindowRun& run, hipStream_t st) {

@@ -89,15 +89,22 @@ inline DecayPlan decay_rule(int64_t bh, int64_t tokens, int64_t value_dim) {
 // ---- attention with a window
 // Whether a workgroup's four waves share 64 queries, two waves a query on alternate tiles
 // of keys, instead of 128: twice the workgroups, of half the length, for up to twice the
-// loads of keys and values.  bh: batch * heads.  us whole / in halves, 64 x 64 heads, all
-// earlier tokens seen: 8 heads of 200 tokens 10.8 / 8.9, 1560 32 / 21, 8160 159 / 135, 16,000 with
-// a window of 4080 (1000 workgroups of 128 queries) 226 / 224.  With wider heads the tiles in
-// halves leave room for one workgroup a CU: 128 x 128, 8 heads over 2 of 1560 tokens (104
-// workgroups) 43 / 29, 16 over 4 of 3000 (384) 86 / 91, 8 of 8160 with a window of 2000 (512)
-// 108 / 146.  Up to 64 tokens there is but one tile.
-inline bool window_halves(int64_t bh, int64_t tokens, int64_t head_dim, int64_t value_dim) {
-  const int64_t blocks = bh * ((tokens + 127) / 128);
-  return tokens > 64 && blocks <= (head_dim <= 64 && value_dim <= 64 ? 1000 : 256);
+// loads of keys and values.  bh: batch * heads, ragged: lengths are given.
+// What is won is the time of the longest workgroup, what is lost the room of a CU, two workgroups of
+// halves with heads up to 64 x 96 and one with wider ones.  As long as all of them fit at once, halves
+// win; where 1024 tokens are seen, up to twice as many, and in a ragged batch, whose sequences take
+// half as long, up to twice as many again.  us whole / in halves, in brackets ragged, workgroups of 128
+// queries of 8 heads of 64 x 64: 8 and 16 x 195 tokens (128, 256) 10.2 / 8.5, 10.8 / 9.8, 32 x 195 (512)
+// 11.3 / 16.5; 8 x 780 (448) 21.5 / 23.8 (19.7 / 15.3); 4, 5 and 8 x 1560 (416, 520, 832) 33.2 / 30.2
+// (32.5 / 23.0), 35.0 / 35.4, 44.4 / 52.8 (34.0 / 29.8); 16 x 1560 (1664) 77.8 / 97.8 (34.8 / 45.4); 1 x 8160
+// (512) 159 / 132, with a window of 4080 106 / 107.  128 x 128: 4, 8 and 16 x 195 (64, 128, 256) 13.9 / 10.5, 14.1 / 10.8,
+// 15.2 / 19.2; 2, 3 and 4 x 1560 (208, 312, 416) 43.3 / 33.5, 45.5 / 48.9, 49.4 / 60.1 (45.8 / 36.2).
+// Up to 64 tokens there is but one tile.
+inline bool window_halves(int64_t bh, int64_t tokens, int64_t head_dim, int64_t value_dim, int64_t window = 0,
+                          int64_t sinks = 0, bool ragged = false) {
+  const int64_t blocks = bh * ((tokens + 127) / 128), seen = window && window + sinks < tokens ? window + sinks : tokens;
+  const int64_t fit = head_dim <= 64 && value_dim <= 96 ? 256 : 128;
+  return tokens > 64 && blocks <= fit * (seen >= 1024 ? 2 : 1) * (ragged && seen >= 512 ? 2 : 1);
 }
 
 // The tiles of 64 keys that the queries i0 .. i0 + queries - 1 of a sequence of `len` tokens see:

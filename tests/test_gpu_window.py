@@ -395,3 +395,13 @@ def ahead(q, k, scale, window, sinks):
     s.sort()
     second = np.where(np.isfinite(s[..., -2]), s[..., -2], s[..., -1] - 1e300)
     return (s[..., -1] - second > 2 * (D + 6) * 2.0 ** -24 * mag + 32).transpose(0, 2, 1)
+
+
+@pytest.mark.parametrize("D,V", [(64, 64), (40, 96), (128, 128)])
+@pytest.mark.parametrize("H,K", [(32, 8), (9, 3), (15, 15)])
+def test_ragged_batches_of_many_blocks(H, K, D, V):
+    # sequences take turns over the places of a launch, whatever number of them there is
+    say("window many ragged", H, K, D, V)
+    B = 10
+    run(B, 150, H, K, D, V, "bf16", 70, 3, lengths=[(150, 0, 1)[b] if b < 3 else 37 * b % 151 for b in range(B)])
+    run(1, 150, H, K, D, V, "fp16", None, 0, lengths=[131])
