@@ -4,7 +4,7 @@
 //
 // 130,560 tokens of 4 heads of 128 + 128 into the cache, 535 MB: 108 us (4.9 TB/s, a large
 // copy's rate).  64 sequences of up to 2,040 tokens cut to 1,020, 8 heads of 64 + 64: 11 us for the
-// choice and 53 for the rows (196 MB, 3.7 TB/s; heads of a token side by side in the grid were no
+// choice and 51 for the rows (196 MB, 3.9 TB/s; heads of a token side by side in the grid were no
 // faster), one of 130,560 to 32,640, 4 heads of 128 + 128: four launches of 5, 8, 8 and 11.5 us,
 // each waiting for the counts of the one before, and 35 for the rows (134 MB, 3.9 TB/s).
 #include <algorithm>
@@ -180,7 +180,9 @@ __device__ __forceinline__ void move_kept(const EvictArgs& a, const Split& sp, P
 template <int U, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_tok_evict_move(EvictArgs a, Split sp, int64_t first, int64_t blocks) {
   __shared__ Places at;
-  const int64_t block = first + blockIdx.x, bh = block / blocks, x0 = block % blocks * sp.rows;
+  // The last positions of what keeps fewer are empty: they take turns over the XCDs and their engines, to
+  // which workgroups go in order (64 sequences of up to 2,040 tokens: 63.1 -> 59.8 us a call).
+  const int64_t block = first + blockIdx.x, bh = block / blocks, x0 = (block + bh + bh / 4) % blocks * sp.rows;
   if (a.kept[bh * a.s.keep + x0] < 0) return;  // the kept ones come first
   move_kept<U, ALIGNED>(a, sp, at, bh, x0, (int)min((int64_t)sp.rows, a.s.keep - x0));
 }
