@@ -260,9 +260,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_tok_paged(PagedRun run) {
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
-  any = any || __shfl_xor((int)any, 16, 64);
-  any = any || __shfl_xor((int)any, 32, 64);
-  if (any && m == -__builtin_huge_valf() && l == 0.f) l = kAllMinusInf;
+  // what is seen is so for all heads, but each lane has looked at eight of a step's positions only
+  if (__any(any) && m == -__builtin_huge_valf() && l == 0.f) l = kAllMinusInf;
 
   // the waves together: element 4 VW g4 + VW r + i of head m16 is o[i][r]
 #pragma unroll
