@@ -39,7 +39,7 @@ struct PagedRun {
   bool q_runs;      // queries are whole 16-byte runs
   int64_t zstride;  // scores of a head in the workspace; 0: they are not kept
   float2* ml;       // batch x heads x splits: maximum and sum
-  float* o;         // batch x heads x splits x value_dim: sums of weighted values
+  float* o;         // batch x heads x splits x value_dim: means of the values
   float* z;         // batch x heads x zstride: scores
 };
 
@@ -61,6 +61,20 @@ __device__ __forceinline__ Steps steps_of(const Seen& s, int n) {
   r.from = max(s.near / kStep, r.lead);
   r.count = n > 0 ? r.lead + max(0, (n + kStep - 1) / kStep - r.from) : 0;
   return r;
+}
+
+// Steps of a split: whole rounds of the workgroup's waves.
+__device__ __forceinline__ int share_of(const Steps& s, int splits) {
+  return ((s.count + splits - 1) / splits + kWaves - 1) / kWaves * kWaves;
+}
+// log2 of the largest weight as the sums hold it.  fp16: its terms keep 2^-38 of that.  bf16: a wave's
+// weights sum up to 1 at most, so that no sum of weighted values leaves fp32 where their mean does not, and none is
+// smaller than it has to be: up to 2^16 positions a wave, a value of 2^-126 that has all the weight keeps its bits
+// above fp32's last, 2^-149.  The sums join as means.
+template <class E>
+__device__ __forceinline__ float top_power(int share) {
+  if (__is_same(E, F16)) return 14.f;
+  return (float)__clz(max(1, share / kWaves) * kStep - 1) - 32.f;
 }
 
 // N elements from p; those from `left` on, or all where !in, are zero.  VEC: whole
@@ -89,7 +103,6 @@ __global__ __launch_bounds__(64 * kWaves) void k_tok_paged(PagedRun run) {
   typedef typename E::T T;
   typedef typename E::V8 V8;
   typedef uint32_t U4 __attribute__((ext_vector_type(4)));
-  constexpr bool F = __is_same(E, F16);
   constexpr int VP = 16 * VW;
   __shared__ float part[kWaves][kHeads][VP + 4], ml[kWaves][2][kHeads];
   const PagedArgs& a = run.a;
@@ -112,8 +125,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_tok_paged(PagedRun run) {
   const int n = (int)min(max((int64_t)a.lengths[b], (int64_t)0), cap);
   const Seen seen = seen_by(n - 1, s.window, s.sinks);
   const Steps steps = steps_of(seen, n);
-  // a split takes whole rounds of the workgroup's waves
-  const int per = ((steps.count + run.splits - 1) / run.splits + kWaves - 1) / kWaves * kWaves;
+  const int per = share_of(steps, run.splits);
   const int x0 = split * per, x1 = min(x0 + per, steps.count);
   const int shift = __ffs(c.page_size) - 1;
   cint* table = (cint*)(a.table + b * s.table_stride);
@@ -171,7 +183,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_tok_paged(PagedRun run) {
     }
   };
 
-  const float scale = s.scale * 1.44269504088896341f, off = F ? 14.f : -kBelow;
+  const float scale = s.scale * 1.44269504088896341f, off = top_power<E>(per);
   floatx4 o[VW] = {};
   float m = -__builtin_huge_valf(), l = 0.f;
   bool any = false;
@@ -275,7 +287,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_tok_paged(PagedRun run) {
   __syncthreads();
   for (int it = threadIdx.x; it < nh * VP; it += 64 * kWaves) {
     const int h = it / VP, d = it % VP;
-    float M = ml[0][0][h], L = 0.f, O = 0.f;
+    float M = ml[0][0][h], L = 0.f, O = 0.f, f[kWaves];
 #pragma unroll
     for (int y = 1; y < kWaves; ++y) M = fmaxf(M, ml[y][0][h]);
     bool none = false;
@@ -283,13 +295,15 @@ __global__ __launch_bounds__(64 * kWaves) void k_tok_paged(PagedRun run) {
     for (int y = 0; y < kWaves; ++y) {
       const float my = ml[y][0][h], ly = ml[y][1][h];
       none = none || ly == kAllMinusInf;
-      const float f = my == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(my - M);
-      L = fmaf(ly, f, L);  // also where f is 0: what is no number stays so
-      O = fmaf(part[y][h][d], f, O);
+      f[y] = my == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(my - M);
+      L = fmaf(ly, f[y], L);  // also where f is 0: what is no number stays so
     }
+    const float by = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+    for (int y = 0; y < kWaves; ++y) O = fmaf(part[y][h][d], f[y] * by, O);
     if (none && L == 0.f) L = kAllMinusInf;
     if (run.splits == 1 && d < V)
-      ((T*)a.o)[b * s.o_batch_stride + (h0 + h) * s.o_head_stride + d] = (T)(L == 0.f ? 0.f : O / (L == kAllMinusInf ? __builtin_nanf("") : L));
+      ((T*)a.o)[b * s.o_batch_stride + (h0 + h) * s.o_head_stride + d] = (T)(L == 0.f ? 0.f : L == kAllMinusInf ? __builtin_nanf("") : O);
     const int64_t to = (bh0 + h) * run.splits + split;
     if (run.ml && d == 0) run.ml[to] = float2{M, L};
     if (run.splits > 1 && d < V) run.o[to * V + d] = O;
@@ -308,7 +322,7 @@ __global__ __launch_bounds__(1024) void k_tok_paged_join(PagedRun run, int heads
   const ncodec_cache_shape& c = a.c;
   const ncodec_paged_shape& s = a.s;
   const int V = c.value_dim, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  // maximum and 1 / sum of head bh, in every lane of a wave; f: what the splits' sums count
+  // maximum and 1 / sum of head bh, in every lane of a wave; f: what the splits' means count
   const auto join = [&](int64_t bh, float (&f)[kMaxSplits / 64]) {
     const float2* ml = run.ml + bh * run.splits;
     float M = -__builtin_huge_valf(), L = 0.f, m[kMaxSplits / 64], l[kMaxSplits / 64];
@@ -329,7 +343,10 @@ __global__ __launch_bounds__(1024) void k_tok_paged_join(PagedRun run, int heads
     }
     for (int w = 32; w; w >>= 1) L += __shfl_xor(L, w, 64);
     if (__any(none) && L == 0.f) L = __builtin_nanf("");
-    return float2{M, L == 0.f ? 0.f : 1.f / L};
+    const float by = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+    for (int y = 0; y < kMaxSplits / 64; ++y) f[y] *= l[y] * by;
+    return float2{M, by};
   };
   if ((int)blockIdx.x < heads_blocks) {
     const int64_t bh = blockIdx.x, b = bh / s.heads;
@@ -365,7 +382,7 @@ __global__ __launch_bounds__(1024) void k_tok_paged_join(PagedRun run, int heads
     if (d < V) {
       float O = 0.f;
       for (int w = 0; w < waves; ++w) O += sums[w][d];
-      ((T*)a.o)[b * s.o_batch_stride + (bh - b * s.heads) * s.o_head_stride + d] = (T)(ml.y == 0.f ? 0.f : O * ml.y);
+      ((T*)a.o)[b * s.o_batch_stride + (bh - b * s.heads) * s.o_head_stride + d] = (T)(ml.y == 0.f ? 0.f : O);
     }
     return;
   }
@@ -386,7 +403,7 @@ __global__ __launch_bounds__(1024) void k_tok_paged_join(PagedRun run, int heads
   }
   __syncthreads();
   float* mass = a.mass + (int64_t)bk * cap;
-  const float off = __is_same(E, F16) ? 14.f : -kBelow;  // the sums hold weights 2^off of the largest
+  const float off = top_power<E>(share_of(steps_of(seen, n), run.splits));
   for (int64_t x = block * (int64_t)blockDim.x + threadIdx.x; x < seen.count; x += (int64_t)mass_blocks * blockDim.x) {
     const int j = seen.at((int)x);
     const int32_t page = a.table[b * s.table_stride + (j >> shift)];

@@ -18,8 +18,4 @@ __device__ __forceinline__ Seen seen_by(int i, int64_t window, int64_t sinks) {
   return s;
 }
 
-// Weights are held 2^-32 below the largest, so that no sum of weighted values leaves
-// fp32 where their mean does not, for up to 2^31 tokens.
-constexpr float kBelow = 32.f;
-
 }  // namespace nc

@@ -1,0 +1,65 @@
+"""Values at both ends of bf16's range: a weighted mean of them is one of them, or lies between them.
+
+Sums of weighted values are fp32 with the largest weight held below 1, at 2^-14 or above where one token has all the weight,
+so that a product with a value of 2^-126 has its last bit at 2^-149: an addition of it errs by 2^-150, which is 2^-136 of an
+output, and there are two for the two terms of the weight.  Halved steps of bf16 there are 2^-134."""
+import numpy as np
+import pytest
+import torch
+
+from attention_util import DEV, Cache, U, f64, gen, rnd, say
+from paper_2502_20762_amd import tokens as tk
+from test_gpu_paged import i32
+
+pytestmark = pytest.mark.gpu
+
+BF, HALF_STEP = torch.bfloat16, 2.0 ** -134
+
+
+def small(g, shape, power):
+    """bf16 numbers of both signs between 2^power and 2^(power + 1)."""
+    x = torch.randint(128, 256, shape, generator=g).double() * torch.where(torch.rand(shape, generator=g) < 0.5, -1.0, 1.0)
+    return (x * 2.0 ** (power - 7)).to(BF)
+
+
+@pytest.mark.parametrize("power", [-90, -105, -109, -112, -117, -120, -125, -126])
+@pytest.mark.parametrize("n", [1, 40, 300, 3000, 20000])
+def test_paged_one_token_has_all_the_weight(n, power):
+    say("paged small", n, power)
+    c = Cache(gen(5), 1, n, 16, 1, 64, 128, "bf16")
+    q = torch.zeros((1, 2, 64), dtype=BF, device=DEV)
+    q[..., 0] = 32.0
+    c.v.copy_(small(gen(6), c.v.shape, power))
+    for at in (0, n // 3, n - 1):
+        c.k.zero_()
+        page, row = int(c.table[0, at // 16]), at % 16
+        c.k[page, row, 0, 0] = 16.0
+        want = f64(c.v[page, row, 0])
+        for mass in (None, torch.zeros((1, 1, c.columns), device=DEV)):
+            o = f64(tk.paged_attention(q, c.k, c.v, c.table, i32([n]), scale=1.0, mass=mass))
+            assert (np.abs(o - want) <= U["bf16"] * np.abs(want) + HALF_STEP + 2 * 2.0 ** -136).all(), at
+        assert float(mass[0, 0, at]) == 2.0 and float(mass.sum()) == 2.0
+
+
+@pytest.mark.parametrize("power", [-90, -109, -117, -126])
+@pytest.mark.parametrize("n", [50, 3000, 20000])
+def test_paged_all_weigh_the_same(n, power):
+    c = Cache(gen(7), 1, n, 16, 1, 64, 64, "bf16")
+    v = small(gen(8), (64,), power).to(DEV)
+    c.v.copy_(v.expand_as(c.v))
+    o = f64(tk.paged_attention(torch.ones((1, 2, 64), dtype=BF, device=DEV), c.k, c.v, c.table, i32([n]), scale=0.0))
+    assert (np.abs(o - f64(v)) <= (U["bf16"] + 2.0 ** -15 + n * 2.0 ** -24) * np.abs(f64(v)) + HALF_STEP + 2.0 ** -135).all()
+
+
+@pytest.mark.parametrize("n", [50, 3000, 20000, 130560])
+@pytest.mark.parametrize("scale", [0.0, 0.1, 1.0])
+def test_paged_means_of_the_largest_values(n, scale):
+    top = float(torch.finfo(BF).max)
+    for B in (1, 70):
+        if B * n > 300000:
+            continue
+        c = Cache(gen(9), B, n, 64, 1, 64, 64, "bf16")
+        c.v.fill_(top)
+        c.v[..., 32:] *= -1
+        o = tk.paged_attention(rnd(gen(10), (B, 2, 64), "bf16").to(DEV), c.k, c.v, c.table, i32([n] * B), scale=scale)
+        assert bool((o == c.v[0, 0]).all())
