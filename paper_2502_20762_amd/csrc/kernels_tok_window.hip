@@ -129,10 +129,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   constexpr int VW = NV == 1 ? 32 : NV == 4 ? 128 : 64;  // LDS row of values; of 96 the last 32 in a tile of their own
   constexpr int KB = kTile * DP * 2, VB = kTile * VW * 2, STAGE = KB + kTile * NV * 64;
   constexpr uint32_t INF = F ? 0x7c00 : 0x7f80;
-  // Weights are held at 2^off of exp(score - base), and base is let lag 2^lag behind the
-  // maximum, so that outputs are seldom rescaled: fp16 terms stay below 2^15 and keep the
-  // bits above 2^-32 of the largest weight, bf16 ones leave room for 2^31 tokens.
-  constexpr float off = F ? 7.f : -40.f, lag = 8.f;
+  // Weights are held at 2^off of the largest, which is let grow to 2^lag of that before the
+  // outputs are rescaled.  fp16 terms stay below 2^15 and keep the bits above 2^-32 of the largest weight.  In
+  // bf16 the values have fp32's range: weights add up to less than a half, 64 of 2^-8 at most to an eighth, and
+  // beyond that all are taken down by 2^8, so that no sum leaves fp32 where the mean does not; and where one token
+  // has all the weight, its value of 2^-126 ends above fp32's last bit.
+  constexpr float off = F ? 7.f : -14.f, lag = F ? 8.f : 6.f, kFull = 0x1p-4f;
   // Scores whose product with c this large a number is would, rounded once for the base and not
   // at all in the weights, leave that room: they are multiplied first.
   constexpr float kLarge = 0x1p22f, kNothing = -0x1.fffffep127f;
@@ -262,7 +264,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       float top = fmaxf(p[0][0], p[1][0]);
 #pragma unroll
       for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, p[0][r]), p[1][r]);
-      if (__any(fmaf(top, cl, -base) > off + lag)) {
+      if (__any(fmaf(top, cl, -base) > off + lag || (!F && sum > kFull))) {
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
         top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
         // each query by its own scores, whatever the wave's others are
@@ -275,8 +277,15 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
           cl = now ? 1.f : cl;
           large = true;
         }
-        const float base1 = rises ? fmaf(top, cl, -off) : base;
-        const float fade = rises ? __builtin_amdgcn_exp2f(base - base1) : 1.f;
+        float base1 = fmaf(top, cl, -off);
+        bool moves = rises;
+        if (!F) {
+          const auto su = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+          base1 = rises ? base1 : base + 8.f;
+          moves = rises || __uint_as_float(su[0]) + __uint_as_float(su[1]) > kFull;
+        }
+        base1 = moves ? base1 : base;
+        const float fade = moves ? __builtin_amdgcn_exp2f(base - base1) : 1.f;
         base = base1;
         sum *= fade;
 #pragma unroll

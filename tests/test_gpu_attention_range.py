@@ -22,6 +22,49 @@ def small(g, shape, power):
     return (x * 2.0 ** (power - 7)).to(BF)
 
 
+def peaked(T, D, at):
+    """Queries and keys whose scores, scale 1, are 0 but for key `at`: 512, past the range of exp, for the tokens from it on;
+    one token has all the weight."""
+    q, k = torch.zeros((1, T, 1, D), dtype=BF), torch.zeros((1, T, 1, D), dtype=BF)
+    q[..., 0] = 32.0
+    k[0, at, 0, 0] = 16.0
+    return q, k
+
+
+@pytest.mark.parametrize("power", [-90, -101, -105, -109, -112, -117, -120, -125, -126])
+@pytest.mark.parametrize("D,T", [(64, 40), (64, 300), (128, 300), (32, 2500)])
+def test_window_one_token_has_all_the_weight(D, T, power):
+    say("window small", D, T, power)
+    v = small(gen(1), (1, T, 1, D), power)
+    for at in (0, T // 3, T - 1):
+        q, k = peaked(T, D, at)
+        o = f64(tk.window_attention(q.to(DEV), k.to(DEV), v.to(DEV), scale=1.0))[0, at:, 0]
+        want = f64(v)[0, at, 0]
+        assert (np.abs(o - want) <= U["bf16"] * np.abs(want) + HALF_STEP + 2 * 2.0 ** -136).all(), at
+
+
+@pytest.mark.parametrize("power", [-90, -101, -109, -117, -126])
+@pytest.mark.parametrize("T", [50, 300, 3000])
+def test_window_all_weigh_the_same(T, power):
+    # of n equal values: n products, each rounded to 2^-149 with the sum at 2^-14 of it at least, beside the weights' 2^-16
+    v = small(gen(2), (1, 1, 1, 64), power).expand(1, T, 1, 64)
+    q = rnd(gen(3), (1, T, 1, 64), "bf16").to(DEV)
+    o = f64(tk.window_attention(q, q, v.to(DEV), scale=0.0))
+    assert (np.abs(o - f64(v)) <= (U["bf16"] + 2.0 ** -15 + T * 2.0 ** -24) * np.abs(f64(v)) + HALF_STEP + 2.0 ** -135).all()
+
+
+@pytest.mark.parametrize("T,window,sinks", [(300, None, 0), (20000, None, 0), (9000, 3000, 70)])
+@pytest.mark.parametrize("scale", [0.0, 0.1, 1.0])
+def test_window_means_of_the_largest_values(T, window, sinks, scale):
+    say("window large values", T, window, sinks, scale)
+    top = float(torch.finfo(BF).max)
+    q = rnd(gen(4), (1, T, 1, 64), "bf16").to(DEV)
+    v = torch.full((1, T, 1, 64), top, device=DEV).to(BF)
+    v[..., 32:] *= -1
+    o = tk.window_attention(q, q, v, window, sinks, scale=scale)
+    assert torch.isfinite(o).all() and bool((o == v).all())
+
+
 @pytest.mark.parametrize("power", [-90, -105, -109, -112, -117, -120, -125, -126])
 @pytest.mark.parametrize("n", [1, 40, 300, 3000, 20000])
 def test_paged_one_token_has_all_the_weight(n, power):
