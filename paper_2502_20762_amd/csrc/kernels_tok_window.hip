@@ -136,8 +136,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   // has all the weight, its value of 2^-126 ends above fp32's last bit.
   constexpr float off = F ? 7.f : -14.f, lag = F ? 8.f : 6.f, kFull = 0x1p-4f;
   // Scores whose product with c this large a number is would, rounded once for the base and not
-  // at all in the weights, leave that room: they are multiplied first.
-  constexpr float kLarge = 0x1p22f, kNothing = -0x1.fffffep127f;
+  // at all in the weights, leave that room: they are multiplied first, and the largest is taken from them, which
+  // then weighs 2^far_off.  In fp16 that is lower than off: one that is 2^15 larger by the unrounded product, up to
+  // which no rise is looked for, may be 2^17 larger by the rounded one.
+  constexpr float kLarge = 0x1p22f, kNothing = -0x1.fffffep127f, far_off = F ? -2.f : off;
   __shared__ __align__(1024) char lds[2 * KS * STAGE];
   const WindowArgs& a = run.a;
   const ncodec_window_shape& s = a.s;
@@ -227,9 +229,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       return NV == 3 && y == 2 ? read_cols<E>(vt + pw0 + 32 * 32 * x, vt + pw1 + 32 * 32 * x)
                                : read_cols<E>(vt + (pv0 ^ (64 * y)) + 32 * VW * x, vt + (pv1 ^ (64 * y)) + 32 * VW * x);
     };
-    float base = kNothing;  // what is taken from each score, times c
-    float cl = c;           // 1: the lane's query has large scores, multiplied already
-    bool large = false;     // has any of the wave's?
+    // a weight is 2^(score * c - base), of a lane whose query has large scores 2^((score * c - base) + far_off)
+    float base = kNothing;
+    bool far = false, large = false;  // has the lane's query, has any of the wave's large scores?
+    float cl = c, less = 0.f;         // what follow() leaves: a weight is 2^(score * cl - less)
 
     // does any of the wave's queries see any of the tile's keys?
     const auto some = [&](int j0) { return j0 < wend && (j0 < sinks || wi0 - (j0 + kTile - 1) < window); };
@@ -252,46 +255,48 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
         p[1] = E::mfma(kf[x][1], qf[x], p[1]);
       }
     };
-    const auto multiply = [&](floatx16(&p)[2], float by) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        p[0][r] *= by;
-        p[1][r] *= by;
-      }
+    const auto rounded = [&](float f) {  // f c
+      f *= c;
+      asm("" : "+v"(f));  // no multiply-add
+      return f;
     };
+    // log2 of the weight of score f
+    const auto power = [&](float f) { return far ? (rounded(f) - base) + far_off : fmaf(f, c, -base); };
     const auto follow = [&](floatx16(&p)[2]) {  // the base after the maximum
-      if (large) multiply(p, cl == c ? 1.f : c);
       float top = fmaxf(p[0][0], p[1][0]);
 #pragma unroll
       for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, p[0][r]), p[1][r]);
-      if (__any(fmaf(top, cl, -base) > off + lag || (!F && sum > kFull))) {
+      if (__any(fmaf(top, c, -base) > off + lag || (!F && sum > kFull))) {  // of large scores: at least where power() is
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
         top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
         // each query by its own scores, whatever the wave's others are
-        const bool rises = fmaf(top, cl, -base) > off + lag;
-        const bool now = rises && cl == c && fabsf(top * cl) >= kLarge;
-        if (__any(now)) {
-          top *= now ? c : 1.f;
-          asm("" : "+v"(top));  // rounded, as the scores are
-          multiply(p, now ? c : 1.f);
-          cl = now ? 1.f : cl;
-          large = true;
-        }
-        float base1 = fmaf(top, cl, -off);
+        const bool rises = power(top) > off + lag, now = rises && !far && fabsf(top * c) >= kLarge;
+        far = far || now;
+        large = large || __any(now);
+        float base1 = far ? rounded(top) : fmaf(top, c, -off);
         bool moves = rises;
         if (!F) {
           const auto su = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
           base1 = rises ? base1 : base + 8.f;
           moves = rises || __uint_as_float(su[0]) + __uint_as_float(su[1]) > kFull;
         }
-        base1 = moves ? base1 : base;
-        const float fade = moves ? __builtin_amdgcn_exp2f(base - base1) : 1.f;
-        base = base1;
+        const float fade = moves ? __builtin_amdgcn_exp2f((base - base1) + (now ? far_off : 0.f)) : 1.f;
+        base = moves ? base1 : base;
         sum *= fade;
 #pragma unroll
         for (int x = 0; x < NV; ++x)
 #pragma unroll
           for (int r = 0; r < 16; ++r) out[x][r] *= fade;
+      }
+      less = base;
+      if (large) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          p[0][r] = power(p[0][r]);
+          p[1][r] = power(p[1][r]);
+        }
+        cl = 1.f;
+        less = 0.f;
       }
     };
     // weights of keys 16 x .. of a tile
@@ -299,7 +304,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       float w[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        w[e] = __builtin_amdgcn_exp2f(fmaf(p[x >> 1][8 * (x & 1) + e], cl, -base));
+        w[e] = __builtin_amdgcn_exp2f(fmaf(p[x >> 1][8 * (x & 1) + e], cl, -less));
         sum += w[e];
       }
       weight_terms(w, hi, lo);
@@ -418,7 +423,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       constexpr int STEP = kWaves / KS * 64 * 4;
       lds_barrier();
       if (ks) {
-        *(floatx4*)mine = floatx4{base, sum, 0.f, 0.f};
+        *(floatx4*)mine = floatx4{base, sum, far ? 1.f : 0.f, 0.f};
 #pragma unroll
         for (int x = 0; x < 4 * NV; ++x)
           *(floatx4*)(mine + (x + 1) * STEP) =
@@ -427,8 +432,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       lds_barrier();
       if (ks) return;
       const floatx4 other = *(const floatx4*)mine;
-      const float b1 = fmaxf(base, other[0]);
-      const float f0 = __builtin_amdgcn_exp2f(base - b1), f1 = __builtin_amdgcn_exp2f(other[0] - b1);
+      // by which power of two a weight of this half counts less than one of the other
+      const float d = (other[0] - base) + far_off * ((far ? 1.f : 0.f) - other[2]);
+      const float f0 = __builtin_amdgcn_exp2f(fminf(-d, 0.f)), f1 = __builtin_amdgcn_exp2f(fminf(d, 0.f));
       sum = sum * f0 + other[1] * f1;
 #pragma unroll
       for (int x = 0; x < 4 * NV; ++x) {

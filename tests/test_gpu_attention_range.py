@@ -65,6 +65,38 @@ def test_window_means_of_the_largest_values(T, window, sinks, scale):
     assert torch.isfinite(o).all() and bool((o == v).all())
 
 
+@pytest.mark.parametrize("scale", [1.0, 1e3, 1e6, 1e8, 1e10, 3e15, 1e25])
+@pytest.mark.parametrize("T", [40, 700])
+def test_window_ties_of_large_scores_over_the_largest_values(T, scale):
+    top = float(torch.finfo(BF).max)
+    for D in (64, 128):
+        x = torch.ones((2, T, 1, D), device=DEV, dtype=BF)
+        v = torch.full_like(x, top)
+        x[1, T // 3:] = 0.5  # the tokens in front are ahead by half the score
+        o = tk.window_attention(torch.ones_like(x), x, v, scale=scale)
+        assert bool((o == v).all())
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("step", [3, 6, 8, 10, 12, 20])
+@pytest.mark.parametrize("large", [10, 13, 15, 18])
+def test_window_large_scores_that_rise_from_tile_to_tile(large, step, dt):
+    # from 2^20 to 2^28, by `step` every 64 keys: fp32 scores there err by 2^4 at most (and by nothing at 2^20 or below)
+    T = 1000
+    q, k = torch.zeros((1, T, 1, 64)), torch.zeros((1, T, 1, 64))
+    q[..., 0], k[..., 0] = 32.0, 32.0
+    q[..., 1] = step * 2.0 ** -large if dt == "bf16" or large <= 13 else step * 2.0 ** -13
+    k[..., 1] = (torch.arange(T) // 64).view(1, T, 1) * (1.0 if dt == "bf16" or large <= 13 else 2.0 ** (13 - large))
+    v = rnd(gen(11), (1, T, 1, 64), dt).to(DEV)
+    o = tk.window_attention(q.to(v.dtype).to(DEV), k.to(v.dtype).to(DEV), v, scale=2.0 ** large)
+    top = float(v.float().abs().max())
+    assert torch.isfinite(o).all() and float(o.float().abs().max()) <= top * (1 + 2 * U[dt])
+    if step == 20 and large <= 15:  # what is a tile behind weighs exp(-20 + 2^2 ln 2) at most
+        for i in range(64, T, 97):
+            want = f64(v)[0, i // 64 * 64:i + 1].mean(0)
+            assert np.abs(f64(o)[0, i] - want).max() <= (U[dt] + 2.0 ** -15 + 2 * 64 * np.exp(-17)) * top, i
+
+
 @pytest.mark.parametrize("power", [-90, -105, -109, -112, -117, -120, -125, -126])
 @pytest.mark.parametrize("n", [1, 40, 300, 3000, 20000])
 def test_paged_one_token_has_all_the_weight(n, power):
