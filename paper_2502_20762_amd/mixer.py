@@ -115,7 +115,8 @@ class TokenCache:
         if keep is not None and not 0 < keep < capacity:
             raise ValueError("keep must be in [1, capacity)")
         self.capacity, self.keep, self.sinks, self.recent, self.weigh = capacity, keep, sinks, recent, weigh
-        self.most = 0  # tokens of the fullest stream at most: known without asking the GPU
+        self.most = 0  # tokens of the fullest stream, at most: known without asking the GPU,
+        self.exact = True  # and just that many as long as all streams get the same
         pages = batch * columns
         count = 2 * pages if keep is not None else pages  # an eviction copies to pages that are free
         self.k = torch.zeros((count, page_size, kv_heads, head_dim), dtype=dtype, device=device)
@@ -126,16 +127,25 @@ class TokenCache:
         self.mass = torch.zeros((batch, kv_heads, columns * page_size), device=device) if keep is not None else None
 
     def append(self, k, v, counts=None):
-        """Adds tokens, k and v (batch, tokens, kv_heads, dim); counts: (batch) int32 of each stream (None: all)."""
+        """Adds tokens, k and v (batch, tokens, kv_heads, dim); counts: (batch) int32 of each stream (None: all).  The
+        host waits for the GPU only where streams of different length come near the capacity."""
         T = k.shape[1]
-        held = self.most if self.keep is None else min(self.most, self.keep)
-        if held + T > self.capacity:  # before anything is let go
-            raise ValueError(f"{T} tokens do not fit a cache of {self.capacity} that holds {held} at least")
-        if self.most + T > self.capacity:
+        new = T if counts is None else counts.clamp(0, T)
+        exact = self.exact and counts is None
+        most = self.most + T
+        if most > self.capacity and not exact and len(self.lengths):
+            most, exact = int((self.lengths + new).max()), True
+        if most > self.capacity:
+            left = most  # of the fullest stream, once it is cut back
+            if self.keep is not None:
+                left = min(self.most, self.keep) + T if counts is None else int((self.lengths.clamp(max=self.keep) + new).max())
+            if left > self.capacity:  # before anything is let go
+                raise ValueError(f"{T} tokens do not fit: a stream would hold {left}, and the cache has room for {self.capacity}")
             self.evict()
+            most = left
         cache_append(k, v, self.k, self.v, self.table, self.lengths, counts, self.mass)
-        self.lengths += T if counts is None else counts.clamp(0, T)
-        self.most += T
+        self.lengths += new
+        self.most, self.exact = most, exact
 
     def attend(self, q, window=None, sinks=0):
         """Attention of each stream's last token, q (batch, heads, dim)."""
