@@ -1,9 +1,12 @@
 """The cache of a batch of streams: what it holds and lets go of, against lists of tokens kept on the host."""
+import numpy as np
 import pytest
 import torch
 
-from attention_util import DEV
-from paper_2502_20762_amd.mixer import TokenCache
+from attention_util import DEV, F32, f64, gen, rnd, weight_error
+from paper_2502_20762_amd.mixer import CacheMixer, TokenCache
+from paper_2502_20762_amd.tokens import grid_positions
+from test_gpu_mixer import U, rms
 
 pytestmark = pytest.mark.gpu
 
@@ -102,3 +105,59 @@ def test_streams_of_the_same_length_are_counted_on_the_host():
     for t in range(40):
         s.append([3, 3], given=False)
         assert s.cache.most == int(s.cache.lengths.max()) and s.cache.exact
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("B,T,H,K,window,sinks,counts", [
+    (1, 150, 4, 2, None, 0, None), (1, 64, 2, 2, 30, 3, None), (3, 70, 4, 1, None, 0, [70, 0, 33]),
+    (70, 9, 2, 1, None, 0, [b % 11 - 1 for b in range(70)]), (2, 1, 2, 2, None, 0, None)])
+def test_a_prompt_weighs_what_its_tokens_one_by_one_do(B, T, H, K, window, sinks, counts, dt):
+    # the same weights, each by its error twice, summed in another order
+    g, D, keep, more = gen(5), 64, max(1, T // 2), 40
+    q, k, v = (rnd(g, (B, T + more, h, D), dt).to(DEV) for h in (H, K, K))
+    n = torch.full((B,), T) if counts is None else torch.tensor(counts).clamp(0, T)
+    a, b = (TokenCache(B, T + 8, K, D, keep=keep, sinks=min(2, keep), dtype=q.dtype, device=DEV) for _ in range(2))
+    given = None if counts is None else torch.tensor(counts, dtype=torch.int32, device=DEV)
+    a.append(k[:, :T], v[:, :T], given)
+    a.weigh_prompt(q[:, :T], given, window, sinks)
+    for t in range(T):
+        one = (t < n).to(torch.int32).to(DEV)
+        before = b.mass.clone()
+        b.append(k[:, t:t + 1], v[:, t:t + 1], one)
+        b.attend(q[:, t], window, sinks)
+        b.mass = torch.where(one[:, None, None] > 0, b.mass, before)  # a stream that got nothing asks nothing
+    assert torch.equal(a.lengths, b.lengths) and a.lengths.tolist() == n.tolist()
+    e = 2 * 2 * weight_error(f64(q), f64(k), D ** -0.5, D, "fp16") + 4 * T * F32
+    assert ((a.mass - b.mass).abs() <= e * b.mass).all()
+    assert np.abs(f64(a.mass.sum((1, 2))) - H * f64(n)).max() <= 1e-3 * H * T
+    # and both keep the same tokens at the evictions that follow
+    for t in range(T, T + more):
+        for c in (a, b):
+            c.append(k[:, t:t + 1], v[:, t:t + 1])
+        x, y = a.attend(q[:, t], window, sinks), b.attend(q[:, t], window, sinks)
+        assert torch.equal(x, y) and torch.equal(a.lengths, b.lengths), t
+
+
+def test_a_prompt_and_steps_keep_what_steps_alone_keep():
+    m = CacheMixer(64, heads=4, kv_heads=2, sinks=3, device=DEV)
+    x = torch.randn((60, 64), generator=gen(6)).half().to(DEV)
+    pos = grid_positions(1, 6, 10, device=DEV)
+    a, b = (m.new_cache(64, keep=40, recent=8) for _ in range(2))
+    m(x[None], pos, a)
+    for t in range(60):
+        m.step(x[t:t + 1], pos[t:t + 1], b)
+    # queries and keys were rounded after products in another order
+    assert rms(a.mass, f64(b.mass)) <= 16 * U[torch.float16]
+    heavy = a.mass[0, :, 3:52].topk(29, 1).indices.sort(1).values
+    kept = a.evict()
+    assert torch.equal(kept[0, :, 3:32].long(), heavy + 3)
+
+
+def test_a_prompt_without_a_budget_weighs_nothing():
+    m = CacheMixer(64, window=9, device=DEV)
+    cache = m.new_cache(40)
+    m(torch.randn((1, 30, 64), device=DEV).half(), grid_positions(1, 5, 6, device=DEV), cache)
+    assert bool((cache.mass == 0).all())
+    cache = CacheMixer(64, device=DEV).new_cache(40)
+    cache.weigh_prompt(torch.ones((1, 30, 4, 64), dtype=torch.float16, device=DEV))
+    assert cache.mass is None
