@@ -114,6 +114,8 @@ class TokenCache:
         columns = -(-capacity // page_size)
         if keep is not None and not 0 < keep < capacity:
             raise ValueError("keep must be in [1, capacity)")
+        if keep is not None and (sinks < 0 or recent < 0 or sinks + recent > keep):
+            raise ValueError("sinks + recent must be in [0, keep]")
         self.capacity, self.keep, self.sinks, self.recent, self.weigh = capacity, keep, sinks, recent, weigh
         self.most = 0  # tokens of the fullest stream, at most: known without asking the GPU,
         self.exact = True  # and just that many as long as all streams get the same
@@ -172,6 +174,8 @@ class TokenCache:
 
     def evict(self):
         """Cuts every stream back to ``keep`` tokens; returns their old positions."""
+        if self.keep is None:
+            raise ValueError("a cache without keep lets go of nothing")
         self.lengths, self.mass, kept = cache_evict(self.k, self.v, self.table, self.lengths, self.mass, self.keep,
                                                     self.free, self.sinks, self.recent)
         self.table, self.free = self.free, self.table
