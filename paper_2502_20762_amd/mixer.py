@@ -143,6 +143,9 @@ class TokenCache:
                 left = min(self.most, self.keep) + T if counts is None else int((self.lengths.clamp(max=self.keep) + new).max())
             if left > self.capacity:  # before anything is let go
                 raise ValueError(f"{T} tokens do not fit: a stream would hold {left}, and the cache has room for {self.capacity}")
+            # of none of these tokens: whatever the write refuses, it does so here
+            none = torch.zeros_like(self.lengths if counts is None else counts)
+            cache_append(k, v, self.k, self.v, self.table, self.lengths, none, self.mass)
             self.evict()
             most = left
         cache_append(k, v, self.k, self.v, self.table, self.lengths, counts, self.mass)

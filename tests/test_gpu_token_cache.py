@@ -161,3 +161,21 @@ def test_a_prompt_without_a_budget_weighs_nothing():
     cache = CacheMixer(64, device=DEV).new_cache(40)
     cache.weigh_prompt(torch.ones((1, 30, 4, 64), dtype=torch.float16, device=DEV))
     assert cache.mass is None
+
+
+def test_a_refused_append_lets_go_of_nothing():
+    s = Streams(2, 12, keep=6, sinks=2, recent=2)
+    s.append([10, 10], given=False)
+    c = s.cache
+    x, two = torch.ones((2, 4, 1, 8), dtype=torch.float16, device=DEV), torch.tensor([2, 1], dtype=torch.int32, device=DEV)
+    mass = c.mass.clone()
+    for bad in ((x.bfloat16(), x.bfloat16()), (x, x.float()), (x[..., :7], x), (x.expand(2, 4, 3, 8), x), (x, x[:, :3]),
+                (x[:1], x[:1]), (x.cpu(), x), (x, x, two.long()), (x, x, two[:1]), (x, x, two.float()), (x, x, two.cpu()),
+                (x, x[..., ::2]), (c.k[:2, :4], x), (x, c.v[:2, :4]), (x.clone().requires_grad_(), x)):
+        table, most = c.table, c.most
+        with pytest.raises((ValueError, RuntimeError)):
+            c.append(*bad)
+        assert c.table is table and c.most == most and c.lengths.tolist() == [10, 10] and torch.equal(c.mass, mass)
+        s.check()
+    s.append([4, 4], given=False)
+    assert c.lengths.tolist() == [10, 10] and c.most == 10
