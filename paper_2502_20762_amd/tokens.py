@@ -7,7 +7,7 @@ value is computed in the HIP kernels.  They take float16 or bfloat16 tensors and
 contiguous) and raise :class:`ValueError` for tensors that do not fit together, :class:`NcodecError` for what the
 library refuses, outputs that overlap an input or each other among it (parts of one buffer may be given, and what a
 function says may be the same).  They have no backward pass: a tensor that requires a gradient is refused where torch records
-gradients, and taken under ``torch.no_grad()``.  ``TokenMixer`` and ``CacheMixer`` run them together: layers that
+gradients, and taken under ``torch.no_grad()``; one with a forward-mode tangent is refused.  ``TokenMixer`` and ``CacheMixer`` run them together: layers that
 read the latents of earlier frames through a state of fixed size, and through a cache of their keys and values.
 """
 from __future__ import annotations
@@ -15,6 +15,7 @@ from __future__ import annotations
 import ctypes
 
 import torch
+import torch.autograd.forward_ad as _forward
 
 from . import ncodec as _nc
 from .ncodec import ACTS, NCODEC_DTYPE_BF16, NCODEC_DTYPE_FP16
@@ -30,9 +31,17 @@ def _need(ok, what):
 _NO_BACKWARD = "no backward pass: call under torch.no_grad(), or with tensors that require no gradient"
 
 
+def _plain(x):
+    """x, looked at inside of a forward-mode level, has no tangent."""
+    if _forward.unpack_dual(x).tangent is not None:
+        raise ValueError("no forward-mode derivative: call with tensors that have no tangent")
+
+
 def _dtype(x):
     if x.requires_grad and torch.is_grad_enabled():
         raise ValueError(_NO_BACKWARD)
+    if _forward._current_level >= 0:
+        _plain(x)
     dt = _DTYPES.get(x.dtype)
     if dt is None or not x.is_cuda:
         raise ValueError(f"tensors must be float16 or bfloat16 on the GPU, not {x.dtype} on {x.device}")
@@ -43,6 +52,8 @@ def _like(t, dtype, device, shape, what):
     """t has this type, device (index) and shape, its last dimension contiguous, and asks for no gradient."""
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(_NO_BACKWARD)
+    if _forward._current_level >= 0:
+        _plain(t)
     if t.dtype != dtype or t.get_device() != device:
         raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {dtype} on cuda:{device}")
     if t.shape != shape:
