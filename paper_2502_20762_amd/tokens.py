@@ -264,7 +264,7 @@ def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None, ou
         out = q.new_empty((B, T, H, V))
     else:
         _like(out, dtype, device, (B, T, H, V), "out")
-    shape = _nc.ncodec_window_shape(dt, H, hk, D, V, D ** -0.5 if scale is None else scale, B, T, _window(window), sinks,
+    shape = _nc.ncodec_window_shape(dt, H, hk, D, V, D ** -0.5 if scale is None else scale, B, T, _window(window), _count(sinks),
                                     *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *out.stride()[:3])
     _call(_nc.load_library().ncodec_window_attention, device, ctypes.byref(shape), q.data_ptr(), k.data_ptr(),
           v.data_ptr(), _ptr(lengths), out.data_ptr())
@@ -275,7 +275,13 @@ def _window(window):
     if window is None:
         return 0
     _need(window >= 1, "a window holds the token itself at least (None: all tokens)")
-    return window
+    return _count(window)
+
+
+def _count(n):
+    """n, for a field of 64 bits, which would keep the lower ones of a larger number."""
+    _need(-1 << 63 <= n < 1 << 63, "a number of tokens has to fit 64 bits")
+    return n
 
 
 def _cache(dtype, device, k_cache, v_cache):
@@ -331,7 +337,7 @@ def paged_attention(q, k_cache, v_cache, page_table, lengths, window=None, sinks
     else:
         _like(out, dtype, device, (B, H, cache.value_dim), "out")
     shape = _nc.ncodec_paged_shape(H, D ** -0.5 if scale is None else scale, B, columns, table_stride, _window(window),
-                                   sinks, *q.stride()[:2], *out.stride()[:2])
+                                   _count(sinks), *q.stride()[:2], *out.stride()[:2])
     lib = _nc.load_library()
     cref, ref = ctypes.byref(cache), ctypes.byref(shape)
     need = lib.ncodec_paged_attention_workspace_bytes(cref, ref, 0 if mass is None else 1)
@@ -394,7 +400,7 @@ def cache_evict(k_cache, v_cache, page_table, lengths, mass, keep, new_table, si
     _mass(new_mass, device, (B, K, new_columns * page), "out[1]")
     _like(kept, torch.int32, device, (B, K, keep), "out[2]")
     _need(kept.is_contiguous(), "out[2] must be contiguous")
-    shape = _nc.ncodec_evict_shape(B, columns, table_stride, new_columns, new_stride, keep, sinks, recent)
+    shape = _nc.ncodec_evict_shape(B, columns, table_stride, new_columns, new_stride, keep, _count(sinks), _count(recent))
     lib = _nc.load_library()
     cref, ref = ctypes.byref(cache), ctypes.byref(shape)
     need = lib.ncodec_cache_evict_workspace_bytes(cref, ref)
