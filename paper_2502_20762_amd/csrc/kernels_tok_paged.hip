@@ -258,7 +258,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_tok_paged(PagedRun run) {
       l += p[e];
     }
     V8 hi, lo;
-    two_terms<E>(p, 1.f, hi, lo);
+    two_terms<E, true>(p, 1.f, hi, lo);
 #pragma unroll
     for (int i = 0; i < VW; ++i) {  // column VW m16 + i of the eight rows
       U4 u;

@@ -6,7 +6,7 @@
 // holds half of one query's scores and its maximum, sum and rescaling are the lane's own;
 // and outputs^T = V^T p^T, whose operand p the accumulators of the scores already are, in
 // the order of keys that a transposed read of V from LDS gives.  Weights enter that product
-// as two 16-bit terms each (22 bits in fp16, 16 in bf16): with one, as many bits as the output,
+// as two 16-bit terms each (22 bits in fp16, 17 in bf16): with one, as many bits as the output,
 // the outputs err 1.4 times as much as their rounding, for 0.74 to 0.85 of the time.
 //
 // A workgroup's four waves share tiles of 64 keys and values in LDS, 32 queries a wave: of
@@ -104,7 +104,7 @@ __device__ __forceinline__ void weight_terms(const float (&w)[8], half8& hi, hal
     lo[i + 1] = (f16)__builtin_fmaf((float)x.y, minus, w[i + 1]);
   }
 }
-__device__ __forceinline__ void weight_terms(const float (&w)[8], bhalf8& hi, bhalf8& lo) { two_terms<BF16>(w, 1.f, hi, lo); }
+__device__ __forceinline__ void weight_terms(const float (&w)[8], bhalf8& hi, bhalf8& lo) { two_terms<BF16, true>(w, 1.f, hi, lo); }
 
 template <class V8>
 __device__ __forceinline__ bool any_not_finite(const V8 (&v)[4], uint32_t inf) {

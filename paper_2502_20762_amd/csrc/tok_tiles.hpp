@@ -54,14 +54,14 @@ __device__ __forceinline__ typename E::V8 read_cols(const char* p0, const char* 
 }
 
 // fp32 values in the unit u, a power of two, as two 16-bit terms, the second the rest of
-// the first: 22 bits in fp16, 16 in bf16.
-template <class E>
+// the first: 22 bits in fp16; in bf16 16, or 17 where the first may be rounded to the nearest (NEAR).
+template <class E, bool NEAR = false>
 __device__ __forceinline__ void two_terms(const float (&x)[8], float u, typename E::V8& hi, typename E::V8& lo) {
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
     const float a = x[i] * u, b = x[i + 1] * u;  // u a power of two: exact, however often it is formed
     typename E::V2 h;
-    if (__is_same(E, F16))
+    if (NEAR || __is_same(E, F16))
       h = {(typename E::T)a, (typename E::T)b};
     else  // bf16 has no unit: the upper halves, which no value close to the end of fp32 rounds up to infinity
       h = __builtin_bit_cast(typename E::V2, __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u));

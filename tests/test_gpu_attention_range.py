@@ -138,3 +138,34 @@ def test_paged_means_of_the_largest_values(n, scale):
         c.v[..., 32:] *= -1
         o = tk.paged_attention(rnd(gen(10), (B, 2, 64), "bf16").to(DEV), c.k, c.v, c.table, i32([n] * B), scale=scale)
         assert bool((o == c.v[0, 0]).all())
+
+
+def nearly_equal(B, dt):
+    """Sequences of three tokens.  The third sees two whose weights differ by 2^-9 of them at most, with values 1 and -1,
+    and itself, heavier and with a value of 0: (queries, keys, values)."""
+    g = gen(12)
+    q, k, v = (torch.zeros((B, 3, 1, 16)) for _ in range(3))
+    q[:, 2, 0, 0], q[:, 2, 0, 1] = 0.7 * torch.rand(B, generator=g), 1.0
+    k[:, :2, 0, 0], k[:, :2, 0, 1] = -1.0, 2.0 ** -9 * torch.rand((B, 2), generator=g)
+    v[:, 0], v[:, 1] = 1.0, -1.0
+    return [x.to(torch.float16 if dt == "fp16" else BF) for x in (q, k, v)]
+
+
+@pytest.mark.parametrize("form", ["prompt", "token"])
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+def test_bits_of_a_weight(form, dt):
+    # a weight's terms hold it to 2^-22 (fp16) and 2^-17 (bf16), its exponential and the sums to 2^-20 together; the
+    # difference of the two, 2^-10 of them, is rounded
+    B = 3000
+    q, k, v = (x.to(DEV) for x in nearly_equal(B, dt))
+    if form == "prompt":
+        o = f64(tk.window_attention(q, k, v, scale=1.0))[:, 2, 0]
+    else:
+        x = torch.zeros((2, B, 4, 1, 16), dtype=q.dtype, device=DEV)
+        x[0, :, :3], x[1, :, :3] = k, v
+        o = f64(tk.paged_attention(q[:, 2], x[0], x[1], torch.arange(B, dtype=torch.int32, device=DEV)[:, None], i32([3] * B), scale=1.0))[:, 0]
+    w = np.exp((f64(q)[:, 2:] * f64(k)).sum((2, 3)))
+    w /= w.sum(1, keepdims=True)
+    want = (w[:, 0] - w[:, 1])[:, None]
+    bound = (2.0 ** (-22 if dt == "fp16" else -17) + 2.0 ** -20) * w[:, :2].sum(1)[:, None] + U[dt] * np.abs(want)
+    assert (np.abs(o - want) <= bound).all(), float((np.abs(o - want) / bound).max())
