@@ -555,8 +555,11 @@ ncodec_status ncodec_decay_attention(const ncodec_decay_shape* shape, const void
  * token and head strides, the last dimension contiguous.  Query head h reads key
  * head h / (heads / kv_heads).  d_lengths: batch int32, the tokens of each
  * sequence, clamped to [0, tokens]; NULL: all.  Past its length a sequence's inputs
- * are not used and its outputs are zero.  Scores, weights and sums are fp32 up to
- * the one rounding of o; scores have to be in the range of fp32.  A NaN or an
+ * are not used and its outputs are zero.  Scores, exponentials and sums are fp32; a weight
+ * meets the values with 22 bits in fp16 (down to 2^-32 of the largest) and with 17 in bf16, and o is
+ * rounded once.  Scores have to be in the range of fp32.  The order of the sums goes by
+ * the shape of the batch: the same sequence in another batch, or token by token over a
+ * cache, has the same outputs up to a rounding.  A NaN or an
  * infinity reaches the tokens that see it and no other; where the formula has an
  * infinity, either of the two may stand.
  * head_dim and value_dim in [1, 128], heads and kv_heads in [1, 4096],

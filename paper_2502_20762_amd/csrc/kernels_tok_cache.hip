@@ -181,7 +181,7 @@ template <int U, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_tok_evict_move(EvictArgs a, Split sp, int64_t first, int64_t blocks) {
   __shared__ Places at;
   // The last positions of what keeps fewer are empty: they take turns over the XCDs and their engines, to
-  // which workgroups go in order (64 sequences of up to 2,040 tokens: 63.1 -> 59.8 us a call).
+  // which workgroups go in order (64 sequences of up to 2,040 tokens: 65.7 -> 61.2 us a call).
   const int64_t block = first + blockIdx.x, bh = block / blocks, x0 = (block + bh + bh / 4) % blocks * sp.rows;
   if (a.kept[bh * a.s.keep + x0] < 0) return;  // the kept ones come first
   move_kept<U, ALIGNED>(a, sp, at, bh, x0, (int)min((int64_t)sp.rows, a.s.keep - x0));

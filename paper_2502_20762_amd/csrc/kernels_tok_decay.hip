@@ -271,11 +271,12 @@ __device__ __forceinline__ float max_finite(float m, const floatx16& v) {
 }
 
 // Operands.  Scores, the state and weighted values are fp32; MFMA operands have 16
-// bits.  They go in as sums of 16-bit terms, each the rest of the one before: two
-// hold 22 bits in fp16 and 16 in bf16, where an output keeps 11 and 8, so that the
-// outputs' own rounding is the only one that counts.  With one term, as many bits as
-// the output, the outputs err 1.4 times as much as their rounding, for 0.88 to 1.1 times
-// the time (130,560 tokens of 16 heads of 128 x 128: 536 us for the last pass, 591 with two).
+// bits.  They go in as sums of two 16-bit terms (two_terms()), which hold 22 bits in
+// fp16 and 16 in bf16, where an output keeps 11 and 8, so that the outputs' own
+// rounding is the only one that counts.  With one term, as many bits as the output,
+// the outputs err 1.4 times as much as their rounding, for 0.88 to 1.1 times the time
+// (130,560 tokens of 16 heads of 128 x 128: 536 us for the last pass, 591 with two).
+//
 // Units.  What becomes an fp16 operand is held in a power-of-two unit, so that
 // neither large nor small magnitudes leave the range in which its terms have
 // their bits.

@@ -14,7 +14,7 @@
 //
 // 64 sequences of up to 8,160 tokens, 4 key heads of 128 + 128, bf16, 557 MB: 119 + 5 us (4.7 TB/s,
 // where a large copy reaches 4.9); one of 130,560, fp16, 267 MB: 54 + 5 (5.0 TB/s); 8 with 4,080 in
-// sight, 8 key heads of 64 + 64, weights summed, 68 MB: 17 + 6.4, of which the start of the
+// sight, 8 key heads of 64 + 64, weights summed, 68 MB: 17 + 6, of which the start of the
 // workgroups, three dependent loads (length, page number, row), takes about 5; one token of 200: 6.5 us,
 // nearly all of it that start and the end.
 #include <algorithm>

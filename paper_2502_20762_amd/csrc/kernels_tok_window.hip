@@ -12,11 +12,11 @@
 // A workgroup's four waves share tiles of 64 keys and values in LDS, 32 queries a wave: of
 // four heads of a group, or of one.  What bounds it is a wave's own sequence of scores,
 // weights and outputs, of which the other wave of the SIMD hides a part: 32,640 tokens of 16
-// heads over 4 of 128 x 128, 8,160 in sight, bf16, 2.0 TFLOP: 2.4 to 2.6 ms (0.8 PFLOP/s, 1.2
-// with the second terms, which is what the library's large product reaches; MFMAs run 60 % of the
-// CUs' busy time, VALU issues 52 %, 30 % of a wave's time goes by at waits and barriers); 8,160
-// tokens of 8 heads of 64 x 64, 4,080 in sight, fp16: 107 to 119 us (MFMAs 42 %, VALU 63 % in a
-// larger case of that kind); 8 ragged sequences of up to 1,560, 8 heads over 2 of 64 x 96: 35 to 37 us.
+// heads over 4 of 128 x 128, 8,160 in sight, bf16, 2.0 TFLOP: 2.4 to 2.7 ms (0.8 PFLOP/s, 1.2
+// with the second terms, which is what the library's large product reaches; MFMAs run 64 % of the
+// CUs' busy time, VALU issues 56 %); 8,160 tokens of 8 heads of 64 x 64, 4,080 in sight, fp16: 107 to
+// 119 us (MFMAs 36 %, VALU 54 %); 8 ragged sequences of up to 1,560, 8 heads over 2 of 64 x 96: 35 to 37 us
+// (39 as a kernel by itself; MFMAs 23 %, VALU 45 %).
 // Tried and no faster there: the next tile's scores beside the weights of this one, weights and
 // products of 16 keys in turn, 64 queries a wave, three waves a SIMD, two or eight waves a workgroup.
 #include <algorithm>
