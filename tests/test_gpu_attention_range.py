@@ -169,3 +169,21 @@ def test_bits_of_a_weight(form, dt):
     want = (w[:, 0] - w[:, 1])[:, None]
     bound = (2.0 ** (-22 if dt == "fp16" else -17) + 2.0 ** -20) * w[:, :2].sum(1)[:, None] + U[dt] * np.abs(want)
     assert (np.abs(o - want) <= bound).all(), float((np.abs(o - want) / bound).max())
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("shift", [-2.0, 0.0, 2.0])
+@pytest.mark.parametrize("d", [-4.0, -1.0, 1.0, 4.0])
+def test_window_scores_around_the_border_of_large_ones(d, shift, dt):
+    # two tiles of 64 keys, each of two waves' own, whose scores of 2^22 ln 2 and d more are taken for large or not; a score
+    # there errs by a quarter of a power of two, for the rounded product, at most
+    for sign in (1.0, -1.0):
+        q, k, v = (torch.zeros((1, 128, 1, 16)) for _ in range(3))
+        q[..., 0], q[..., 1], k[..., 0] = 32.0, 2.0 ** -5, 32.0
+        scale = sign * (2.0 ** 22 * np.log(2) + shift) / 1024
+        k[0, 64:, 0, 1] = d / scale * 32
+        v[0, :64] = 1.0
+        q, k, v = (x.to(torch.float16 if dt == "fp16" else BF).to(DEV) for x in (q, k, v))
+        o = f64(tk.window_attention(q, k, v, scale=float(scale)))[0, 127, 0]
+        delta = f64(k)[0, 127, 0, 1] * scale / 32
+        assert (np.abs(np.log(o / (1 - o)) + delta) <= 0.5 * np.log(2) + 2 * U[dt] / min(o[0], 1 - o[0])).all(), (sign, o)
